@@ -32,7 +32,7 @@
  *     k_scale, v_scale [num_blocks] fp32               (FP8 caches only)
  *     block_tables [num_seqs][max_blocks_per_seq] int32 physical block ids
  *     seq_lens   [num_seqs] int32
- *     out        [num_seqs][Hq][D] fp32
+ *     out        [num_seqs][Hq][D] fp32 or bf16 (out_dtype)
  * - Semantics (Sec. 3.1 generation step): seq_lens[b] counts the cached
  *   tokens of beam b including the current one (its K/V are already in the
  *   cache). Query head h uses KV head h / (Hq / Hkv). The result is
@@ -42,6 +42,13 @@
  *   slots of a partially filled last block.
  * - FP8 KV: OCP E4M3FN codes; the value of a code in block p is
  *   decode(code) * k_scale[p] (keys) or * v_scale[p] (values).
+ * - MXFP4 KV (OCP Microscaling): E2M1 codes, two to a byte, the lower half
+ *   first, and one E8M0 scale byte e per 32 consecutive head dims of a token;
+ *   the value of a code is decode(code) * 2^(e - 127) (e = 255: NaN). Of each
+ *   (block, KV head) the cache holds the 16 * D codes, in the order above
+ *   (keys token-major, values dim-major), then the 16 * D / 32 scales (keys
+ *   [16][D / 32], values [D / 32][16]): 8.5 * D bytes, so a cache is
+ *   [num_blocks][Hkv][17 * D / 2] bytes. k_scale and v_scale are NULL.
  * - Device-side errors: a block id outside [0, num_blocks) read from a
  *   device table (any entry in the paged call; an entry appended after the
  *   metadata was built in the prefix call -- entries in use at build time
@@ -72,11 +79,12 @@ typedef enum {
   TTS_ERR_NOMEM = -6
 } tts_status;
 
-typedef enum { TTS_F32 = 0, TTS_BF16 = 1, TTS_FP8_E4M3 = 2 } tts_dtype;
+typedef enum { TTS_F32 = 0, TTS_BF16 = 1, TTS_FP8_E4M3 = 2, TTS_MXFP4 = 3 } tts_dtype;
 
 /* Attention shape. Supported: Hq % Hkv == 0, head_dim 64 or 128,
- * block_size 16; (q, kv) dtypes (F32, F32), (BF16, BF16), (BF16, FP8_E4M3);
- * out_dtype F32. scale <= 0 selects 1/sqrt(head_dim). */
+ * block_size 16; (q, kv) dtypes (F32, F32), (BF16, BF16), (BF16, FP8_E4M3),
+ * (BF16, MXFP4); out_dtype F32 or BF16 (rounded once from fp32). scale <= 0
+ * selects 1/sqrt(head_dim). */
 typedef struct {
   int32_t num_q_heads;
   int32_t num_kv_heads;
@@ -281,7 +289,7 @@ tts_status tts_build_verify_meta(int32_t num_reqs, const int32_t* req_seq_offset
                                  int32_t q_len, int32_t block_size, int32_t num_blocks, const tts_attn_desc* desc,
                                  hipStream_t stream, tts_prefix_meta** out);
 
-/* q: [num_seqs][q_len][Hq][D], out: [num_seqs][q_len][Hq][D] fp32;
+/* q: [num_seqs][q_len][Hq][D], out: [num_seqs][q_len][Hq][D] fp32 or bf16;
  * block_tables [num_seqs][max_blocks_per_seq] and seq_lens [num_seqs] are
  * the beams' own (device); the other arguments and rules are those of
  * tts_prefix_decode_attn (which refuses a verification metadata). The
@@ -291,6 +299,35 @@ tts_status tts_prefix_verify_attn(const tts_attn_desc* d, const tts_prefix_meta*
                                   const float* v_scale, const int32_t* block_tables, int32_t max_blocks_per_seq,
                                   const int32_t* seq_lens, int32_t num_blocks, void* out, void* workspace,
                                   size_t workspace_bytes, hipStream_t stream);
+
+/* ---- Prefill attention ------------------------------------------------------
+ *
+ * Causal attention of a chunk of every sequence's last tokens over its paged
+ * cache, of any length: the prompts and reasoning steps that a verifier reads
+ * (its requests are prefills, Sec. 2.2 and 4.3) and a generator's prompts.
+ * tok_offsets, num_tokens and seq_lens as for tts_rope_append_kv (which has
+ * stored the chunk's keys and values): query i of sequence b, row
+ * tok_offsets[b] + i, is token seq_lens[b] - n_b + i and attends to the tokens
+ * 0 .. itself. What is stored at tokens that a query does not see, infinities
+ * and NaN included, does not reach its row.
+ *   q [num_tokens][Hq][D], out [num_tokens][Hq][D]; rows behind the last
+ *     sequence's are left as they are; both and the caches aligned to 16 bytes.
+ *   max_seq_len: host upper bound on seq_lens.
+ *   workspace: at least tts_paged_prefill_workspace_size bytes (chunks of few
+ *     rows are split over the tokens; 0 and NULL otherwise). Calls that
+ *     overlap in time must not share one.
+ * Device-side errors: a sequence longer than max_seq_len or its table row, or
+ * shorter than its new tokens, has NaN rows (seq_len <= 0: zero rows); a block
+ * id outside [0, num_blocks) makes the rows that see the block NaN. More than
+ * 2^31 - 1 query rows (num_tokens * Hq) are TTS_ERR_UNSUPPORTED. */
+size_t tts_paged_prefill_workspace_size(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens,
+                                        int32_t max_seq_len);
+tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens,
+                                  const int32_t* tok_offsets, const void* q, const void* k_cache, const void* v_cache,
+                                  const float* k_scale, const float* v_scale, const int32_t* block_tables,
+                                  int32_t max_blocks_per_seq, const int32_t* seq_lens, int32_t max_seq_len,
+                                  int32_t num_blocks, void* out, void* workspace, size_t workspace_bytes,
+                                  hipStream_t stream);
 
 /* The two launches of tts_prefix_decode_attn, for callers that schedule
  * them separately (to overlap the merge with other work, or to time the
@@ -341,6 +378,67 @@ tts_status tts_append_kv(const tts_attn_desc* d, int32_t num_seqs, const void* k
                          const int32_t* block_tables, int32_t max_blocks_per_seq, const int32_t* seq_lens,
                          int32_t num_blocks, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
                          hipStream_t stream);
+
+/* MXFP4 caches: the token's values are quantised in groups of 32 dims, each
+ * by itself (no other token is read or changed): e = floor(log2(amax)) - 2 +
+ * 127, at least 1, of the group's largest magnitude, and codes nearest to
+ * value / 2^(e - 127), ties to even, saturating at +-6. A group that holds an
+ * infinity or NaN gets e = 255 and reads back as NaN. */
+
+/* Rotary position embedding: pair i (i < rot_dim / 2) of a head at position t
+ * is turned by the angle whose cosine and sine are cos[t][i] and sin[t][i]:
+ *   (x, y) -> (x cos - y sin, y cos + x sin),
+ * each product and the sum rounded to fp32. Pairs are dims (i, i + rot_dim / 2),
+ * or with interleaved = 1 dims (2i, 2i + 1); dims from rot_dim on are left as
+ * they are. */
+typedef struct {
+  int32_t rot_dim;     /* even, 0 <= rot_dim <= head_dim */
+  int32_t interleaved; /* 0 or 1 */
+  int32_t max_pos;     /* rows of the tables */
+  const float* cos;    /* device, [max_pos][rot_dim / 2] */
+  const float* sin;
+} tts_rope_desc;
+
+/* Host: the tables of the usual angles t * theta^(-2i / rot_dim), computed in
+ * double. cos and sin are host arrays [max_pos][rot_dim / 2]. */
+tts_status tts_rope_tables(int32_t rot_dim, double theta, int32_t max_pos, float* cos, float* sin);
+
+/* Append with rotation: the new tokens of every sequence, each rotated by its
+ * position and stored in the cache, and the queries rotated beside them: what
+ * a layer does between its projections and its attention, for the one token
+ * of a decode step (tok_offsets NULL: row b is sequence b's, and num_tokens is
+ * num_seqs), the few of a verification and the chunks of a prefill.
+ *   tok_offsets [num_seqs + 1] (device): rows tok_offsets[b] ..
+ *     tok_offsets[b + 1] are the new tokens of sequence b, which are its last
+ *     n_b of seq_lens[b] tokens; tok_offsets[0] is 0, offsets do not decrease
+ *     and end at most at num_tokens. Rows behind the last one are neither
+ *     read nor written (padded batches).
+ *   positions [num_tokens] (device) or NULL: the rows of the rotation tables;
+ *     NULL: each token's index in its sequence.
+ *   q, k_new, v_new: rows of Hq, Hkv and Hkv heads, bf16 (F32 caches: fp32),
+ *     q_stride, k_stride and v_stride elements from one token to the next, so
+ *     that the three may lie in one projection's output. q may be NULL.
+ *   q_out [num_tokens][Hq][D], in q's type; may be q itself (without gaps).
+ *   rope: NULL appends keys as they are (then q and positions are NULL too).
+ * Keys and values are stored as by tts_append_kv, from the fp32 value of the
+ * rotation, except that an FP8 block's scale is set or raised once for all of
+ * the call's tokens in it (and its earlier codes re-encoded once): with one
+ * token per sequence it is the same.
+ * A sequence with seq_len <= 0 is idle: none of its rows is read or written.
+ * Device-side errors: a sequence shorter than its new tokens stores nothing
+ * and its queries are NaN; a position outside [0, max_pos) makes its token's
+ * queries NaN and stores nothing of it; a block index past the table row or a
+ * block id outside [0, num_blocks) stores nothing. As for tts_append_kv, the
+ * blocks that new tokens go to belong to one sequence each. The caches are
+ * aligned to 16 bytes. Rows of 16-byte alignment (and rot_dim a multiple of
+ * 16, interleaved 8) are read eight elements at a time, others one by one.
+ * More than 8192 query heads are TTS_ERR_UNSUPPORTED. */
+tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope, int32_t num_seqs, int32_t num_tokens,
+                              const int32_t* tok_offsets, const int32_t* positions, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                              const int32_t* block_tables, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                              int32_t num_blocks, void* q_out, void* k_cache, void* v_cache, float* k_scale,
+                              float* v_scale, hipStream_t stream);
 
 /* Copy whole blocks: for each i < num_pairs, K and V of every KV head of
  * block pairs[2i] into block pairs[2i + 1] (and the fp8 scales). pairs is a

@@ -12,6 +12,7 @@ from .tts import (  # noqa: F401
     PrefixMeta,
     load,
     make_desc,
+    make_rope,
     tts_append_kv,
     tts_build_prefix_meta,
     tts_build_verify_meta,
@@ -25,6 +26,8 @@ from .tts import (  # noqa: F401
     tts_prefix_verify_attn,
     tts_paged_decode_attn,
     tts_paged_decode_workspace_size,
+    tts_paged_prefill_attn,
+    tts_paged_prefill_workspace_size,
     tts_prefix_decode_attn,
     tts_prefix_decode_attn_noalloc,
     tts_prefix_decode_merge,
@@ -35,4 +38,6 @@ from .tts import (  # noqa: F401
     tts_prefix_meta_export,
     tts_prefix_meta_stats,
     tts_plan_units_host,
+    tts_rope_append_kv,
+    tts_rope_tables,
 )

@@ -11,13 +11,17 @@
 #include <vector>
 
 #include "tts.h"
+#include "tts_kv.h"
 #include "tts_meta.h"
+#include "tts_prefill.h"
 #include "tts_work.h"
 
 namespace tts {
 hipError_t launch_attn(const AttnParams& p, int grid, int head_dim, int kv_kind, hipStream_t stream);
 hipError_t launch_merge(const MergeParams& p, int head_dim, int kv_kind, hipStream_t stream);
 hipError_t scratch_buffer(void** ptr, size_t* bytes);
+hipError_t launch_rope_append(RopeParams p, int kv_kind, hipStream_t stream);
+hipError_t launch_prefill(const PrefillParams& p, int head_dim, int kv_kind, hipStream_t stream);
 hipError_t launch_append(const void* k_new, const void* v_new, const int32_t* block_tables, const int32_t* seq_lens,
                          void* k_cache, void* v_cache, float* k_scale, float* v_scale, int num_seqs, int max_blocks,
                          int num_blocks, int hkv, int head_dim, int kv_kind, hipStream_t stream);
@@ -64,6 +68,8 @@ tts_status ok() {
 
 // Paged path: blocks per split of a long sequence.
 constexpr int32_t kPagedSplitBlocks = 32;
+// Query heads of a rotating append: the parts of its grid stay below 65,536.
+constexpr int32_t kMaxRopeHeads = 8192;
 
 tts_status check_desc(const tts_attn_desc* d) {
   if (!d) return fail(TTS_ERR_INVALID_ARG, "desc is NULL");
@@ -74,15 +80,25 @@ tts_status check_desc(const tts_attn_desc* d) {
   if (d->head_dim != 64 && d->head_dim != 128) return fail(TTS_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
   if (d->block_size != 16) return fail(TTS_ERR_UNSUPPORTED, "block_size must be 16");
   const bool f32 = d->q_dtype == TTS_F32 && d->kv_dtype == TTS_F32;
-  const bool bf = d->q_dtype == TTS_BF16 && (d->kv_dtype == TTS_BF16 || d->kv_dtype == TTS_FP8_E4M3);
+  const bool bf = d->q_dtype == TTS_BF16 &&
+                  (d->kv_dtype == TTS_BF16 || d->kv_dtype == TTS_FP8_E4M3 || d->kv_dtype == TTS_MXFP4);
   if (!f32 && !bf) return fail(TTS_ERR_UNSUPPORTED, "unsupported (q_dtype, kv_dtype) combination");
-  if (d->out_dtype != TTS_F32) return fail(TTS_ERR_UNSUPPORTED, "out_dtype must be F32");
+  if (d->out_dtype != TTS_F32 && d->out_dtype != TTS_BF16)
+    return fail(TTS_ERR_UNSUPPORTED, "out_dtype must be F32 or BF16");
   if (!std::isfinite(d->scale)) return fail(TTS_ERR_INVALID_ARG, "scale is not finite");
   return TTS_OK;
 }
 
-int kv_kind(const tts_attn_desc* d) { return d->kv_dtype == TTS_F32 ? 0 : (d->kv_dtype == TTS_BF16 ? 1 : 2); }
+int kv_kind(const tts_attn_desc* d) { return static_cast<int>(d->kv_dtype); }  // KvKind's order
+// Bytes of a cached element as the planner prices it: 4-bit caches are
+// converted code by code as fp8 ones are, and take their cost terms.
 int kv_bytes(const tts_attn_desc* d) { return d->kv_dtype == TTS_F32 ? 4 : (d->kv_dtype == TTS_BF16 ? 2 : 1); }
+// Bytes of one block of K (all KV heads), = V's.
+int64_t block_bytes(const tts_attn_desc* d) {
+  const int64_t elems = static_cast<int64_t>(d->num_kv_heads) * d->block_size * d->head_dim;
+  if (d->kv_dtype == TTS_MXFP4) return elems / 2 + elems / 32;  // codes, and a scale byte to 32 of them
+  return elems * kv_bytes(d);
+}
 
 float scale_log2(const tts_attn_desc* d) {
   const double s = d->scale > 0.f ? d->scale : 1.0 / std::sqrt(static_cast<double>(d->head_dim));
@@ -450,7 +466,7 @@ tts_status tts_paged_decode_attn(const tts_attn_desc* d, int32_t num_seqs, const
   p.v_scale = v_scale;
   p.block_tables = block_tables;
   p.seq_lens = seq_lens;
-  p.out = static_cast<float*>(out);
+  p.out = out;
   p.part_o = ns > 1 ? workspace : nullptr;
   p.part_ml = ns > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + part_o_bytes(d, rows))
                      : nullptr;
@@ -466,6 +482,7 @@ tts_status tts_paged_decode_attn(const tts_attn_desc* d, int32_t num_seqs, const
   p.paged_max_len = max_seq_len;
   p.q_len = 1;
   p.two_windows = 0;
+  p.out_bf16 = d->out_dtype == TTS_BF16;
   const int64_t units = static_cast<int64_t>(num_seqs) * d->num_kv_heads * ns;
   if (units > 0x7FFFFFFF) return fail(TTS_ERR_UNSUPPORTED, "grid too large");
   hipError_t e = tts::launch_attn(p, static_cast<int>(units), d->head_dim, kv_kind(d), stream);
@@ -481,6 +498,7 @@ tts_status tts_paged_decode_attn(const tts_attn_desc* d, int32_t num_seqs, const
     mp.g = d->num_q_heads / d->num_kv_heads;
     mp.paged_nsplit = ns;
     mp.q_len = 1;
+    mp.out_bf16 = p.out_bf16;
     e = tts::launch_merge(mp, d->head_dim, kv_kind(d), stream);
     if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("merge launch: ") + hipGetErrorString(e));
   }
@@ -533,7 +551,7 @@ tts_status prefix_params(const tts_attn_desc* d, const tts_prefix_meta* m, const
   p->v_scale = v_scale;
   p->block_tables = block_tables;
   p->seq_lens = seq_lens;
-  p->out = static_cast<float*>(out);
+  p->out = out;
   p->part_o = workspace;
   p->part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_o_bytes(d, rows));
   p->recs = reinterpret_cast<const tts::UnitRec*>(dev + m->off_recs);
@@ -548,6 +566,7 @@ tts_status prefix_params(const tts_attn_desc* d, const tts_prefix_meta* m, const
   p->scale_log2 = scale_log2(d);
   p->q_len = m->q_len;
   p->two_windows = m->plan.two_windows ? 1 : 0;
+  p->out_bf16 = d->out_dtype == TTS_BF16;
   return TTS_OK;
 }
 
@@ -574,6 +593,7 @@ tts_status launch_prefix_merge(const tts_attn_desc* d, const tts_prefix_meta* m,
   mp.g = p.g;
   mp.q_len = p.q_len;
   mp.rows_per_head = p.rows_per_head;
+  mp.out_bf16 = p.out_bf16;
   hipError_t e = tts::launch_merge(mp, d->head_dim, kv_kind(d), stream);
   if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("merge launch: ") + hipGetErrorString(e));
   return TTS_OK;
@@ -662,6 +682,87 @@ tts_status tts_prefix_decode_merge(const tts_attn_desc* d, const tts_prefix_meta
   return ok();
 }
 
+// ---- ragged prefill ------------------------------------------------------------
+
+// Splits of every tile of rows over its tokens: as many as fill the card's
+// 256 compute units with two workgroups each.
+static int32_t prefill_nsplit(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens, int32_t max_seq_len) {
+  const int64_t g = d->num_q_heads / d->num_kv_heads;
+  const int64_t units = tts::prefill_items(num_seqs, num_tokens, g) * d->num_kv_heads;
+  const int64_t fill = units > 0 ? 512 / units : 1;
+  const int64_t fit = max_seq_len / tts::kPrefillSplitTokens;
+  const int64_t n = std::min({fill, fit, static_cast<int64_t>(tts::kPrefillMaxSplit)});
+  return n < 1 ? 1 : static_cast<int32_t>(n);
+}
+
+static size_t prefill_rows(const tts_attn_desc* d, int32_t num_tokens) {
+  return static_cast<size_t>(num_tokens) * d->num_q_heads;
+}
+
+size_t tts_paged_prefill_workspace_size(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens,
+                                        int32_t max_seq_len) {
+  if (!d || check_desc(d) != TTS_OK || num_seqs < 0 || num_tokens < 0 || max_seq_len < 0) return 0;
+  const size_t ns = prefill_nsplit(d, num_seqs, num_tokens, max_seq_len);
+  if (ns == 1) return 0;
+  const size_t rows = ns * prefill_rows(d, num_tokens);
+  return align256(rows * d->head_dim * 4) + align256(rows * 8);
+}
+
+tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens,
+                                  const int32_t* tok_offsets, const void* q, const void* k_cache, const void* v_cache,
+                                  const float* k_scale, const float* v_scale, const int32_t* block_tables,
+                                  int32_t max_blocks_per_seq, const int32_t* seq_lens, int32_t max_seq_len,
+                                  int32_t num_blocks, void* out, void* workspace, size_t workspace_bytes,
+                                  hipStream_t stream) {
+  tts_status s = check_desc(d);
+  if (s != TTS_OK) return s;
+  if ((s = check_scales(d, k_scale, v_scale)) != TTS_OK) return s;
+  if (num_seqs < 0 || num_tokens < 0 || max_blocks_per_seq < 0 || max_seq_len < 0 || num_blocks < 0)
+    return fail(TTS_ERR_INVALID_ARG, "negative size");
+  if (static_cast<int64_t>(max_seq_len) > static_cast<int64_t>(max_blocks_per_seq) * 16)
+    return fail(TTS_ERR_INVALID_ARG, "max_seq_len exceeds max_blocks_per_seq * block_size");
+  if (static_cast<int64_t>(num_tokens) * d->num_q_heads > 0x7FFFFFFF)
+    return fail(TTS_ERR_UNSUPPORTED, "more than 2^31 - 1 query rows");
+  if (num_seqs == 0 || num_tokens == 0) return ok();
+  if (!tok_offsets || !q || !k_cache || !v_cache || !block_tables || !seq_lens || !out)
+    return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
+  for (const void* x : {q, k_cache, v_cache, const_cast<const void*>(out)})
+    if (reinterpret_cast<uintptr_t>(x) % 16 != 0)
+      return fail(TTS_ERR_INVALID_ARG, "q, out and the caches must be aligned to 16 bytes");
+  const size_t need = tts_paged_prefill_workspace_size(d, num_seqs, num_tokens, max_seq_len);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(TTS_ERR_WORKSPACE, "workspace smaller than tts_paged_prefill_workspace_size");
+  tts::PrefillParams p{};
+  p.q = q;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.tok_offsets = tok_offsets;
+  p.block_tables = block_tables;
+  p.seq_lens = seq_lens;
+  p.out = out;
+  p.num_seqs = num_seqs;
+  p.num_tokens = num_tokens;
+  p.max_blocks = max_blocks_per_seq;
+  p.num_blocks = num_blocks;
+  p.max_seq_len = max_seq_len;
+  p.hq = d->num_q_heads;
+  p.hkv = d->num_kv_heads;
+  p.g = d->num_q_heads / d->num_kv_heads;
+  p.nsplit = prefill_nsplit(d, num_seqs, num_tokens, max_seq_len);
+  p.out_bf16 = d->out_dtype == TTS_BF16;
+  p.scale_log2 = scale_log2(d);
+  if (p.nsplit > 1) {
+    p.part_o = static_cast<float*>(workspace);
+    p.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                         align256(p.nsplit * prefill_rows(d, num_tokens) * d->head_dim * 4));
+  }
+  const hipError_t e = tts::launch_prefill(p, d->head_dim, kv_kind(d), stream);
+  if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("prefill launch: ") + hipGetErrorString(e));
+  return ok();
+}
+
 // ---- KV maintenance ----------------------------------------------------------
 
 tts_status tts_append_kv(const tts_attn_desc* d, int32_t num_seqs, const void* k_new, const void* v_new,
@@ -675,9 +776,103 @@ tts_status tts_append_kv(const tts_attn_desc* d, int32_t num_seqs, const void* k
   if (num_seqs == 0) return ok();
   if (!k_new || !v_new || !block_tables || !seq_lens || !k_cache || !v_cache)
     return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
+  if (d->kv_dtype == TTS_MXFP4) {
+    const int64_t token = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
+    return tts_rope_append_kv(d, nullptr, num_seqs, num_seqs, nullptr, nullptr, nullptr, 0, k_new, token, v_new, token,
+                              block_tables, max_blocks_per_seq, seq_lens, num_blocks, nullptr, k_cache, v_cache,
+                              nullptr, nullptr, stream);
+  }
   hipError_t e = tts::launch_append(k_new, v_new, block_tables, seq_lens, k_cache, v_cache, k_scale, v_scale, num_seqs,
                                     max_blocks_per_seq, num_blocks, d->num_kv_heads, d->head_dim, kv_kind(d), stream);
   if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("append launch: ") + hipGetErrorString(e));
+  return ok();
+}
+
+tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope, int32_t num_seqs, int32_t num_tokens,
+                              const int32_t* tok_offsets, const int32_t* positions, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                              const int32_t* block_tables, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                              int32_t num_blocks, void* q_out, void* k_cache, void* v_cache, float* k_scale,
+                              float* v_scale, hipStream_t stream) {
+  tts_status s = check_desc(d);
+  if (s != TTS_OK) return s;
+  if ((s = check_scales(d, k_scale, v_scale)) != TTS_OK) return s;
+  if (num_seqs < 0 || num_tokens < 0 || max_blocks_per_seq < 0 || num_blocks < 0)
+    return fail(TTS_ERR_INVALID_ARG, "negative size");
+  if (!tok_offsets && num_tokens != num_seqs)
+    return fail(TTS_ERR_INVALID_ARG, "without tok_offsets num_tokens must be num_seqs");
+  if (d->num_q_heads > kMaxRopeHeads) return fail(TTS_ERR_UNSUPPORTED, "more than 8192 query heads");
+  if (rope) {
+    if (rope->rot_dim < 0 || rope->rot_dim % 2 != 0 || rope->rot_dim > d->head_dim)
+      return fail(TTS_ERR_INVALID_ARG, "rot_dim must be even and lie in [0, head_dim]");
+    if (rope->max_pos < 0) return fail(TTS_ERR_INVALID_ARG, "negative max_pos");
+    if (rope->interleaved != 0 && rope->interleaved != 1)
+      return fail(TTS_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  }
+  const bool turned = rope && rope->rot_dim > 0;
+  if (!rope && (q || q_out || positions))
+    return fail(TTS_ERR_INVALID_ARG, "queries and positions need a rotation (rope is NULL)");
+  if ((q != nullptr) != (q_out != nullptr)) return fail(TTS_ERR_INVALID_ARG, "q and q_out go together");
+  const int64_t kv_token = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
+  const int64_t q_token = static_cast<int64_t>(d->num_q_heads) * d->head_dim;
+  if (k_stride < kv_token || v_stride < kv_token || (q && q_stride < q_token))
+    return fail(TTS_ERR_INVALID_ARG, "a token stride is smaller than a token");
+  if (q && q == q_out && q_stride != q_token)
+    return fail(TTS_ERR_INVALID_ARG, "queries are rotated in place only without gaps (q_stride)");
+  if (num_seqs == 0 || num_tokens == 0) return ok();
+  if (!k_new || !v_new || !block_tables || !seq_lens || !k_cache || !v_cache ||
+      (turned && rope->max_pos > 0 && (!rope->cos || !rope->sin)))
+    return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
+  if (reinterpret_cast<uintptr_t>(k_cache) % 16 != 0 || reinterpret_cast<uintptr_t>(v_cache) % 16 != 0)
+    return fail(TTS_ERR_INVALID_ARG, "caches must be aligned to 16 bytes");
+  tts::RopeParams p{};
+  p.q = q;
+  p.k_new = k_new;
+  p.v_new = v_new;
+  p.q_out = q_out;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.tok_offsets = tok_offsets;
+  p.positions = positions;
+  p.block_tables = block_tables;
+  p.seq_lens = seq_lens;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.num_seqs = num_seqs;
+  p.num_tokens = num_tokens;
+  p.max_blocks = max_blocks_per_seq;
+  p.num_blocks = num_blocks;
+  p.hq = d->num_q_heads;
+  p.hkv = d->num_kv_heads;
+  p.head_dim = d->head_dim;
+  if (turned) {
+    p.rot = rope->rot_dim;
+    p.interleaved = rope->interleaved;
+    p.max_pos = rope->max_pos;
+    p.cos = rope->cos;
+    p.sin = rope->sin;
+  }
+  const hipError_t e = tts::launch_rope_append(p, kv_kind(d), stream);
+  if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("append launch: ") + hipGetErrorString(e));
+  return ok();
+}
+
+tts_status tts_rope_tables(int32_t rot_dim, double theta, int32_t max_pos, float* cos, float* sin) {
+  if (rot_dim < 0 || rot_dim % 2 != 0 || max_pos < 0)
+    return fail(TTS_ERR_INVALID_ARG, "rot_dim must be even and >= 0, max_pos >= 0");
+  if (!(theta > 0) || !std::isfinite(theta)) return fail(TTS_ERR_INVALID_ARG, "theta must be finite and > 0");
+  if (rot_dim > 0 && max_pos > 0 && (!cos || !sin)) return fail(TTS_ERR_INVALID_ARG, "NULL host array");
+  const int32_t half = rot_dim / 2;
+  for (int32_t i = 0; i < half; ++i) {
+    const double inv = std::pow(theta, -static_cast<double>(i) / half);
+    for (int32_t t = 0; t < max_pos; ++t) {
+      cos[static_cast<int64_t>(t) * half + i] = static_cast<float>(std::cos(t * inv));
+      sin[static_cast<int64_t>(t) * half + i] = static_cast<float>(std::sin(t * inv));
+    }
+  }
   return ok();
 }
 
@@ -689,10 +884,8 @@ tts_status tts_copy_blocks(const tts_attn_desc* d, int32_t num_pairs, const int3
   if (num_pairs < 0 || num_blocks < 0) return fail(TTS_ERR_INVALID_ARG, "negative size");
   if (num_pairs == 0) return ok();
   if (!pairs || !k_cache || !v_cache) return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
-  const int64_t eb = d->kv_dtype == TTS_F32 ? 4 : (d->kv_dtype == TTS_BF16 ? 2 : 1);
-  const int64_t blk_bytes = static_cast<int64_t>(d->num_kv_heads) * d->block_size * d->head_dim * eb;
-  hipError_t e = tts::launch_copy_blocks(pairs, num_pairs, k_cache, v_cache, k_scale, v_scale, blk_bytes, num_blocks,
-                                         stream);
+  hipError_t e = tts::launch_copy_blocks(pairs, num_pairs, k_cache, v_cache, k_scale, v_scale, block_bytes(d),
+                                         num_blocks, stream);
   if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("copy launch: ") + hipGetErrorString(e));
   return ok();
 }

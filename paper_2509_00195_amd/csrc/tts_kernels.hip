@@ -62,6 +62,7 @@
 #include <mutex>
 #include <type_traits>
 
+#include "tts_device.h"
 #include "tts_work.h"
 
 namespace tts {
@@ -80,12 +81,6 @@ __device__ uint64_t g_prof[kProfSlots][8];
 #define TTS_PROF_MARK(k, i) do {} while (0)
 #endif
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kTok = 16;  // tokens per KV block
 constexpr int kThreads = 64 * kUnitWaves;
 constexpr int kWaves = kThreads / 64;
 constexpr int kTiles = kMaxRows / 16;
@@ -95,43 +90,19 @@ constexpr float kNegInf = -__builtin_inff();
 constexpr float kInf = __builtin_inff();
 constexpr float kRefWindow = 64.0f;  // |row max| (log2 units) handled with m_ref = 0
 
-enum KvKind : int { kKvF32 = 0, kKvBf16 = 1, kKvFp8 = 2 };
-
-template <int KV>
-struct KvBytes {
-  static constexpr int value = KV == kKvF32 ? 4 : (KV == kKvBf16 ? 2 : 1);
-};
-
 template <int D, int KV>
-struct Geo {
-  static constexpr int eb = KvBytes<KV>::value;
-  static constexpr int row_bytes = D * eb;           // one token of K
-  static constexpr int blk_bytes = kTok * row_bytes;  // one (block, head) of K or V
-  static constexpr int vrow_bytes = kTok * eb;        // one dim of V (16 tokens)
+struct Geo : KvGeo<D, KV> {
   // End-of-unit combine: per (wave, tile) 16 rows of D floats padded by 4
   // (bank spread), then m and l.
   static constexpr int comb_row = D + 4;
   static constexpr int comb_floats = kTok * comb_row + 2 * kTok;
 };
 
+// Caches that are converted to bf16 on the way to the products.
+template <int KV>
+constexpr bool kCoded = KV == kKvFp8 || KV == kKvMx4;
+
 __device__ __forceinline__ uint32_t f32_bits(float x) { return __builtin_bit_cast(uint32_t, x); }
-
-// Two OCP E4M3 codes (byte pair kHi of w) -> two bf16 in one dword, in one
-// conversion instruction with unit scale. Every E4M3 value fits bf16
-// exactly, so the conversion is exact.
-template <bool kHi>
-__device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t w) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, kHi));
-}
-
-__device__ __forceinline__ uint4 fp8x8_to_bf16x8(uint2 w) {
-  return uint4{fp8x2_to_bf16x2<false>(w.x), fp8x2_to_bf16x2<true>(w.x), fp8x2_to_bf16x2<false>(w.y),
-               fp8x2_to_bf16x2<true>(w.y)};
-}
-
-__device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));  // RNE
-}
 
 __device__ __forceinline__ float xlane_max16(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -286,8 +257,30 @@ struct Fp8Frags {
   uint2 v[D / 16][1];
 };
 
+// 4-bit caches: raw codes and scale bytes. A lane's dims of a token are one
+// run of D / 4 (one 16-byte load for D = 128, all under one scale), so K's
+// dims are taken in another order than for the other caches:
+//   k[t]: token pair_token(t, ln), dims (D / 4) lq .. + D / 4; ks[t]: their scale byte;
+//   v[dt]: as above; vs[i]: the scale bytes of tokens 8 lq .. + 8, dims 32 i .. + 32.
+template <int D>
+struct Mx4Frags {
+  typedef typename std::conditional<D == 128, uint4, uint2>::type T;
+  T k[2];
+  uint32_t ks[2];
+  uint32_t v[D / 16];
+  uint2 vs[D / kMxGroup];
+};
+
 template <int D, int KV>
-using Frags = typename std::conditional<KV == kKvFp8, Fp8Frags<D>, Ops<D, KV>>::type;
+using Frags = typename std::conditional<KV == kKvMx4, Mx4Frags<D>,
+                                        typename std::conditional<KV == kKvFp8, Fp8Frags<D>, Ops<D, KV>>::type>::type;
+
+// The 8 dims that step j of the score product takes from lane quarter lq, as
+// a column of 8 of the query row (and of the K row).
+template <int D, int KV>
+__device__ __forceinline__ int dim_col(int j, int lq) {
+  return KV == kKvMx4 ? D / 32 * lq + j : 4 * j + lq;
+}
 
 template <int D, int KV>
 __device__ __forceinline__ void load_k(Frags<D, KV>& f, const unsigned char* kb0, const unsigned char* kb1, int ln,
@@ -298,10 +291,16 @@ __device__ __forceinline__ void load_k(Frags<D, KV>& f, const unsigned char* kb0
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int tok = pair_token(t, ln);
-    const unsigned char* kr = (tok < 16 ? kb0 : kb1) + (tok & 15) * G::row_bytes;
+    const unsigned char* kb = tok < 16 ? kb0 : kb1;
+    const unsigned char* kr = kb + (tok & 15) * G::row_bytes;
+    if constexpr (KV == kKvMx4) {
+      f.k[t] = *reinterpret_cast<const T*>(kr + D / 8 * lq);
+      f.ks[t] = kb[G::code_bytes + ((tok & 15) * D + D / 4 * lq) / kMxGroup];
+    } else {
 #pragma unroll
-    for (int j = 0; j < F::kk; ++j)
-      f.k[t][j] = *reinterpret_cast<const T*>(kr + (KV == kKvFp8 ? 32 * j + 8 * lq : (4 * j + lq) * 16));
+      for (int j = 0; j < F::kk; ++j)
+        f.k[t][j] = *reinterpret_cast<const T*>(kr + (KV == kKvFp8 ? 32 * j + 8 * lq : (4 * j + lq) * 16));
+    }
   }
 }
 
@@ -310,12 +309,22 @@ __device__ __forceinline__ void load_v(Frags<D, KV>& f, const unsigned char* vb0
                                        int lq) {
   using G = Geo<D, KV>;
   typedef typename Frags<D, KV>::T T;
-  const unsigned char* vb = (lq >= 2 ? vb1 : vb0) + (lq & 1) * 8 * G::eb + ln * G::vrow_bytes;
+  const unsigned char* blk = lq >= 2 ? vb1 : vb0;
+  const unsigned char* vb = blk + (lq & 1) * G::vhalf_bytes + ln * G::vrow_bytes;
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
     const unsigned char* vr = vb + 16 * dt * G::vrow_bytes;
-    f.v[dt][0] = *reinterpret_cast<const T*>(vr);
-    if constexpr (KV == kKvF32) f.v[dt][1] = *reinterpret_cast<const T*>(vr + 16);
+    if constexpr (KV == kKvMx4) {
+      f.v[dt] = *reinterpret_cast<const uint32_t*>(vr);
+    } else {
+      f.v[dt][0] = *reinterpret_cast<const T*>(vr);
+      if constexpr (KV == kKvF32) f.v[dt][1] = *reinterpret_cast<const T*>(vr + 16);
+    }
+  }
+  if constexpr (KV == kKvMx4) {
+#pragma unroll
+    for (int i = 0; i < D / kMxGroup; ++i)
+      f.vs[i] = *reinterpret_cast<const uint2*>(blk + G::code_bytes + kTok * i + 8 * (lq & 1));
   }
 }
 
@@ -329,6 +338,15 @@ __device__ __forceinline__ KOps<D, KV> k_ops(const Frags<D, KV>& f) {
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) o.k[t][j] = fp8x8_to_bf16x8(f.k[t][j]);
     return o;
+  } else if constexpr (KV == kKvMx4) {
+    KOps<D, KV> o;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(&f.k[t]);
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) o.k[t][j] = mx4x8_to_bf16x8(w[j], mx_scale<0>(f.ks[t]));
+    }
+    return o;
   } else {
     return f;
   }
@@ -339,6 +357,11 @@ __device__ __forceinline__ VOps<D, KV> v_ops(const Frags<D, KV>& f) {
     VOps<D, KV> o;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) o.v[dt][0] = fp8x8_to_bf16x8(f.v[dt][0]);
+    return o;
+  } else if constexpr (KV == kKvMx4) {
+    VOps<D, KV> o;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) o.v[dt][0] = mx4x8_to_bf16x8(f.v[dt], f.vs[16 * dt / kMxGroup]);
     return o;
   } else {
     return f;
@@ -475,7 +498,7 @@ __device__ __forceinline__ QFrag<D, KV> q_from_lds(const unsigned char* qlds, in
   QFrag<D, KV> qf;
 #pragma unroll
   for (int j = 0; j < O::kk; ++j)
-    qf.q[j] = *reinterpret_cast<const typename O::T*>(qlds + Q::offset(16 * r + ln, 4 * j + lq));
+    qf.q[j] = *reinterpret_cast<const typename O::T*>(qlds + Q::offset(16 * r + ln, dim_col<D, KV>(j, lq)));
   return qf;
 }
 
@@ -524,6 +547,10 @@ struct Probs<kKvBf16> {
 };
 template <>
 struct Probs<kKvFp8> {
+  bf16x8 p;
+};
+template <>
+struct Probs<kKvMx4> {
   bf16x8 p;
 };
 
@@ -614,7 +641,7 @@ __device__ __forceinline__ void tile_values(const VOps<D, KV>& f, const Probs<KV
 // wave reads all chunks. (Plain loads stream faster than global-to-LDS
 // copies here.)
 template <int D, int KV>
-struct Stage {  // bf16 operands (fp8 caches stage their codes converted)
+struct Stage {  // bf16 operands (fp8 and 4-bit caches stage their codes converted)
   static constexpr int kKChunks = 2 * (D / 32);
   static constexpr int kChunks = kKChunks + D / 16;
   static constexpr int kPerWave = kChunks / kWaves;
@@ -631,18 +658,19 @@ __device__ __forceinline__ const unsigned char* frag_src(int c, const unsigned c
   if (c < S::kKChunks) {
     const int t = c / (D / 32), j = c % (D / 32);
     const int tok = pair_token(t, ln);
-    return (tok < 16 ? kb0 : kb1) + (tok & 15) * G::row_bytes + (KV == kKvFp8 ? 32 * j + 8 * lq : (4 * j + lq) * 16);
+    return (tok < 16 ? kb0 : kb1) + (tok & 15) * G::row_bytes + dim_col<D, KV>(j, lq) * G::bits;
   }
   const int dt = c - S::kKChunks;
-  return (lq >= 2 ? vb1 : vb0) + (lq & 1) * 8 * G::eb + ln * G::vrow_bytes + 16 * dt * G::vrow_bytes;
+  return (lq >= 2 ? vb1 : vb0) + (lq & 1) * G::vhalf_bytes + ln * G::vrow_bytes + 16 * dt * G::vrow_bytes;
 }
 
 // (A vector value rather than an array, so that it stays in registers.)
 // fp8 caches hold the raw codes (8 bytes per fragment) until the slice is
-// stored, converted, to the stage.
+// stored, converted, to the stage; 4-bit caches 4 bytes and their scale bytes
+// (K: one; V: those of the fragment's eight tokens).
 template <int D, int KV>
 struct Slice {
-  static constexpr int kWords = KV == kKvFp8 ? 2 : 4;  // dwords per fragment
+  static constexpr int kWords = KV == kKvFp8 ? 2 : (KV == kKvMx4 ? 3 : 4);  // dwords per fragment
   typedef unsigned int V __attribute__((ext_vector_type(kWords * Stage<D, KV>::kPerWave)));
   V v;
 };
@@ -663,6 +691,20 @@ __device__ __forceinline__ void load_slice(Slice<D, KV>& q, int id0, int id1, co
       const uint2 t = *reinterpret_cast<const uint2*>(src);
       q.v[2 * i] = t.x;
       q.v[2 * i + 1] = t.y;
+    } else if constexpr (KV == kKvMx4) {
+      using G = Geo<D, KV>;
+      const int c = wave + kWaves * i;
+      q.v[3 * i] = *reinterpret_cast<const uint32_t*>(src);
+      uint2 t;
+      if (c < S::kKChunks) {
+        const int tok = pair_token(c / (D / 32), ln);
+        t = uint2{(tok < 16 ? kb0 : kb1)[G::code_bytes + ((tok & 15) * D + D / 4 * lq) / kMxGroup], 0u};
+      } else {
+        t = *reinterpret_cast<const uint2*>((lq >= 2 ? vb1 : vb0) + G::code_bytes +
+                                            kTok * (16 * (c - S::kKChunks) / kMxGroup) + 8 * (lq & 1));
+      }
+      q.v[3 * i + 1] = t.x;
+      q.v[3 * i + 2] = t.y;
     } else {
       const uint4 t = *reinterpret_cast<const uint4*>(src);
       q.v[4 * i] = t.x;
@@ -680,6 +722,9 @@ __device__ __forceinline__ void store_slice(const Slice<D, KV>& q, unsigned char
     uint4 w;
     if constexpr (KV == kKvFp8)
       w = fp8x8_to_bf16x8(uint2{q.v[2 * i], q.v[2 * i + 1]});
+    else if constexpr (KV == kKvMx4)
+      w = wave + kWaves * i < Stage<D, KV>::kKChunks ? mx4x8_to_bf16x8(q.v[3 * i], mx_scale<0>(q.v[3 * i + 1]))
+                                                     : mx4x8_to_bf16x8(q.v[3 * i], uint2{q.v[3 * i + 1], q.v[3 * i + 2]});
     else
       w = uint4{q.v[4 * i], q.v[4 * i + 1], q.v[4 * i + 2], q.v[4 * i + 3]};
     *reinterpret_cast<uint4*>(stage + (wave + kWaves * i) * 1024 + lane * 16) = w;
@@ -849,7 +894,7 @@ __device__ __forceinline__ void run_window(const Window& win, int n, int nrows, 
       const int r = ws.grp * kNt + i;
       act[i] = 16 * r < nrows && 16 * r < hi && 16 * r + 16 > lo;
     }
-    if constexpr (KV == kKvFp8) {
+    if constexpr (kCoded<KV>) {
       // All tiles' scores, then all value products, so that only one of the
       // converted operands is held at a time.
       Scores s[kNt];
@@ -1156,7 +1201,7 @@ __global__ __launch_bounds__(kThreads, 1) void attn_kernel(AttnParams p) {
           const uint16_t* qrow = static_cast<const uint16_t*>(p.q) + (static_cast<int64_t>(b) * p.hq + qh) * D;
 #pragma unroll
           for (int j = 0; j < Ops<D, KV>::kk; ++j)
-            qw[i].q[j] = ok ? *reinterpret_cast<const uint4*>(qrow + 32 * j + 8 * lq) : uint4{0u, 0u, 0u, 0u};
+            qw[i].q[j] = ok ? *reinterpret_cast<const uint4*>(qrow + 8 * dim_col<D, KV>(j, lq)) : uint4{0u, 0u, 0u, 0u};
         }
         unsigned char* stages = lds + Q::bytes;
         const int np = (nst + 1) >> 1;
@@ -1659,13 +1704,13 @@ __global__ __launch_bounds__(kThreads, 1) void attn_kernel(AttnParams p) {
         if (paged && p.paged_nsplit == 1) {
           // Whole sequence in this unit: the normalised result.
           if (row < nrows) {
-            float* orow = p.out + (static_cast<int64_t>(paged_b) * p.hq + kvh * p.g + row) * D;
+            const int64_t orow = (static_cast<int64_t>(paged_b) * p.hq + kvh * p.g + row) * D;
             const float qnan = __builtin_nanf("");
 #pragma unroll
             for (int e = 0; e < kEl / 4; ++e) {
               f32x4 v = o[e] * inv;
               if (bad) v = f32x4{qnan, qnan, qnan, qnan};
-              *reinterpret_cast<f32x4*>(orow + 16 * (tt + e) + 4 * q4) = v;
+              store_out4(p.out, p.out_bf16 != 0, orow + 16 * (tt + e) + 4 * q4, v);
             }
           }
         } else {
@@ -1732,7 +1777,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, KV == kKvF32 && D == 128 ? 2 : 3)
                                (static_cast<int64_t>(b) * p.hq + kvh * p.g + (ln < p.g ? ln : 0)) * kRowBytes;
 #pragma unroll
     for (int i = 0; i < KOps<D, KV>::kk; ++i)
-      q.q[i] = *reinterpret_cast<const typename KOps<D, KV>::T*>(row + (4 * i + lq) * 16);
+      q.q[i] = *reinterpret_cast<const typename KOps<D, KV>::T*>(row + dim_col<D, KV>(i, lq) * 16);
   }
   int nb = (L + kTok - 1) / kTok;
   bool bad = false;
@@ -1832,12 +1877,12 @@ __global__ __launch_bounds__(64 * kPagedWaves, KV == kKvF32 && D == 128 ? 2 : 3)
   if (p.paged_nsplit == 1) {
     // Whole sequence in this unit: the normalised result.
     if (row < p.g) {
-      float* orow = p.out + (static_cast<int64_t>(b) * p.hq + kvh * p.g + row) * D;
+      const int64_t orow = (static_cast<int64_t>(b) * p.hq + kvh * p.g + row) * D;
 #pragma unroll
       for (int e = 0; e < kEl / 4; ++e) {
         f32x4 x = o[e] * inv;
         if (bad) x = f32x4{qnan, qnan, qnan, qnan};
-        *reinterpret_cast<f32x4*>(orow + 16 * ((ln & 3) * (kEl / 4) + e) + 4 * (ln >> 2)) = x;
+        store_out4(p.out, p.out_bf16 != 0, orow + 16 * ((ln & 3) * (kEl / 4) + e) + 4 * (ln >> 2), x);
       }
     }
   } else {
@@ -1979,12 +2024,22 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(MergeParams p) {
   // Stored position pos holds dimension 16 t + 4 q + i for pos = (D / 4) q + 4 t + i.
   const int pos = kEl * lane;
   const int dim = 16 * ((pos % (D / 4)) / 4) + 4 * (pos / (D / 4)) + pos % 4;
-  float* dst = p.out + static_cast<int64_t>(r) * D + dim;
+  const int64_t at = static_cast<int64_t>(r) * D + dim;
+  float* dst = static_cast<float*>(p.out) + at;
+  uint16_t* half = static_cast<uint16_t*>(p.out) + at;
   const float q = __builtin_nanf("");
   if constexpr (kEl == 2) {
-    *reinterpret_cast<f32x2*>(dst) = nan ? f32x2{q, q} : f32x2{acc[0] * inv, acc[1] * inv};
+    const f32x2 x = nan ? f32x2{q, q} : f32x2{acc[0] * inv, acc[1] * inv};
+    if (p.out_bf16)
+      *reinterpret_cast<uint32_t*>(half) = pack_bf16x2(x.x, x.y);
+    else
+      *reinterpret_cast<f32x2*>(dst) = x;
   } else {
-    *dst = nan ? q : acc[0] * inv;
+    const float x = nan ? q : acc[0] * inv;
+    if (p.out_bf16)
+      *half = static_cast<uint16_t>(pack_bf16x2(x, x));
+    else
+      *dst = x;
   }
 }
 
@@ -2013,7 +2068,7 @@ static hipError_t launch_paged_t(AttnParams p, hipStream_t stream) {
     p.q = static_cast<const char*>(p.q) + n * q_beam;
     p.block_tables += n * p.max_blocks;
     p.seq_lens += n;
-    p.out += n * p.hq * D;
+    p.out = static_cast<char*>(p.out) + n * p.hq * D * (p.out_bf16 ? 2 : 4);
     if (p.paged_nsplit > 1) {
       const int64_t rows = n * p.paged_nsplit * p.hq;
       p.part_o = static_cast<char*>(p.part_o) + rows * D * (KV == kKvF32 ? 4 : 2);
@@ -2047,7 +2102,7 @@ static hipError_t launch_merge_t(MergeParams p, hipStream_t stream) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     p.seq_lens += n / p.q_len;
-    p.out += n * p.hq * D;
+    p.out = static_cast<char*>(p.out) + n * p.hq * D * (p.out_bf16 ? 2 : 4);
     if (p.slot_tab) {
       p.slot_tab += n * p.slot_stride;
       p.build_len += n;
@@ -2071,10 +2126,12 @@ hipError_t launch_attn(const AttnParams& p, int grid, int head_dim, int kv_kind,
   if (head_dim == 128) {
     if (kv_kind == kKvBf16) return launch_attn_t<128, kKvBf16>(p, grid, stream);
     if (kv_kind == kKvFp8) return launch_attn_t<128, kKvFp8>(p, grid, stream);
+    if (kv_kind == kKvMx4) return launch_attn_t<128, kKvMx4>(p, grid, stream);
     return launch_attn_t<128, kKvF32>(p, grid, stream);
   }
   if (kv_kind == kKvBf16) return launch_attn_t<64, kKvBf16>(p, grid, stream);
   if (kv_kind == kKvFp8) return launch_attn_t<64, kKvFp8>(p, grid, stream);
+  if (kv_kind == kKvMx4) return launch_attn_t<64, kKvMx4>(p, grid, stream);
   return launch_attn_t<64, kKvF32>(p, grid, stream);
 }
 

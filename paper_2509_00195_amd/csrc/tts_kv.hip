@@ -1,6 +1,7 @@
 // KV-cache maintenance around the decode step: appending each beam's new
-// token to its block (with the fp8 block-scale policy) and copying blocks
-// for copy-on-write beam duplication.
+// token to its block (with the fp8 block-scale policy), appending chunks of
+// tokens with their position rotation, and copying blocks for copy-on-write
+// beam duplication.
 //
 // A decode step of the search writes one token per beam into the paged
 // cache before attention reads it (the current token is part of seq_len),
@@ -11,6 +12,9 @@
 
 #include <cstdint>
 #include <type_traits>
+
+#include "tts_device.h"
+#include "tts_kv.h"
 
 namespace tts {
 namespace {
@@ -46,10 +50,6 @@ __device__ __forceinline__ uint32_t e4m3_encode(float x) {
 
 __device__ __forceinline__ float e4m3_decode(uint32_t code) {
   return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(code), 0);  // exact
-}
-
-__device__ __forceinline__ float bf16_to_f32(uint16_t b) {
-  return __builtin_bit_cast(float, static_cast<uint32_t>(b) << 16);
 }
 
 __device__ __forceinline__ float block_max(float v, float* red) {
@@ -221,6 +221,525 @@ __global__ __launch_bounds__(kKvThreads) void append_kernel(AppendParams p) {
   }
 }
 
+// ---- rotating append ---------------------------------------------------------
+// A workgroup takes one part of one item, an item being one cache block of
+// one sequence and the up to sixteen new tokens that go there, so that what
+// a block shares (an fp8 scale, a byte of two 4-bit tokens, a line of a
+// dim-major V row) has one writer and no atomics. Parts: the K rows of
+// `heads_per` heads, the V rows of as many, kRopeTasks pieces of the query
+// rows. Bound by memory for chunks, by the round trips (offsets, length,
+// table and table rows, token) for a step's single tokens.
+//
+// The products of the rotation and their sum are rounded one by one (no
+// fused multiply-add), so codes do not depend on how the compiler contracts.
+constexpr int kRopeThreads = kKvThreads;
+
+struct RopeItem {
+  int seq, n;     // sequence, tokens of it in this block
+  int row;        // first token's row of q, k_new, v_new
+  int pos, slot;  // its index in the sequence, its slot in the block
+  int blk;        // physical block, -1: nothing is stored
+  bool bad;       // the sequence is shorter than its new tokens: NaN queries
+};
+
+// The item's sequence: items [f(b), f(b + 1)) belong to sequence b, with
+// f(b) = offsets[b] / 16 + 2 b. A sequence of n > 0 new tokens touches at
+// most (n + 30) / 16 blocks (rounded down), which is at most
+// f(b + 1) - f(b); the items past its last block are empty. Found by every
+// wave alone in steps of 64 (in bounds and finite whatever the offsets hold).
+__device__ __forceinline__ int64_t first_item(const RopeParams& p, int64_t b) {
+  return (static_cast<int64_t>(p.tok_offsets[b]) >> 4) + 2 * b;
+}
+
+__device__ __forceinline__ RopeItem rope_item(const RopeParams& p, int64_t item) {
+  const int lane = threadIdx.x & 63;
+  RopeItem it{0, 0, 0, 0, 0, -1, false};
+  int64_t j = 0;
+  int t0, t1;
+  if (p.tok_offsets) {
+    int64_t lo = 0, hi = p.num_seqs;
+    while (hi - lo > 1) {
+      const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+      const bool le = lane == 0 || (at < hi && first_item(p, at) <= item);
+      lo += (__builtin_popcountll(__builtin_amdgcn_ballot_w64(le)) - 1) * step;
+      hi = hi < lo + step ? hi : lo + step;
+    }
+    it.seq = __builtin_amdgcn_readfirstlane(static_cast<int>(lo));
+    t0 = p.tok_offsets[it.seq];
+    t1 = p.tok_offsets[it.seq + 1];
+    j = item - ((static_cast<int64_t>(t0) >> 4) + 2 * static_cast<int64_t>(it.seq));
+    if (t0 < 0 || t1 < t0 || t1 > p.num_tokens || j < 0) return it;
+  } else {
+    it.seq = static_cast<int>(item);
+    t0 = it.seq;
+    t1 = t0 + 1;
+  }
+  const int n = t1 - t0, len = p.seq_lens[it.seq];
+  if (len <= 0 || n == 0) return it;  // idle
+  it.bad = len < n;
+  const int pos0 = it.bad ? 0 : len - n;
+  const int64_t lb = pos0 / kSlots + j, last = static_cast<int64_t>(pos0) + n;
+  if (lb * kSlots >= last) return it;
+  it.pos = lb * kSlots > pos0 ? static_cast<int>(lb * kSlots) : pos0;
+  it.slot = it.pos % kSlots;
+  it.n = static_cast<int>((lb + 1) * kSlots < last ? (lb + 1) * kSlots : last) - it.pos;
+  it.row = t0 + it.pos - pos0;
+  if (!it.bad && lb < p.max_blocks) {
+    it.blk = p.block_tables[static_cast<int64_t>(it.seq) * p.max_blocks + lb];
+    if (it.blk < 0 || it.blk >= p.num_blocks) it.blk = -1;
+  }
+  return it;
+}
+
+// W consecutive elements of a token.
+template <int W>
+__device__ __forceinline__ void load_elems(const uint16_t* src, float (&x)[W]) {
+  if constexpr (W == 8) {
+    const uint4 t = *reinterpret_cast<const uint4*>(src);
+    const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+      x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = bf16_to_f32(src[i]);
+  }
+}
+template <int W>
+__device__ __forceinline__ void load_elems(const float* src, float (&x)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; i += 4) {
+    if constexpr (W >= 4) {
+      const f32x4 t = *reinterpret_cast<const f32x4*>(src + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[i + k] = t[k];
+    } else {
+      x[i] = src[i];
+    }
+  }
+}
+template <int W>
+__device__ __forceinline__ void store_elems(uint16_t* dst, const float (&x)[W]) {
+  if constexpr (W == 8)
+    *reinterpret_cast<uint4*>(dst) = uint4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                           pack_bf16x2(x[6], x[7])};
+  else
+#pragma unroll
+    for (int i = 0; i < W; ++i) dst[i] = static_cast<uint16_t>(pack_bf16x2(x[i], x[i]));
+}
+template <int W>
+__device__ __forceinline__ void store_elems(float* dst, const float (&x)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; i += 4) {
+    if constexpr (W >= 4)
+      *reinterpret_cast<f32x4*>(dst + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    else
+      dst[i] = x[i];
+  }
+}
+
+// One unit of a row of a head: W rotated pairs, or W elements passed through
+// (interleaved and W > 1: W elements, which are W / 2 pairs or passed).
+// Elements at[0] .. + W and, for two-part units, at[1] .. + W.
+template <int W>
+struct RopeUnit {
+  int parts, at[2];
+  float x[2][W];
+};
+
+template <int W>
+__device__ __forceinline__ int rope_units(const RopeParams& p) {
+  const int passed = (p.head_dim - p.rot) / W;
+  return (p.interleaved && W > 1 ? p.rot / W : p.rot / 2 / W) + passed;
+}
+
+template <int W, typename E>
+__device__ __forceinline__ RopeUnit<W> rope_unit(const RopeParams& p, const E* src, int u, const float* cos,
+                                                 const float* sin) {
+#pragma clang fp contract(off)
+  RopeUnit<W> r;
+  const int half = p.rot / 2, turned = p.interleaved && W > 1 ? p.rot / W : half / W;
+  if (u >= turned) {
+    r.parts = 1;
+    r.at[0] = p.rot + (u - turned) * W;
+    load_elems<W>(src + r.at[0], r.x[0]);
+  } else if (W > 1 && p.interleaved) {
+    constexpr int kPairs = W > 1 ? W / 2 : 1;
+    r.parts = 1;
+    r.at[0] = u * W;
+    float x[W], c[kPairs], s[kPairs];
+    load_elems<W>(src + u * W, x);
+    load_elems<kPairs>(cos + u * kPairs, c);
+    load_elems<kPairs>(sin + u * kPairs, s);
+#pragma unroll
+    for (int i = 0; i + 1 < W; i += 2) {
+      const float xc = x[i] * c[i / 2], ys = x[i + 1] * s[i / 2], yc = x[i + 1] * c[i / 2], xs = x[i] * s[i / 2];
+      r.x[0][i] = xc - ys;
+      r.x[0][i + 1] = yc + xs;
+    }
+  } else {
+    r.parts = 2;
+    r.at[0] = p.interleaved ? 2 * u : u * W;
+    r.at[1] = p.interleaved ? 2 * u + 1 : half + u * W;
+    float x[W], y[W], c[W], s[W];
+    load_elems<W>(src + r.at[0], x);
+    load_elems<W>(src + r.at[1], y);
+    load_elems<W>(cos + u * W, c);
+    load_elems<W>(sin + u * W, s);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float xc = x[i] * c[i], ys = y[i] * s[i], yc = y[i] * c[i], xs = x[i] * s[i];
+      r.x[0][i] = xc - ys;
+      r.x[1][i] = yc + xs;
+    }
+  }
+  return r;
+}
+
+__device__ __forceinline__ int64_t rope_pos(const RopeParams& p, const RopeItem& it, int i) {
+  return p.positions ? p.positions[it.row + i] : it.pos + i;
+}
+
+// The item's tokens whose position has a row of the tables (bit i: token i).
+__device__ __forceinline__ uint32_t rope_tokens(const RopeParams& p, const RopeItem& it) {
+  const int lane = threadIdx.x & 63;
+  bool good = lane < it.n;
+  if (good && p.rot > 0) {
+    const int64_t at = rope_pos(p, it, lane);
+    good = at >= 0 && at < p.max_pos;
+  }
+  return static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(good));
+}
+
+// Calls f(token, head - h0, unit) for the units of heads h0 .. h1 of the
+// item's good tokens, with the unit rotated.
+template <int W, typename E, typename F>
+__device__ __forceinline__ void rope_each(const RopeParams& p, const RopeItem& it, uint32_t good, const E* src,
+                                          int64_t stride, int h0, int h1, int first, int last, F f) {
+  const int units = rope_units<W>(p), heads = h1 - h0, total = it.n * heads * units;
+  const int end = last < total ? last : total;
+  for (int i = first + static_cast<int>(threadIdx.x); i < end; i += kRopeThreads) {
+    const int u = i % units, h = i / units % heads, t = i / units / heads;
+    if (!((good >> t) & 1u)) continue;
+    const int64_t at = p.rot > 0 ? rope_pos(p, it, t) * (p.rot / 2) : 0;
+    f(t, h, rope_unit<W>(p, src + (it.row + t) * stride + static_cast<int64_t>(h0 + h) * p.head_dim, u, p.cos + at,
+                         p.sin + at));
+  }
+}
+
+// Query rows: pieces [first, first + kRopeTasks) of the item's.
+template <int W, typename E>
+__device__ __forceinline__ void rope_query(const RopeParams& p, const RopeItem& it, uint32_t good, int part) {
+  E* out = static_cast<E*>(p.q_out);
+  const int first = part * kRopeTasks;
+  if (it.bad || good != (1u << it.n) - 1u) {
+    // NaN rows (all of a bad sequence's, else the tokens without a position), written by the first part.
+    const float qnan[1] = {__builtin_nanf("")};
+    const int row = p.hq * p.head_dim;
+    for (int t = 0; part == 0 && t < it.n; ++t)
+      if (it.bad || !((good >> t) & 1u))
+        for (int i = threadIdx.x; i < row; i += kRopeThreads)
+          store_elems<1>(out + static_cast<int64_t>(it.row + t) * row + i, qnan);
+    if (it.bad) return;
+  }
+  rope_each<W>(p, it, good, static_cast<const E*>(p.q), p.q_stride, 0, p.hq, first, first + kRopeTasks,
+               [&](int t, int h, const RopeUnit<W>& r) {
+                 E* dst = out + (static_cast<int64_t>(it.row + t) * p.hq + h) * p.head_dim;
+                 store_elems<W>(dst + r.at[0], r.x[0]);
+                 if (r.parts == 2) store_elems<W>(dst + r.at[1], r.x[1]);
+               });
+}
+
+// The scale of an fp8 block after the item's tokens, of largest magnitude
+// `top`: set by them when they open the block, raised to fit them when they
+// exceed it. `lut`: the earlier codes' new values, when it is raised.
+__device__ __forceinline__ float fp8_scale(float top, float old, bool opens, bool* again, uint8_t* lut) {
+  *again = !opens && top > 448.f * old;
+  const float s = opens ? (top > 0.f ? top / 448.f : 1.f) : (*again ? top / 448.f : old);
+  if (*again) lut[threadIdx.x] = static_cast<uint8_t>(e4m3_encode(e4m3_decode(threadIdx.x) * old / s));
+  __syncthreads();
+  return s;
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
+
+// The scale byte of a group of largest magnitude `top` (bits): 2 to the
+// power floor(log2 top) - 2, so that top / scale lies in [4, 8) (E2M1
+// reaches 6; above 5 a value saturates or rounds to it). Infinities and
+// NaN: 255, which makes the group's values NaN.
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t top) {
+  const uint32_t e = top >> 23;
+  return e == 255u ? 255u : (e > 3u ? e - 2u : 1u);
+}
+
+// E2M1 codes (nearest, ties to even, saturating) of eight values over the scale.
+__device__ __forceinline__ uint32_t mx_encode(const float (&x)[8], uint32_t scale) {
+  if (scale == 255u) return 0u;
+  const float s = mx_scale<0>(scale);
+  uint32_t w = 0u;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+}
+
+// Scale byte and codes of eight of a group's 32 values, four adjacent lanes
+// to a group (all four call together).
+__device__ __forceinline__ uint32_t mx_quantise(const float (&x)[8], uint32_t* scale) {
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = top > abs_bits(x[i]) ? top : abs_bits(x[i]);
+  for (int o = 1; o < 4; o <<= 1) {
+    const uint32_t y = __shfl_xor(top, o);
+    top = top > y ? top : y;
+  }
+  *scale = mx_scale_byte(top);
+  return mx_encode(x, *scale);
+}
+
+// K rows of heads h0 .. h1.
+template <int KV, int W, typename E>
+__device__ __forceinline__ void rope_keys(const RopeParams& p, const RopeItem& it, uint32_t good, int h0, int h1,
+                                          void* lds, float* red) {
+  const int D = p.head_dim;
+  const E* src = static_cast<const E*>(p.k_new);
+  constexpr int kAll = 0x7FFFFFFF;
+  if constexpr (KV == kKvF32 || KV == kKvBf16) {
+    E* blk = static_cast<E*>(p.k_cache) + (static_cast<int64_t>(it.blk) * p.hkv + h0) * kSlots * D;
+    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
+      E* dst = blk + (h * kSlots + it.slot + t) * D;
+      store_elems<W>(dst + r.at[0], r.x[0]);
+      if (r.parts == 2) store_elems<W>(dst + r.at[1], r.x[1]);
+    });
+  } else if constexpr (KV == kKvFp8) {
+    uint8_t* lut = static_cast<uint8_t*>(lds);
+    const float old = p.k_scale[it.blk];
+    float top = 0.f;
+    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int, int, const RopeUnit<W>& r) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < W; ++i) top = k < r.parts ? fmaxf(top, __builtin_fabsf(r.x[k][i])) : top;
+    });
+    top = block_max(top, red);
+    bool again;
+    const float s = fp8_scale(top, old, it.slot == 0, &again, lut);
+    uint8_t* blk = static_cast<uint8_t*>(p.k_cache) + static_cast<int64_t>(it.blk) * p.hkv * kSlots * D;
+    if (again) {
+      const int per = it.slot * D / 16, total = p.hkv * per;
+      for (int c = threadIdx.x; c < total; c += kRopeThreads) {
+        uint4* x = reinterpret_cast<uint4*>(blk + c / per * kSlots * D) + c % per;
+        *x = map_codes(*x, lut, 16, -1, 0);
+      }
+    }
+    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
+      uint8_t* dst = blk + (h * kSlots + it.slot + t) * D;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (k >= r.parts) continue;
+        uint32_t c[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) c[i] = e4m3_encode(r.x[k][i] / s);
+        if constexpr (W == 8)
+          *reinterpret_cast<uint2*>(dst + r.at[k]) = uint2{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24,
+                                                           c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
+        else
+          for (int i = 0; i < W; ++i) dst[r.at[k] + i] = static_cast<uint8_t>(c[i]);
+      }
+    });
+    if (threadIdx.x == 0) p.k_scale[it.blk] = s;  // (read by every thread before block_max's barriers)
+  } else {
+    // Rotated rows in LDS, then four lanes to a group of 32 dims.
+    float* tile = static_cast<float*>(lds);
+    const int heads = h1 - h0;
+    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
+      float* dst = tile + (t * heads + h) * D;
+      store_elems<W>(dst + r.at[0], r.x[0]);
+      if (r.parts == 2) store_elems<W>(dst + r.at[1], r.x[1]);
+    });
+    __syncthreads();
+    const int code_bytes = kSlots * D / 2, blk_bytes = code_bytes + kSlots * D / kMxGroup;
+    uint8_t* blk = static_cast<uint8_t*>(p.k_cache) + (static_cast<int64_t>(it.blk) * p.hkv + h0) * blk_bytes;
+    const int pieces = D / 8, total = it.n * heads * pieces;  // (a multiple of 8: groups are whole)
+    for (int i = threadIdx.x; i < total; i += kRopeThreads) {
+      const int piece = i % pieces, h = i / pieces % heads, t = i / pieces / heads;
+      float x[8];
+      load_elems<8>(tile + i * 8, x);
+      uint32_t scale;
+      const uint32_t codes = mx_quantise(x, &scale);
+      if (!((good >> t) & 1u)) continue;
+      uint8_t* b = blk + static_cast<int64_t>(h) * blk_bytes;
+      *reinterpret_cast<uint32_t*>(b + ((it.slot + t) * D + 8 * piece) / 2) = codes;
+      if (i % 4 == 0) b[code_bytes + ((it.slot + t) * D + 8 * piece) / kMxGroup] = static_cast<uint8_t>(scale);
+    }
+  }
+}
+
+// V rows of heads h0 .. h1: a dim's tokens lie side by side in the cache, so
+// a thread takes dims (kVw of them) with all of the item's tokens.
+template <int KV, int kVw, typename E>
+__device__ __forceinline__ void rope_values(const RopeParams& p, const RopeItem& it, uint32_t good, int h0, int h1,
+                                            void* lds, float* red) {
+  const int D = p.head_dim, heads = h1 - h0;
+  const E* src = static_cast<const E*>(p.v_new) + it.row * p.v_stride + static_cast<int64_t>(h0) * D;
+  typedef E Vec __attribute__((ext_vector_type(kVw)));
+  const bool full = good == 0xFFFFu;
+  const uint32_t slots = good << it.slot;  // the block's slots that are written
+  auto load = [&](int d, Vec (&x)[kSlots]) {  // by slot
+#pragma unroll
+    for (int k = 0; k < kSlots; ++k) {
+      Vec v = Vec(0);
+      if ((slots >> k) & 1u) v = *reinterpret_cast<const Vec*>(src + (k - it.slot) * p.v_stride + d);
+      x[k] = v;
+    }
+  };
+  if constexpr (KV == kKvF32 || KV == kKvBf16) {
+    E* blk = static_cast<E*>(p.v_cache) + (static_cast<int64_t>(it.blk) * p.hkv + h0) * kSlots * D;
+    for (int d = threadIdx.x * kVw; d < heads * D; d += kRopeThreads * kVw) {
+      Vec x[kSlots];
+      load(d, x);
+#pragma unroll
+      for (int e = 0; e < kVw; ++e) {
+        E* dst = blk + static_cast<int64_t>(d + e) * kSlots;
+        if (full) {
+          constexpr int kPer = 16 / sizeof(E);
+          typedef E Out __attribute__((ext_vector_type(kPer)));
+#pragma unroll
+          for (int k = 0; k < kSlots; k += kPer) {
+            Out o;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) o[i] = x[k + i][e];
+            *reinterpret_cast<Out*>(dst + k) = o;
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < kSlots; ++k)
+            if ((slots >> k) & 1u) dst[k] = x[k][e];
+        }
+      }
+    }
+  } else if constexpr (KV == kKvFp8) {
+    uint8_t* lut = static_cast<uint8_t*>(lds);
+    const float old = p.v_scale[it.blk];
+    float top = 0.f;
+    for (int d = threadIdx.x * kVw; d < heads * D; d += kRopeThreads * kVw) {
+      Vec x[kSlots];
+      load(d, x);
+#pragma unroll
+      for (int k = 0; k < kSlots; ++k)
+#pragma unroll
+        for (int e = 0; e < kVw; ++e) top = fmaxf(top, __builtin_fabsf(bf16_to_f32(x[k][e])));
+    }
+    top = block_max(top, red);
+    bool again;
+    const float s = fp8_scale(top, old, it.slot == 0, &again, lut);
+    uint8_t* blk = static_cast<uint8_t*>(p.v_cache) + (static_cast<int64_t>(it.blk) * p.hkv + h0) * kSlots * D;
+    for (int d = threadIdx.x * kVw; d < heads * D; d += kRopeThreads * kVw) {
+      Vec x[kSlots];
+      load(d, x);
+#pragma unroll
+      for (int e = 0; e < kVw; ++e) {
+        uint8_t* dst = blk + static_cast<int64_t>(d + e) * kSlots;
+        if (!full && !again) {
+#pragma unroll
+          for (int k = 0; k < kSlots; ++k)
+            if ((slots >> k) & 1u) dst[k] = static_cast<uint8_t>(e4m3_encode(bf16_to_f32(x[k][e]) / s));
+          continue;
+        }
+        uint4 w = {0u, 0u, 0u, 0u};
+        if (!full) w = map_codes(*reinterpret_cast<const uint4*>(dst), lut, it.slot, -1, 0);
+        uint32_t c[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < kSlots; ++k)
+          if ((slots >> k) & 1u)
+            c[k / 4] = (c[k / 4] & ~(0xFFu << (8 * (k % 4)))) | e4m3_encode(bf16_to_f32(x[k][e]) / s) << (8 * (k % 4));
+        *reinterpret_cast<uint4*>(dst) = uint4{c[0], c[1], c[2], c[3]};
+      }
+    }
+    if (threadIdx.x == 0) p.v_scale[it.blk] = s;
+  } else {
+    // Codes in LDS, a byte each by (slot, dim); then eight bytes of a dim.
+    uint8_t* tile = static_cast<uint8_t*>(lds);
+    const int row = heads * D, code_bytes = kSlots * D / 2, blk_bytes = code_bytes + kSlots * D / kMxGroup;
+    uint8_t* blk = static_cast<uint8_t*>(p.v_cache) + (static_cast<int64_t>(it.blk) * p.hkv + h0) * blk_bytes;
+    const int pieces = row / 8;
+    for (int i = threadIdx.x; i < it.n * pieces; i += kRopeThreads) {
+      const int t = i / pieces, d = i % pieces * 8;
+      float x[8];
+      if constexpr (kVw == 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = bf16_to_f32(src[t * p.v_stride + d + k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(src + t * p.v_stride + d + k);
+          x[k] = __builtin_bit_cast(float, w << 16);
+          x[k + 1] = __builtin_bit_cast(float, w & 0xFFFF0000u);
+        }
+      }
+      uint32_t scale;
+      const uint32_t codes = mx_quantise(x, &scale);
+      uint2 bytes = {0u, 0u};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        bytes.x |= ((codes >> (4 * k)) & 15u) << (8 * k);
+        bytes.y |= ((codes >> (4 * k + 16)) & 15u) << (8 * k);
+      }
+      *reinterpret_cast<uint2*>(tile + t * row + d) = bytes;
+      if (i % 4 == 0 && ((good >> t) & 1u))
+        blk[d / D * blk_bytes + code_bytes + d % D / kMxGroup * kSlots + it.slot + t] = static_cast<uint8_t>(scale);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < row; d += kRopeThreads) {
+      uint2* dst = reinterpret_cast<uint2*>(blk + d / D * blk_bytes + d % D * (kSlots / 2));
+      uint64_t w = 0u;
+      if (!full) {
+        const uint2 o = *dst;
+        w = o.x | static_cast<uint64_t>(o.y) << 32;
+      }
+#pragma unroll
+      for (int k = 0; k < kSlots; ++k)
+        if ((slots >> k) & 1u)
+          w = (w & ~(15ull << (4 * k))) | static_cast<uint64_t>(tile[(k - it.slot) * row + d]) << (4 * k);
+      *dst = uint2{static_cast<uint32_t>(w), static_cast<uint32_t>(w >> 32)};
+    }
+  }
+}
+
+template <int KV>
+__global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeParams p) {
+  typedef typename std::conditional<KV == kKvF32, float, uint16_t>::type E;
+  // 4-bit K: rotated rows in fp32; 4-bit V: codes; fp8: the codes' table.
+  __shared__ __attribute__((aligned(16))) float lds[KV == kKvMx4 ? kRopeTile : (KV == kKvFp8 ? 64 : 4)];
+  __shared__ float red[kRopeThreads / 64];
+  const RopeItem it = rope_item(p, p.item0 + blockIdx.x);
+  if (it.n == 0) return;
+  const int part = static_cast<int>(blockIdx.y);
+  const uint32_t good = rope_tokens(p, it);
+  if (part >= 2 * p.kv_parts) {
+    if (p.q_wide)
+      rope_query<8, E>(p, it, good, part - 2 * p.kv_parts);
+    else
+      rope_query<1, E>(p, it, good, part - 2 * p.kv_parts);
+    return;
+  }
+  if (it.blk < 0 || good == 0) return;
+  const int h0 = part / 2 * p.heads_per, h1 = h0 + p.heads_per < p.hkv ? h0 + p.heads_per : p.hkv;
+  if (part % 2 == 0) {
+    if (p.k_wide)
+      rope_keys<KV, 8, E>(p, it, good, h0, h1, lds, red);
+    else
+      rope_keys<KV, 1, E>(p, it, good, h0, h1, lds, red);
+  } else {
+    if (p.v_wide)
+      rope_values<KV, 2, E>(p, it, good, h0, h1, lds, red);
+    else
+      rope_values<KV, 1, E>(p, it, good, h0, h1, lds, red);
+  }
+}
+
 struct CopyParams {
   const int32_t* pairs;  // [n][2]: source, destination block
   void* k_cache;
@@ -292,6 +811,48 @@ hipError_t launch_append(const void* k_new, const void* v_new, const int32_t* bl
   if (kv_kind == 0) return launch_append_t<0>(p, num_seqs, stream);
   if (kv_kind == 1) return launch_append_t<1>(p, num_seqs, stream);
   return launch_append_t<2>(p, num_seqs, stream);
+}
+
+// Whether rows at `ptr` of `stride` elements start at multiples of `bytes`.
+static bool rows_at(const void* ptr, int64_t stride, int elem, int bytes) {
+  return reinterpret_cast<uintptr_t>(ptr) % bytes == 0 && stride * elem % bytes == 0;
+}
+
+hipError_t launch_rope_append(RopeParams p, int kv_kind, hipStream_t stream) {
+  const int elem = kv_kind == kKvF32 ? 4 : 2, half = p.rot / 2;
+  // Eight elements at a time where rows, tables and the rotated part allow it.
+  const bool parts8 = p.interleaved ? p.rot % 8 == 0 : half % 8 == 0;
+  const bool tables8 = p.rot == 0 || (rows_at(p.cos, half, 4, 16) && rows_at(p.sin, half, 4, 16));
+  p.q_wide = p.q && parts8 && tables8 && rows_at(p.q, p.q_stride, elem, 16) && rows_at(p.q_out, 0, elem, 16);
+  p.k_wide = parts8 && tables8 && rows_at(p.k_new, p.k_stride, elem, 16);
+  p.v_wide = rows_at(p.v_new, p.v_stride, elem, 2 * elem);
+  const int most_tokens = p.tok_offsets ? kSlots : 1;
+  // fp8: one scale for all heads of a block, so one part.
+  p.heads_per = kRopeTile / (most_tokens * p.head_dim);
+  if (kv_kind == kKvFp8 || p.heads_per > p.hkv) p.heads_per = p.hkv;
+  p.kv_parts = (p.hkv + p.heads_per - 1) / p.heads_per;
+  const int width = p.q_wide ? 8 : 1;
+  const int64_t units = (p.interleaved && p.q_wide ? p.rot / width : half / width) + (p.head_dim - p.rot) / width;
+  const int64_t q_parts = p.q ? (most_tokens * p.hq * units + kRopeTasks - 1) / kRopeTasks : 0;
+  const int64_t parts = 2 * static_cast<int64_t>(p.kv_parts) + q_parts;
+  if (parts > kMaxGridY) return hipErrorInvalidValue;
+  const int64_t items = p.tok_offsets ? static_cast<int64_t>(p.num_tokens) / kSlots + 2 * static_cast<int64_t>(p.num_seqs)
+                                      : p.num_seqs;
+  const int64_t most = 0xFFFFFFFFll / kRopeThreads / parts;  // (a launch holds fewer than 2^32 threads)
+  for (int64_t done = 0; done < items; done += most) {
+    const int64_t n = items - done < most ? items - done : most;
+    p.item0 = done;
+    const dim3 grid(static_cast<unsigned>(n), static_cast<unsigned>(parts));
+    switch (kv_kind) {
+      case kKvF32: hipLaunchKernelGGL(rope_append_kernel<kKvF32>, grid, dim3(kRopeThreads), 0, stream, p); break;
+      case kKvBf16: hipLaunchKernelGGL(rope_append_kernel<kKvBf16>, grid, dim3(kRopeThreads), 0, stream, p); break;
+      case kKvFp8: hipLaunchKernelGGL(rope_append_kernel<kKvFp8>, grid, dim3(kRopeThreads), 0, stream, p); break;
+      default: hipLaunchKernelGGL(rope_append_kernel<kKvMx4>, grid, dim3(kRopeThreads), 0, stream, p); break;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_copy_blocks(const int32_t* pairs, int num_pairs, void* k_cache, void* v_cache, float* k_scale,

@@ -1,0 +1,561 @@
+// HIP kernels (gfx950) of the ragged prefill attention: causal attention of
+// each sequence's last tokens over its paged KV cache.
+//
+// A workgroup of four waves takes 128 query rows (tokens x query heads of one
+// KV head) and walks the tokens that they see, a tile at a time: 64 tokens
+// (fp32: 32) of K and V go from the paged cache through registers, converted
+// to bf16 for fp8 and 4-bit caches, into one of two LDS buffers, while the
+// waves work on the other; one barrier per tile. Each wave holds 32 rows:
+//   S^T = K Q^T   : v_mfma_f32_32x32x16_bf16 (M = 32 tokens, N = 32 rows)
+//   O^T += V^T P^T: the same (M = 32 dims, N = 32 rows, K = 16 tokens)
+// K's rows are read in the order token_of, so that a lane's scores are those
+// of 8 consecutive tokens per step of the second product: its B operand
+// without an exchange between lanes. Values are dim-major in the cache, so
+// the matching A operand is one 16-byte read.
+//
+// Softmax in one pass: exponentials against a reference per row that only
+// moves (with a rescaling of the sums) when a tile's maximum exceeds it by
+// more than kRefSlack: sums stay below 2^kRefSlack times the token count, far
+// inside fp32's range, and the usual tile rescales nothing.
+//
+// LDS: a tile's 16-byte pieces lie fragment by fragment (one fragment is what
+// the 64 lanes of a wave read for one operand), and inside a fragment at a
+// place XORed with the piece's column, so that neither the stores (rows of
+// the cache, 16 bytes per thread) nor the reads meet in a bank.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "tts_device.h"
+#include "tts_prefill.h"
+
+namespace tts {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kPfWaves = kPrefillRows / 32;
+constexpr int kPfThreads = 64 * kPfWaves;
+constexpr float kNegInf = -__builtin_inff();
+constexpr float kRefSlack = 16.f;  // log2 units
+
+template <int D, int KV>
+struct PfGeo {
+  static constexpr bool f32 = KV == kKvF32;
+  static constexpr int eb = f32 ? 4 : 2;                 // bytes of a staged element
+  static constexpr int tokens = f32 ? 32 : 64;           // of a tile
+  static constexpr int blocks = tokens / kTok;
+  static constexpr int per = 16 / eb;                    // elements of a piece
+  static constexpr int kcols = D / per;                  // pieces of a K row
+  static constexpr int vcols = kTok / per;               // pieces of a V row
+  static constexpr int blk_pieces = kTok * kcols;        // of K, and of V, in a block
+  static constexpr int pieces = blocks * blk_pieces / kPfThreads;  // per thread and tensor
+  static constexpr int tensor_bytes = tokens * D * eb;
+  static constexpr int buf_bytes = 2 * tensor_bytes;
+  static constexpr int ksteps = kcols / 2;               // fragments of 32 tokens of K
+  static constexpr int vsteps = tokens / (2 * per);      // fragments of 32 dims of V
+};
+
+// Token (of 32) in row m of the score product: see the header. (fp32 products
+// take two tokens at a time, one per lane half: rows in their order.)
+template <bool F32>
+__device__ __forceinline__ int row_of_token(int t) {
+  // token 16 a + 8 h + 4 b + j -> row 16 a + 8 b + 4 h + j
+  return F32 ? t : (t & 0x13) | (t & 8) >> 1 | (t & 4) << 1;
+}
+// The token of accumulator register r in lane half 0 (half 1: 8, or 4, more).
+template <bool F32>
+__host__ __device__ constexpr int reg_token(int r) {
+  return F32 ? 8 * (r >> 2) + (r & 3) : 16 * (r >> 3) + (r & 7);
+}
+
+// Byte of the LDS place of K piece (token of the tile, column) and V piece
+// (dim, column of the tile's tokens).
+template <int D, int KV>
+__device__ __forceinline__ int k_place(int tok, int col) {
+  using G = PfGeo<D, KV>;
+  const int m = row_of_token<G::f32>(tok & 31);
+  return ((tok >> 5) * G::ksteps + (col >> 1)) * 1024 + (col & 1) * 512 + ((m ^ (col & 15)) << 4);
+}
+template <int D, int KV>
+__device__ __forceinline__ int v_place(int dim, int col) {
+  using G = PfGeo<D, KV>;
+  return ((dim >> 5) * G::vsteps + (col >> 1)) * 1024 + (col & 1) * 512 +
+         (((dim & 31) ^ ((col & (G::vcols - 1)) * (16 / G::vcols))) << 4);
+}
+
+// A thread's pieces of a tile on their way from the cache.
+template <int D, int KV>
+struct PfRegs {
+  typedef typename std::conditional<
+      KV == kKvMx4, uint32_t, typename std::conditional<KV == kKvFp8, uint2, uint4>::type>::type T;
+  T k[PfGeo<D, KV>::pieces], v[PfGeo<D, KV>::pieces];
+  // 4-bit caches: scale bytes.
+  uint32_t ks[KV == kKvMx4 ? PfGeo<D, KV>::pieces : 1];
+  uint2 vs[KV == kKvMx4 ? PfGeo<D, KV>::pieces : 1];
+};
+
+template <int KV, typename T>
+__device__ __forceinline__ uint4 staged(T raw) {
+  if constexpr (KV == kKvFp8)
+    return fp8x8_to_bf16x8(raw);
+  else
+    return raw;
+}
+
+// Zeroes the elements from `keep` on.
+template <bool F32>
+__device__ __forceinline__ void keep_first(uint4& x, int keep) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F32)
+      w[i] = i < keep ? w[i] : 0u;
+    else
+      w[i] &= (2 * i < keep ? 0xFFFFu : 0u) | (2 * i + 1 < keep ? 0xFFFF0000u : 0u);
+  }
+}
+// Zeroes elements that are not finite; the first one's place (or 8).
+template <bool F32>
+__device__ __forceinline__ int drop_nonfinite(uint4& x) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+  int first = 8;
+#pragma unroll
+  for (int i = 3; i >= 0; --i) {
+    if constexpr (F32) {
+      if ((w[i] & 0x7F800000u) == 0x7F800000u) {
+        w[i] = 0u;
+        first = i;
+      }
+    } else {
+      if ((w[i] & 0x7F800000u) == 0x7F800000u) {
+        w[i] &= 0xFFFFu;
+        first = 2 * i + 1;
+      }
+      if ((w[i] & 0x7F80u) == 0x7F80u) {
+        w[i] &= 0xFFFF0000u;
+        first = 2 * i;
+      }
+    }
+  }
+  return first;
+}
+
+struct PfItem {
+  int seq, n, len;  // its new tokens and its length
+  int row0;         // first row (token x g + head of the group) of the tile
+  int64_t tok0;     // first new token's row of q
+};
+
+// The sequence of an item (as in the rotating append: every wave alone, in
+// bounds whatever the offsets hold).
+__device__ __forceinline__ PfItem prefill_item(const PrefillParams& p, int64_t item) {
+  const int lane = threadIdx.x & 63;
+  auto first = [&](int64_t b) { return static_cast<int64_t>(p.tok_offsets[b]) * p.g / kPrefillRows + b; };
+  int64_t lo = 0, hi = p.num_seqs;
+  while (hi - lo > 1) {
+    const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const bool le = lane == 0 || (at < hi && first(at) <= item);
+    lo += (__builtin_popcountll(__builtin_amdgcn_ballot_w64(le)) - 1) * step;
+    hi = hi < lo + step ? hi : lo + step;
+  }
+  PfItem it;
+  it.seq = __builtin_amdgcn_readfirstlane(static_cast<int>(lo));
+  const int t0 = p.tok_offsets[it.seq], t1 = p.tok_offsets[it.seq + 1];
+  it.tok0 = t0;
+  it.n = t1 - t0;
+  it.len = p.seq_lens[it.seq];
+  const int64_t row0 = (item - first(it.seq)) * kPrefillRows;
+  if (t0 < 0 || t1 < t0 || t1 > p.num_tokens || row0 < 0 || row0 >= static_cast<int64_t>(it.n) * p.g) it.n = 0;
+  it.row0 = static_cast<int>(row0);
+  return it;
+}
+
+template <int D, int KV>
+__global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p) {
+  using G = PfGeo<D, KV>;
+  using C = KvGeo<D, KV>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * G::buf_bytes];
+  __shared__ int bad_dim[D];  // first token whose value in this dim is not finite (tiles with hidden tokens)
+
+  // Units in the order (tile of rows, split, KV head), the last tiles of a
+  // call (which see the most tokens) first: KV heads side by side, so that
+  // the XCDs (workgroups are dealt to them in turn) read few heads each.
+  const int64_t unit = p.units - 1 - (p.unit0 + blockIdx.x);
+  const int kvh = static_cast<int>(unit % p.hkv), split = static_cast<int>(unit / p.hkv % p.nsplit);
+  const PfItem it = prefill_item(p, unit / p.hkv / p.nsplit);
+  if (it.n <= 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nrows = it.n * p.g - it.row0 < kPrefillRows ? it.n * p.g - it.row0 : kPrefillRows;
+  const int row = it.row0 + 32 * wave + ln;  // this lane's row of the sequence
+  const bool active = 32 * wave + ln < nrows;
+  const int64_t orow = (it.tok0 + row / p.g) * p.hq + kvh * p.g + row % p.g;
+  // Tokens it sees: 0 .. lim. A sequence of length 0, one shorter than its
+  // new tokens or longer than its table: no tokens.
+  const bool bad = it.len > 0 && (it.len < it.n || it.len > p.max_seq_len || (it.len + kTok - 1) / kTok > p.max_blocks);
+  const int before = it.len > 0 && !bad ? it.len - it.n : -1;  // tokens cached before the new ones
+  const int lim = active && before >= 0 ? before + row / p.g : -1;
+  const int wave_row = it.row0 + 32 * wave;
+  const int first_lim = before >= 0 ? before + wave_row / p.g : -1;  // what the wave's first row sees,
+  const int last_row = wave_row + 31 < it.row0 + nrows - 1 ? wave_row + 31 : it.row0 + nrows - 1;
+  const int wave_lim = 32 * wave < nrows && before >= 0 ? before + last_row / p.g : -1;  // and its last
+  const int seen = before >= 0 ? before + (it.row0 + nrows - 1) / p.g + 1 : 0;  // tokens the tile of rows sees
+  const int all_see = before >= 0 ? before + it.row0 / p.g : -1;                // the last token that every row sees
+  const int ntiles = (seen + G::tokens - 1) / G::tokens;
+  const int tile0 = static_cast<int>(static_cast<int64_t>(ntiles) * split / p.nsplit);
+  const int tile1 = static_cast<int>(static_cast<int64_t>(ntiles) * (split + 1) / p.nsplit);
+
+  for (int i = tid; i < D; i += kPfThreads) bad_dim[i] = 0x7FFFFFFF;
+
+  typedef typename std::conditional<G::f32, f32x4, uint4>::type Frag;
+  // Query rows as the B operand.
+  Frag q[G::ksteps];
+  {
+    const unsigned char* src = static_cast<const unsigned char*>(p.q) + orow * D * G::eb;
+#pragma unroll
+    for (int s = 0; s < G::ksteps; ++s)
+      q[s] = active ? *reinterpret_cast<const Frag*>(src + (2 * s + half) * 16) : Frag{0, 0, 0, 0};
+  }
+
+  const size_t blk_stride = static_cast<size_t>(p.hkv) * C::blk_bytes;
+  const unsigned char* kbase = static_cast<const unsigned char*>(p.k_cache) + static_cast<size_t>(kvh) * C::blk_bytes;
+  const unsigned char* vbase = static_cast<const unsigned char*>(p.v_cache) + static_cast<size_t>(kvh) * C::blk_bytes;
+  const int32_t* table = p.block_tables + static_cast<int64_t>(it.seq) * p.max_blocks;
+  const int nblk = (seen + kTok - 1) / kTok;
+  int first_bad = 0x7FFFFFFF;  // first token of a block that is not in the pool
+
+  // Block ids of a tile (-1: none to read), uniform over the workgroup.
+  struct Ids {
+    int id[G::blocks];
+  };
+  auto load_ids = [&](int tile) {
+    Ids x;
+#pragma unroll
+    for (int i = 0; i < G::blocks; ++i) {
+      const int lb = tile * G::blocks + i;
+      x.id[i] = tile < tile1 && lb < nblk ? table[lb] : -1;
+    }
+    return x;
+  };
+  auto check_ids = [&](Ids& x, int tile) {
+#pragma unroll
+    for (int i = 0; i < G::blocks; ++i) {
+      const int lb = tile * G::blocks + i;
+      if (tile < tile1 && lb < nblk && (x.id[i] < 0 || x.id[i] >= p.num_blocks)) {
+        first_bad = first_bad < lb * kTok ? first_bad : lb * kTok;
+        x.id[i] = -1;
+      }
+    }
+  };
+  struct Scales {  // fp8
+    float k[G::blocks], v[G::blocks];
+  };
+  auto load_scales = [&](const Ids& x) {
+    Scales s;
+    if constexpr (KV == kKvFp8) {
+#pragma unroll
+      for (int i = 0; i < G::blocks; ++i) {
+        s.k[i] = x.id[i] >= 0 ? p.k_scale[x.id[i]] : 0.f;
+        s.v[i] = x.id[i] >= 0 ? p.v_scale[x.id[i]] : 0.f;
+      }
+    }
+    return s;
+  };
+  // A V scale that is not finite makes every value of its block infinite or
+  // NaN: the rows that see the block are NaN, and the others never meet it.
+  auto check_scales = [&](Scales& s, int tile) {
+    if constexpr (KV == kKvFp8) {
+#pragma unroll
+      for (int i = 0; i < G::blocks; ++i)
+        if (!(__builtin_fabsf(s.v[i]) < __builtin_inff())) {
+          const int tok = tile * G::tokens + i * kTok;
+          first_bad = first_bad < tok ? first_bad : tok;
+          s.v[i] = 0.f;
+        }
+    }
+  };
+  auto load_tile = [&](PfRegs<D, KV>& r, const Ids& x) {
+    typedef typename PfRegs<D, KV>::T T;
+#pragma unroll
+    for (int i = 0; i < G::pieces; ++i) {
+      const int piece = tid + kPfThreads * i;
+      const int blk = __builtin_amdgcn_readfirstlane(piece / G::blk_pieces), at = piece % G::blk_pieces;
+      int id = -1;
+#pragma unroll
+      for (int k = 0; k < G::blocks; ++k) id = blk == k ? x.id[k] : id;
+      r.k[i] = T{};
+      r.v[i] = T{};
+      if constexpr (KV == kKvMx4) {
+        r.ks[i] = 0u;
+        r.vs[i] = uint2{0u, 0u};
+      }
+      if (id < 0) continue;  // uniform over the wave
+      const unsigned char* kb = kbase + id * blk_stride;
+      const unsigned char* vb = vbase + id * blk_stride;
+      r.k[i] = *reinterpret_cast<const T*>(kb + at * static_cast<int>(sizeof(T)));
+      r.v[i] = *reinterpret_cast<const T*>(vb + at * static_cast<int>(sizeof(T)));
+      if constexpr (KV == kKvMx4) {
+        r.ks[i] = kb[C::code_bytes + at * 8 / kMxGroup];
+        r.vs[i] = *reinterpret_cast<const uint2*>(vb + C::code_bytes + at / G::vcols / kMxGroup * kTok + 8 * (at % G::vcols));
+      }
+    }
+  };
+  auto store_tile = [&](const PfRegs<D, KV>& r, int tile) {
+    unsigned char* buf = lds + (tile & 1) * G::buf_bytes;
+    // Values past the last token seen are unused slots; those that some rows
+    // see and others do not may hold infinities or NaN, which a zero
+    // probability would not keep out.
+    const bool edge = (tile + 1) * G::tokens > seen, hidden = (tile + 1) * G::tokens - 1 > all_see;
+#pragma unroll
+    for (int i = 0; i < G::pieces; ++i) {
+      const int piece = tid + kPfThreads * i;
+      const int blk = piece / G::blk_pieces, at = piece % G::blk_pieces;
+      const int dim = at / G::vcols, vcol = blk * G::vcols + at % G::vcols;
+      uint4 k, v;
+      if constexpr (KV == kKvMx4) {
+        k = mx4x8_to_bf16x8(r.k[i], mx_scale<0>(r.ks[i]));
+        v = mx4x8_to_bf16x8(r.v[i], r.vs[i]);
+      } else {
+        k = staged<KV>(r.k[i]);
+        v = staged<KV>(r.v[i]);
+      }
+      const int tok = tile * G::tokens + vcol * G::per;  // V piece's first token
+      if (edge) keep_first<G::f32>(v, seen - tok);
+      if (hidden) {
+        const int at_bad = drop_nonfinite<G::f32>(v);
+        if (at_bad < 8) atomicMin(&bad_dim[dim], tok + at_bad);
+      }
+      *reinterpret_cast<uint4*>(buf + k_place<D, KV>(blk * kTok + at / G::kcols, at % G::kcols)) = k;
+      *reinterpret_cast<uint4*>(buf + G::tensor_bytes + v_place<D, KV>(dim, vcol)) = v;
+    }
+  };
+
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  float ref = kNegInf, sum = 0.f;  // reference of the row (both halves alike), this lane's part of the sum
+
+  if (tile0 < tile1) {
+    PfRegs<D, KV> regs;
+    Ids ids = load_ids(tile0);
+    check_ids(ids, tile0);
+    load_tile(regs, ids);
+    Scales scales = load_scales(ids), next_scales;
+    ids = load_ids(tile0 + 1);
+    __syncthreads();  // bad_dim is set
+    store_tile(regs, tile0);
+    check_ids(ids, tile0 + 1);
+    load_tile(regs, ids);
+    next_scales = load_scales(ids);
+    ids = load_ids(tile0 + 2);
+    __syncthreads();
+    for (int tile = tile0; tile < tile1; ++tile) {
+      check_scales(scales, tile);
+      const unsigned char* kbuf = lds + (tile & 1) * G::buf_bytes;
+      const unsigned char* vbuf = kbuf + G::tensor_bytes;
+      const int t0 = tile * G::tokens;
+      if (t0 <= wave_lim) {
+        f32x16 s[G::tokens / 32];
+#pragma unroll
+        for (int t = 0; t < G::tokens / 32; ++t) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+          for (int j = 0; j < G::ksteps; ++j) {
+            const Frag k = *reinterpret_cast<const Frag*>(kbuf + (t * G::ksteps + j) * 1024 + half * 512 +
+                                                          ((ln ^ ((2 * j + half) & 15)) << 4));
+            if constexpr (G::f32) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[j][e], s[t], 0, 0, 0);
+            } else {
+              s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
+                                                             __builtin_bit_cast(bf16x8, q[j]), s[t], 0, 0, 0);
+            }
+          }
+        }
+        // Scores in log2 units; hidden tokens -inf.
+        const bool partly = t0 + G::tokens - 1 > first_lim;
+        const int left = lim - t0 - half * (G::f32 ? 4 : 8);
+        float mx = kNegInf;
+#pragma unroll
+        for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int tok = 32 * t + reg_token<G::f32>(i);
+            float sc = p.scale_log2;
+            if constexpr (KV == kKvFp8) sc *= scales.k[tok / kTok];
+            s[t][i] *= sc;
+            if (partly) s[t][i] = tok <= left ? s[t][i] : kNegInf;
+            mx = fmaxf(mx, s[t][i]);
+          }
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (__builtin_amdgcn_ballot_w64(mx > ref + kRefSlack || (ref == kNegInf && mx > kNegInf)) != 0) {
+          const float now = mx > ref ? mx : ref;
+          const float f = ref == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ref - now);
+          sum *= f;
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) o[d] *= f;
+          ref = now;
+        }
+        const float sub = ref == kNegInf ? 0.f : ref;
+#pragma unroll
+        for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - sub);
+            sum += s[t][i];
+          }
+#pragma unroll
+        for (int j = 0; j < G::vsteps; ++j) {
+          if constexpr (G::f32) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+              const Frag v = *reinterpret_cast<const Frag*>(
+                  vbuf + (d * G::vsteps + j) * 1024 + half * 512 +
+                  ((ln ^ (((2 * j + half) & (G::vcols - 1)) * (16 / G::vcols))) << 4));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], s[0][4 * j + e], o[d], 0, 0, 0);
+            }
+          } else {
+            float pv[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              pv[e] = s[j >> 1][8 * (j & 1) + e];
+              if constexpr (KV == kKvFp8) pv[e] *= scales.v[j];
+            }
+            const uint4 pb = {pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
+                              pack_bf16x2(pv[6], pv[7])};
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+              const Frag v = *reinterpret_cast<const Frag*>(vbuf + (d * G::vsteps + j) * 1024 + half * 512 +
+                                                            ((ln ^ (half * 8)) << 4));
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v),
+                                                             __builtin_bit_cast(bf16x8, pb), o[d], 0, 0, 0);
+            }
+          }
+        }
+      }
+      if (tile + 1 < tile1) {
+        store_tile(regs, tile + 1);
+        scales = next_scales;
+        check_ids(ids, tile + 2);
+        load_tile(regs, ids);
+        next_scales = load_scales(ids);
+        ids = load_ids(tile + 3);
+      }
+      __syncthreads();
+    }
+  }
+  if (!active) return;
+
+  sum += __shfl_xor(sum, 32);
+  const float qnan = __builtin_nanf("");
+  const bool nan_row = bad || lim >= first_bad;
+  if (nan_row) sum = qnan;
+  // Lane (row, half): dims 32 d + 8 i + 4 half .. + 4.
+  const float f = p.nsplit > 1 ? 1.f : (nan_row ? qnan : (sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : qnan)));
+  const int64_t part_row = static_cast<int64_t>(split) * p.num_tokens * p.hq + orow;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int dim = 32 * d + 8 * i + 4 * half;
+      f32x4 x = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+      x *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (tile0 < tile1 && lim >= bad_dim[dim + e]) x[e] = qnan;
+      if (p.nsplit > 1)
+        *reinterpret_cast<f32x4*>(p.part_o + part_row * D + dim) = x;
+      else
+        store_out4(p.out, p.out_bf16 != 0, orow * D + dim, x);
+    }
+  if (p.nsplit > 1 && half == 0)
+    *reinterpret_cast<f32x2*>(p.part_ml + 2 * part_row) = f32x2{ref, sum};
+}
+
+// The splits of a row joined, in their order. A wave per row; lane j holds
+// split j's reference and sum (at most kPrefillMaxSplit of them). Rows
+// behind the last sequence are left as they are.
+template <int D>
+__global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillParams p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r = p.unit0 + static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t rows = static_cast<int64_t>(p.num_tokens) * p.hq;
+  if (r >= rows || r / p.hq < p.tok_offsets[0] || r / p.hq >= p.tok_offsets[p.num_seqs]) return;
+  f32x2 ml = {kNegInf, 0.f};
+  if (lane < p.nsplit) ml = *reinterpret_cast<const f32x2*>(p.part_ml + 2 * (lane * rows + r));
+  const bool nan = __builtin_amdgcn_ballot_w64(ml.y != ml.y) != 0;
+  float mx = ml.x;
+#pragma unroll
+  for (int o = 1; o < kPrefillMaxSplit; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  const float w = ml.x == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ml.x - mx);
+  float den = ml.y * w;
+#pragma unroll
+  for (int o = 1; o < kPrefillMaxSplit; o <<= 1) den += __shfl_xor(den, o);
+  constexpr int kEl = D / 64;
+  float acc[kEl] = {};
+  for (int k = 0; k < p.nsplit; ++k) {
+    const float wk = __shfl(w, k);
+#pragma unroll
+    for (int e = 0; e < kEl; ++e) acc[e] += wk * p.part_o[(k * rows + r) * D + kEl * lane + e];
+  }
+  den = __shfl(den, 0);
+  const float inv = nan ? __builtin_nanf("") : (den > 0.f ? 1.f / den : 0.f);
+#pragma unroll
+  for (int e = 0; e < kEl; ++e) {
+    const int64_t at = r * D + kEl * lane + e;
+    const float x = acc[e] * inv;
+    if (p.out_bf16)
+      static_cast<uint16_t*>(p.out)[at] = static_cast<uint16_t>(pack_bf16x2(x, x));
+    else
+      static_cast<float*>(p.out)[at] = x;
+  }
+}
+
+template <int D, int KV>
+hipError_t launch_prefill_t(PrefillParams p, hipStream_t stream) {
+  // (A launch holds fewer than 2^32 threads.)
+  constexpr int64_t kMost = 0xFFFFFFFFll / kPfThreads;
+  p.units = prefill_items(p.num_seqs, p.num_tokens, p.g) * p.hkv * p.nsplit;
+  for (p.unit0 = 0; p.unit0 < p.units; p.unit0 += kMost) {
+    const int64_t n = p.units - p.unit0 < kMost ? p.units - p.unit0 : kMost;
+    hipLaunchKernelGGL((prefill_kernel<D, KV>), dim3(static_cast<unsigned>(n)), dim3(kPfThreads), 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (p.nsplit > 1) {
+    const int64_t rows = static_cast<int64_t>(p.num_tokens) * p.hq;
+    constexpr int64_t kMostRows = 0xFFFFFFFFll / 256 * 4;
+    for (p.unit0 = 0; p.unit0 < rows; p.unit0 += kMostRows) {
+      const int64_t n = rows - p.unit0 < kMostRows ? rows - p.unit0 : kMostRows;
+      hipLaunchKernelGGL((prefill_merge_kernel<D>), dim3(static_cast<unsigned>((n + 3) / 4)), dim3(256), 0, stream, p);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+template <int D>
+hipError_t launch_prefill_d(const PrefillParams& p, int kv_kind, hipStream_t stream) {
+  switch (kv_kind) {
+    case kKvF32: return launch_prefill_t<D, kKvF32>(p, stream);
+    case kKvBf16: return launch_prefill_t<D, kKvBf16>(p, stream);
+    case kKvFp8: return launch_prefill_t<D, kKvFp8>(p, stream);
+    default: return launch_prefill_t<D, kKvMx4>(p, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_prefill(const PrefillParams& p, int head_dim, int kv_kind, hipStream_t stream) {
+  return head_dim == 128 ? launch_prefill_d<128>(p, kv_kind, stream) : launch_prefill_d<64>(p, kv_kind, stream);
+}
+
+}  // namespace tts

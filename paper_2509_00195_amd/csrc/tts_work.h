@@ -95,7 +95,7 @@ struct AttnParams {
   const float* v_scale;
   const int32_t* block_tables;
   const int32_t* seq_lens;
-  float* out;
+  void* out;       // fp32, or bf16 where out_bf16
   void* part_o;    // [rows][D] fp16 (fp32 for fp32 caches), lane order
   float* part_ml;  // [rows][kPartMl]: m, l, z, 0
   // prefix path (null recs: paged path)
@@ -118,6 +118,7 @@ struct AttnParams {
   // Some unit of the plan has a second entry window: selects the kernel
   // build that reads them (the other keeps the pair loop's registers).
   int32_t two_windows;
+  int32_t out_bf16;
 };
 
 // Readable int32 words after the start of any slot-table row (the table is
@@ -132,10 +133,10 @@ struct MergeParams {
   // (KV head 0) for each slot in merge order; null for the paged path
   const int32_t* slot_tab;
   int32_t slot_stride;
-  int32_t pad0;
+  int32_t out_bf16;
   const int32_t* seq_lens;
   const int32_t* build_len;  // prefix path: stale-metadata check (else null)
-  float* out;
+  void* out;  // fp32, or bf16 where out_bf16
   int32_t num_seqs;
   int32_t hq;
   int32_t g;

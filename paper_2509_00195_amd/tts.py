@@ -30,8 +30,8 @@ TTS_ERR_NOMEM = -6
 STATUS_NAMES = {0: "TTS_OK", -1: "TTS_ERR_INVALID_ARG", -2: "TTS_ERR_UNSUPPORTED", -3: "TTS_ERR_OUT_OF_RANGE",
                 -4: "TTS_ERR_WORKSPACE", -5: "TTS_ERR_HIP", -6: "TTS_ERR_NOMEM"}
 
-TTS_F32, TTS_BF16, TTS_FP8_E4M3 = 0, 1, 2
-DTYPES = {"f32": TTS_F32, "bf16": TTS_BF16, "fp8": TTS_FP8_E4M3}
+TTS_F32, TTS_BF16, TTS_FP8_E4M3, TTS_MXFP4 = 0, 1, 2, 3
+DTYPES = {"f32": TTS_F32, "bf16": TTS_BF16, "fp8": TTS_FP8_E4M3, "mx4": TTS_MXFP4}
 
 EXPORTED = [
     "tts_build_prefix_meta", "tts_prefix_meta_destroy", "tts_prefix_meta_export", "tts_prefix_meta_coverage",
@@ -40,7 +40,8 @@ EXPORTED = [
     "tts_prefix_decode_partials",
     "tts_prefix_decode_merge", "tts_append_kv", "tts_copy_blocks", "tts_fork_tables", "tts_kv_alloc_time",
     "tts_kv_alloc_search", "tts_prefix_schedule", "tts_build_verify_meta", "tts_prefix_verify_attn",
-    "tts_last_error", "tts_fork_prefix_meta", "tts_truncated_lengths",
+    "tts_last_error", "tts_fork_prefix_meta", "tts_truncated_lengths", "tts_rope_append_kv", "tts_rope_tables",
+    "tts_paged_prefill_workspace_size", "tts_paged_prefill_attn",
 ]
 
 
@@ -54,6 +55,11 @@ class tts_attn_desc(C.Structure):
     _fields_ = [("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("block_size", C.c_int32), ("q_dtype", C.c_int), ("kv_dtype", C.c_int), ("out_dtype", C.c_int),
                 ("scale", C.c_float)]
+
+
+class tts_rope_desc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("max_pos", C.c_int32), ("cos", C.c_void_p),
+                ("sin", C.c_void_p)]
 
 
 class tts_model_cost(C.Structure):
@@ -143,6 +149,16 @@ def load() -> C.CDLL:
     lib.tts_prefix_decode_merge.argtypes = [P(tts_attn_desc), VP, VP, VP, VP, C.c_size_t, VP]
     lib.tts_append_kv.restype = C.c_int
     lib.tts_append_kv.argtypes = [P(tts_attn_desc), I32, VP, VP, VP, I32, VP, I32, VP, VP, VP, VP, VP]
+    lib.tts_rope_append_kv.restype = C.c_int
+    lib.tts_rope_append_kv.argtypes = [P(tts_attn_desc), P(tts_rope_desc), I32, I32, VP, VP, VP, I64, VP, I64, VP, I64,
+                                       VP, I32, VP, I32, VP, VP, VP, VP, VP, VP]
+    lib.tts_rope_tables.restype = C.c_int
+    lib.tts_rope_tables.argtypes = [I32, C.c_double, I32, P(C.c_float), P(C.c_float)]
+    lib.tts_paged_prefill_workspace_size.restype = C.c_size_t
+    lib.tts_paged_prefill_workspace_size.argtypes = [P(tts_attn_desc), I32, I32, I32]
+    lib.tts_paged_prefill_attn.restype = C.c_int
+    lib.tts_paged_prefill_attn.argtypes = [P(tts_attn_desc), I32, I32, VP, VP, VP, VP, VP, VP, VP, I32, VP, I32, I32, VP,
+                                           VP, C.c_size_t, VP]
     lib.tts_copy_blocks.restype = C.c_int
     lib.tts_copy_blocks.argtypes = [P(tts_attn_desc), I32, VP, I32, VP, VP, VP, VP, VP]
     lib.tts_kv_alloc_time.restype = C.c_int
@@ -410,6 +426,63 @@ def tts_append_kv(desc: tts_attn_desc, num_seqs: int, k_new, v_new, block_tables
     _check(load().tts_append_kv(
         C.byref(desc), num_seqs, _ptr(k_new), _ptr(v_new), _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens),
         num_blocks, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+
+
+def tts_rope_tables(rot_dim: int, theta: float, max_pos: int):
+    """Host call; returns (cos, sin), float32 [max_pos][rot_dim / 2]."""
+    shape = (max(max_pos, 0), max(rot_dim, 0) // 2)
+    cos, sin = np.zeros(shape, np.float32), np.zeros(shape, np.float32)
+    ptr = lambda a: a.ctypes.data_as(C.POINTER(C.c_float))  # noqa: E731
+    _check(load().tts_rope_tables(rot_dim, float(theta), max_pos, ptr(cos), ptr(sin)))
+    return cos, sin
+
+
+def make_rope(cos, sin, interleaved: bool = False) -> tts_rope_desc:
+    """The rotation by device tables cos and sin, float32 [max_pos][rot_dim / 2] (which the caller keeps)."""
+    if cos.shape != sin.shape or cos.ndim != 2:
+        raise ValueError("cos and sin must both be [max_pos][rot_dim / 2]")
+    if "float32" not in str(cos.dtype) or "float32" not in str(sin.dtype):
+        raise ValueError("cos and sin must be float32")
+    return tts_rope_desc(2 * int(cos.shape[1]), int(bool(interleaved)), int(cos.shape[0]), _ptr(cos), _ptr(sin))
+
+
+def _rows(x, heads: int, head_dim: int):
+    """(address, elements between tokens) of [tokens][heads][head_dim] rows whose tokens may lie apart."""
+    if x is None:
+        return None, 0
+    if isinstance(x, int):
+        return x, heads * head_dim
+    if x.ndim != 3 or tuple(x.shape[1:]) != (heads, head_dim):
+        raise ValueError(f"expected rows of [{heads}][{head_dim}], got {tuple(x.shape)}")
+    if x.shape[0] and (x.stride(2) != 1 or x.stride(1) != head_dim):
+        raise ValueError("the heads of a token must be contiguous")
+    return x.data_ptr(), int(x.stride(0)) if x.shape[0] > 1 else heads * head_dim
+
+
+def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_new, v_new, block_tables,
+                       max_blocks_per_seq: int, seq_lens, num_blocks: int, k_cache, v_cache, k_scale=None, v_scale=None,
+                       rope: Optional[tts_rope_desc] = None, q=None, q_out=None, tok_offsets=None, positions=None,
+                       stream=None):
+    """q, k_new and v_new: [tokens][heads][head_dim], possibly views of one projection's output."""
+    hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, hq, d), _rows(k_new, hkv, d), _rows(v_new, hkv, d)
+    _check(load().tts_rope_append_kv(
+        C.byref(desc), C.byref(rope) if rope is not None else None, num_seqs, num_tokens, _ptr(tok_offsets),
+        _ptr(positions), qp, qs, kp, ks, vp, vs, _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens), num_blocks,
+        _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+
+
+def tts_paged_prefill_workspace_size(desc: tts_attn_desc, num_seqs: int, num_tokens: int, max_seq_len: int) -> int:
+    return int(load().tts_paged_prefill_workspace_size(C.byref(desc), num_seqs, num_tokens, max_seq_len))
+
+
+def tts_paged_prefill_attn(desc: tts_attn_desc, num_seqs: int, num_tokens: int, tok_offsets, q, k_cache, v_cache,
+                           k_scale, v_scale, block_tables, max_blocks_per_seq: int, seq_lens, max_seq_len: int,
+                           num_blocks: int, out, workspace, workspace_bytes: int, stream=None):
+    _check(load().tts_paged_prefill_attn(
+        C.byref(desc), num_seqs, num_tokens, _ptr(tok_offsets), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+        _ptr(v_scale), _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens), max_seq_len, num_blocks, _ptr(out),
+        _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def tts_copy_blocks(desc: tts_attn_desc, num_pairs: int, pairs, num_blocks: int, k_cache, v_cache, k_scale=None,
