@@ -1,0 +1,217 @@
+"""Attention over 4-bit caches, and bf16 outputs of every cache, against 64 bits."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_00195_amd import (tts_build_prefix_meta, tts_build_verify_meta, tts_paged_decode_attn,
+                                  tts_paged_decode_workspace_size, tts_plan_units_host, tts_prefix_decode_attn,
+                                  tts_prefix_decode_attn_noalloc,
+                                  tts_prefix_decode_merge, tts_prefix_decode_partials, tts_prefix_decode_workspace_size,
+                                  tts_prefix_verify_attn)
+from tests._cached import BS, DEV, KINDS, Cache, close, desc_of, queries, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def _up(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def _paged(c, desc, q, out, lens=None, tables=None, most=None):
+    lens = c.lens if lens is None else lens
+    t = c.tables if tables is None else tables
+    most = int(max(lens.max(), 1)) if most is None else most
+    size = tts_paged_decode_workspace_size(desc, len(lens), most)
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device=DEV)
+    tts_paged_decode_attn(desc, len(lens), q, *c.device(), _up(t), t.shape[1], _up(lens), most, c.nb, out, ws, size)
+    torch.cuda.synchronize()
+
+
+def _check(c, out, qv, rounded, skip=()):
+    for b in range(len(c.lens)):
+        if b in skip:
+            continue
+        if c.lens[b] == 0:
+            assert (out[b] == 0).all()
+            continue
+        want, tol = reference(c, b, qv[b][None])
+        close(out[b][None], want, tol, rounded)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 64), (15, 5, 64), (28, 4, 128), (12, 2, 128), (16, 16, 64), (34, 2, 128),
+                                      (40, 1, 64)])
+@pytest.mark.parametrize("out_t", ["f32", "bf16"])
+def test_paged(hq, hkv, d, out_t):
+    """Lengths around blocks, pairs and the splits of 512 tokens; unused slots and blocks hold NaN scales."""
+    rng = np.random.default_rng(0)
+    c = Cache("mx4", hkv, d, [1, 0, 15, 16, 17, 31, 32, 33, 511, 512, 513, 700], rng)
+    c.poison()
+    q, qv = queries("mx4", (len(c.lens), hq, d), rng, 2.0)
+    out = torch.full((len(c.lens), hq, d), 5.0, dtype=torch.float32 if out_t == "f32" else torch.bfloat16, device=DEV)
+    _paged(c, desc_of("mx4", hq, hkv, d, out_t), q, out)
+    _check(c, out, qv, out_t == "bf16")
+    # short enough for one split: written without a merge
+    s = Cache("mx4", hkv, d, [1, 0, 40, 16], rng)
+    s.poison()
+    _paged(s, desc_of("mx4", hq, hkv, d, out_t), q[:4].contiguous(), out[:4])
+    _check(s, out, qv, out_t == "bf16")
+
+
+def test_paged_errors_and_special_scales():
+    rng = np.random.default_rng(1)
+    c = Cache("mx4", 2, 64, [40, 40, 40, 40, 40], rng)
+    half = BS * 64 // 2
+    # sequence 1: a NaN scale in a K group; 2: in a V group (its 32 dims alone); 3: scale bytes 0 (2^-127)
+    c.k[c.tables[1, 1], 0, half + 3] = 255
+    c.v[c.tables[2, 0], 1, half + BS + 4] = 255
+    c.k[c.tables[3, 0], 0, half:half + 2 * BS] = 0
+    c.v[c.tables[3, 0], 0, half:half + 2 * BS] = 0
+    tables = c.tables.copy()
+    tables[4, 2] = c.nb
+    q, qv = queries("mx4", (5, 4, 64), rng)
+    out = torch.zeros((5, 4, 64), device=DEV)
+    _paged(c, desc_of("mx4", 4, 2, 64), q, out, tables=tables)
+    got = out.cpu().numpy()
+    assert np.isnan(got[4]).all() and np.isnan(got[1, :2]).all() and np.isfinite(got[1, 2:]).all()
+    assert np.isnan(got[2, 2:, 32:]).all() and np.isfinite(got[2, 2:, :32]).all() and np.isfinite(got[2, :2]).all()
+    _check(c, out, qv, False, skip=(1, 2, 4))
+    _paged(c, desc_of("mx4", 4, 2, 64), q, out, lens=np.array([41, 40, 40, 40, -1], np.int32), most=40)
+    assert np.isnan(out[0].cpu().numpy()).all() and np.isnan(out[4].cpu().numpy()).all()
+
+
+def _tree(kind, hq, hkv, d, rng, beams=24, share=9, lo=170, hi=420, gain=1.0):
+    """Beams of two requests; each request's share `share` blocks, groups of four a further three."""
+    lens = rng.integers(lo, hi, beams)
+    c = Cache(kind, hkv, d, lens, rng, gain=gain)
+    half = beams // 2
+    for b in range(beams):
+        first, group = b // half * half, b // half * half + b % half // 4 * 4
+        c.tables[b, :share] = c.tables[first, :share]
+        c.tables[b, share:share + 3 - 2] = c.tables[group, share:share + 1]
+    return c, np.array([0, half, beams], np.int32)
+
+
+@pytest.mark.parametrize("kind,out_t", [("mx4", "f32"), ("mx4", "bf16"), ("bf16", "bf16"), ("fp8", "bf16"), ("f32", "bf16")])
+@pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (15, 5, 64), (16, 1, 64)])
+def test_prefix(kind, out_t, hq, hkv, d):
+    """Shared segments (wide and narrow units) and tails, the workspace, allocation-free and two-launch calls alike; then
+    lengths grown past the metadata's."""
+    rng = np.random.default_rng(2)
+    c, offs = _tree(kind, hq, hkv, d, rng, gain=2.0)
+    c.poison()
+    desc = desc_of(kind, hq, hkv, d, out_t)
+    q, qv = queries(kind, (len(c.lens), hq, d), rng)
+    meta = tts_build_prefix_meta(offs, c.tables, c.lens, BS, c.nb, desc=desc)
+    size = tts_prefix_decode_workspace_size(desc, meta)
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device=DEV)
+    dt = torch.float32 if out_t == "f32" else torch.bfloat16
+    out = torch.full((len(c.lens), hq, d), 5.0, dtype=dt, device=DEV)
+    args = (q, *c.device(), _up(c.tables), c.tables.shape[1], _up(c.lens), c.nb)
+    tts_prefix_decode_attn(desc, meta, *args, out, ws, size)
+    _check(c, out, qv, out_t == "bf16")
+    other = torch.zeros_like(out)
+    tts_prefix_decode_attn_noalloc(desc, meta, *args, other)
+    assert torch.equal(out, other)
+    other.zero_()
+    tts_prefix_decode_partials(desc, meta, *args, other, ws, size)
+    tts_prefix_decode_merge(desc, meta, _up(c.lens), other, ws, size)
+    assert torch.equal(out, other)
+
+
+def test_prefix_growth():
+    """Beams that grew by up to 90 tokens since the metadata was built."""
+    rng = np.random.default_rng(3)
+    c, offs = _tree("mx4", 28, 4, 128, rng)
+    short = np.maximum(c.lens - rng.integers(0, 91, len(c.lens)), 13 * BS).astype(np.int32)
+    short = np.minimum(short, c.lens)
+    desc = desc_of("mx4", 28, 4, 128)
+    q, qv = queries("mx4", (len(c.lens), 28, 128), rng)
+    meta = tts_build_prefix_meta(offs, c.tables, short, BS, c.nb, desc=desc)
+    size = tts_prefix_decode_workspace_size(desc, meta)
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device=DEV)
+    out = torch.zeros((len(c.lens), 28, 128), device=DEV)
+    tts_prefix_decode_attn(desc, meta, q, *c.device(), _up(c.tables), c.tables.shape[1], _up(c.lens), c.nb, out, ws, size)
+    _check(c, out, qv, False)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (16, 2, 64)])
+@pytest.mark.parametrize("gain", [1.0, 6.0])
+def test_wide_units(hq, hkv, d, gain):
+    """Segments shared by many beams, staged in LDS (an odd number of blocks too); at gain 6 with the repeat."""
+    rng = np.random.default_rng(8)
+    c, offs = _tree("mx4", hq, hkv, d, rng, beams=64, share=59, lo=1020, hi=1100, gain=gain)
+    desc = desc_of("mx4", hq, hkv, d)
+    rows, _ = tts_plan_units_host(offs, c.tables, c.lens, BS, c.nb, desc, 256)
+    assert (rows[:, 6] & 8).any()
+    q, qv = queries("mx4", (64, hq, d), rng, gain)
+    meta = tts_build_prefix_meta(offs, c.tables, c.lens, BS, c.nb, desc=desc)
+    size = tts_prefix_decode_workspace_size(desc, meta)
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device=DEV)
+    out = torch.zeros((64, hq, d), device=DEV)
+    tts_prefix_decode_attn(desc, meta, q, *c.device(), _up(c.tables), c.tables.shape[1], _up(c.lens), c.nb, out, ws, size)
+    _check(c, out, qv, False)
+
+
+def test_prefix_scores_beyond_the_reference_window():
+    """Scores of hundreds (log2 units): the exact-maximum repeat, in wide and narrow units."""
+    rng = np.random.default_rng(4)
+    c, offs = _tree("mx4", 28, 4, 128, rng, gain=6.0)
+    desc = desc_of("mx4", 28, 4, 128)
+    q, qv = queries("mx4", (len(c.lens), 28, 128), rng, 8.0)
+    meta = tts_build_prefix_meta(offs, c.tables, c.lens, BS, c.nb, desc=desc)
+    size = tts_prefix_decode_workspace_size(desc, meta)
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device=DEV)
+    out = torch.zeros((len(c.lens), 28, 128), device=DEV)
+    tts_prefix_decode_attn(desc, meta, q, *c.device(), _up(c.tables), c.tables.shape[1], _up(c.lens), c.nb, out, ws, size)
+    _check(c, out, qv, False)
+
+
+@pytest.mark.parametrize("q_len", [1, 3, 8])
+def test_verify(q_len):
+    rng = np.random.default_rng(5)
+    c, offs = _tree("mx4", 15, 5, 64, rng, beams=12)
+    c.poison()
+    desc = desc_of("mx4", 15, 5, 64, "bf16")
+    q, qv = queries("mx4", (len(c.lens), q_len, 15, 64), rng)
+    meta = tts_build_verify_meta(offs, c.tables, c.lens, q_len, BS, c.nb, desc=desc)
+    size = tts_prefix_decode_workspace_size(desc, meta)
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device=DEV)
+    out = torch.zeros((len(c.lens), q_len, 15, 64), dtype=torch.bfloat16, device=DEV)
+    tts_prefix_verify_attn(desc, meta, q, *c.device(), _up(c.tables), c.tables.shape[1], _up(c.lens), c.nb, out, ws, size)
+    for b in range(len(c.lens)):
+        want, tol = reference(c, b, qv[b])
+        close(out[b], want, tol, True)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_paged_bf16_output(kind):
+    rng = np.random.default_rng(6)
+    c = Cache(kind, 3, 64, [0, 1, 40, 600], rng)
+    c.poison()
+    q, qv = queries(kind, (4, 9, 64), rng)
+    out = torch.full((4, 9, 64), 5.0, dtype=torch.bfloat16, device=DEV)
+    _paged(c, desc_of(kind, 9, 3, 64, "bf16"), q, out)
+    _check(c, out, qv, True)
+
+
+def test_long_sequences_past_32_bit_offsets():
+    """70,000 tokens split and joined, in the last blocks of a cache of over 4 GiB per tensor."""
+    rng = np.random.default_rng(7)
+    hkv, d = 2, 128
+    c = Cache("mx4", hkv, d, [70001], rng, spare=0)
+    per = hkv * 17 * d // 2
+    nb = (1 << 32) // per + c.nb
+    k, v, _, _ = c.device()
+    big = [torch.empty((nb, per), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    for x, y in zip(big, (k, v)):
+        x[nb - c.nb:] = y.reshape(c.nb, -1)
+    t = np.where(c.tables >= 0, c.tables + (nb - c.nb), c.tables).astype(np.int32)
+    desc = desc_of("mx4", 4, hkv, d)
+    q, qv = queries("mx4", (1, 4, d), rng)
+    out = torch.zeros((1, 4, d), device=DEV)
+    size = tts_paged_decode_workspace_size(desc, 1, 70001)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    tts_paged_decode_attn(desc, 1, q, *big, None, None, _up(t), t.shape[1], _up(c.lens), 70001, nb, out, ws, size)
+    want, tol = reference(c, 0, qv)
+    close(out, want, tol)
