@@ -1891,6 +1891,209 @@ __global__ __launch_bounds__(64 * kPagedWaves, KV == kKvF32 && D == 128 ? 2 : 3)
   }
 }
 
+// ---- the paged path over 4-bit caches, up to 16 query heads per KV head ------
+// As paged_kernel, but a wave takes four blocks (64 tokens) at a time and the
+// next four are in flight while it works: a 4-bit block is small (2 x 1088
+// bytes for D = 128), so that what bounds a short workgroup is its chain of
+// round trips, not bytes. Rows of the score products are tokens in the order
+// (tile t, row m) -> block m / 4, slot 4 t + m % 4, so lane quarter lq ends up
+// with the scores of all 16 tokens of block lq, and the value products' step h
+// takes tokens 8 h .. + 8 of every block: a lane reads a dim's whole row of
+// codes (8 bytes) and a group's 16 scales at once.
+template <int D>
+struct Mx4Quad {
+  typedef typename Mx4Frags<D>::T T;
+  T k[4];
+  uint32_t ks[4];
+  uint2 v[D / 16];
+  uint4 vs[D / kMxGroup];
+};
+
+constexpr int kQuadTokens = 4 * kTok;
+
+template <int D>
+__global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_mx4_kernel(AttnParams p) {
+  constexpr int KV = kKvMx4;
+  using G = Geo<D, KV>;
+  __shared__ __attribute__((aligned(16))) float comb[kPagedWaves * G::comb_floats];
+  const unsigned total = static_cast<unsigned>(p.num_seqs) * p.hkv * p.paged_nsplit;
+  const unsigned at = blockIdx.x % kXcds * ((total + kXcds - 1) / kXcds) + blockIdx.x / kXcds;
+  if (at >= total) return;
+  const int unit = static_cast<int>(at);
+  const int b = unit % p.num_seqs, kvh = unit / p.num_seqs % p.hkv, split = unit / p.num_seqs / p.hkv;
+  const int wave = rfl(static_cast<int>(threadIdx.x) >> 6);
+  const int lane = threadIdx.x & 63, ln = lane & 15, lq = lane >> 4;
+  const size_t blk_stride = static_cast<size_t>(p.hkv) * G::blk_bytes;
+  const unsigned char* kbase = static_cast<const unsigned char*>(p.k_cache) + kvh * G::blk_bytes;
+  const unsigned char* vbase = static_cast<const unsigned char*>(p.v_cache) + kvh * G::blk_bytes;
+  // Split j covers blocks [j * per, (j + 1) * per) of the beam.
+  const int per = (p.paged_max_len + kTok * p.paged_nsplit - 1) / (kTok * p.paged_nsplit);
+  const int L = p.seq_lens[b];
+  QFrag<D, KV> q;
+  {
+    const unsigned char* row = static_cast<const unsigned char*>(p.q) +
+                               (static_cast<int64_t>(b) * p.hq + kvh * p.g + (ln < p.g ? ln : 0)) * D * 2;
+#pragma unroll
+    for (int i = 0; i < KOps<D, KV>::kk; ++i) q.q[i] = *reinterpret_cast<const uint4*>(row + dim_col<D, KV>(i, lq) * 16);
+  }
+  bool bad = false;
+  int nb = (L + kTok - 1) / kTok;
+  if (L < 0 || L > p.paged_max_len || nb > p.max_blocks) {
+    bad = true;
+    nb = 0;
+  }
+  const int first = split * per;
+  int n = nb - first;
+  n = n < 0 ? 0 : (n < per ? n : per);
+  const int32_t* table = p.block_tables + static_cast<int64_t>(b) * p.max_blocks + first;
+  const int nq = (n + 3) >> 2, mine = nq > wave ? (nq - wave + kPagedWaves - 1) / kPagedWaves : 0;
+
+  // This wave's quads are wave, wave + kPagedWaves, ...: lane l holds the id of
+  // block l % 4 of the wave's quad l / 4 of a window of 16.
+  auto load_ids = [&](int k0) {
+    const int j = 4 * (wave + kPagedWaves * (k0 + (lane >> 2))) + (lane & 3);
+    int id = j < n ? table[j] : -1;  // (-1: no block, or a bad one)
+    if (j < n && (id < 0 || id >= p.num_blocks)) {
+      bad = true;
+      id = -1;
+    }
+    return id;
+  };
+  auto load_quad = [&](Mx4Quad<D>& f, int ids, int k) {
+    typedef typename Mx4Quad<D>::T T;
+    const int kid = __shfl(ids, 4 * (k & 15) + (ln >> 2)), vid = __shfl(ids, 4 * (k & 15) + lq);
+    const unsigned char* kb = kbase + (kid > 0 ? kid : 0) * blk_stride;
+    const unsigned char* vb = vbase + (vid > 0 ? vid : 0) * blk_stride;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int slot = 4 * t + (ln & 3);
+      f.k[t] = *reinterpret_cast<const T*>(kb + slot * G::row_bytes + D / 8 * lq);
+      f.ks[t] = kb[G::code_bytes + (slot * D + D / 4 * lq) / kMxGroup];
+    }
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) f.v[dt] = *reinterpret_cast<const uint2*>(vb + (16 * dt + ln) * G::vrow_bytes);
+#pragma unroll
+    for (int i = 0; i < D / kMxGroup; ++i) f.vs[i] = *reinterpret_cast<const uint4*>(vb + G::code_bytes + kTok * i);
+  };
+
+  RowState<D> st;
+  float m_exact = 0.f;
+  for (int attempt = 0;; ++attempt) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st.m = m_exact;
+    st.l = 0.f;
+    st.seen = kNegInf;
+    if (mine > 0 && p.num_blocks > 0) {
+      Mx4Quad<D> next;
+      int ids = load_ids(0);
+      load_quad(next, ids, 0);
+      for (int k = 0; k < mine; ++k) {
+        const Mx4Quad<D> f = next;
+        // (A bad block's tokens take no part; its beam's row is NaN.)
+        const int left = L - kTok * (first + 4 * (wave + kPagedWaves * k) + lq);
+        const int valid = __shfl(ids, 4 * (k & 15) + lq) < 0 ? 0 : (left < 0 ? 0 : (left < kTok ? left : kTok));
+        if (k + 1 < mine) {
+          if (((k + 1) & 15) == 0) ids = load_ids(k + 1);
+          load_quad(next, ids, k + 1);
+        }
+        f32x4 acc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(&f.k[t]);
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j)
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, mx4x8_to_bf16x8(w[j], mx_scale<0>(f.ks[t]))),
+                __builtin_bit_cast(bf16x8, q.q[j]), acc[t], 0, 0, 0);
+        }
+        const bool partly = __builtin_amdgcn_ballot_w64(valid < kTok) != 0;
+        float x[kTok];
+#pragma unroll
+        for (int i = 0; i < kTok; ++i) {
+          x[i] = __builtin_fmaf(acc[i >> 2][i & 3], p.scale_log2, -st.m);
+          if (partly) x[i] = i < valid ? x[i] : kNegInf;
+          st.seen = fmaxf(st.seen, x[i]);
+          x[i] = __builtin_amdgcn_exp2f(x[i]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // The sum is that of the rounded probabilities, which the product uses.
+          uint32_t pb[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pb[i] = pack_bf16x2(x[8 * h + 2 * i], x[8 * h + 2 * i + 1]);
+            st.l += __builtin_bit_cast(float, pb[i] << 16) + __builtin_bit_cast(float, pb[i] & 0xFFFF0000u);
+          }
+          const bf16x8 pr = __builtin_bit_cast(bf16x8, uint4{pb[0], pb[1], pb[2], pb[3]});
+#pragma unroll
+          for (int dt = 0; dt < D / 16; ++dt) {
+            const uint4 s = f.vs[16 * dt / kMxGroup];
+            uint4 v = mx4x8_to_bf16x8(h ? f.v[dt].y : f.v[dt].x, h ? uint2{s.z, s.w} : uint2{s.x, s.y});
+            if (partly) {
+              uint32_t* a = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                a[e] &= (8 * h + 2 * e < valid ? 0xFFFFu : 0u) | (8 * h + 2 * e + 1 < valid ? 0xFFFF0000u : 0u);
+            }
+            st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pr, st.o[dt], 0, 0, 0);
+          }
+        }
+      }
+    }
+    if (attempt > 0) break;
+    const float mx = xlane_max16(st.seen);
+    const bool redo = mx > kRefWindow || (mx < -kRefWindow && mx != kNegInf);
+    m_exact = mx == kNegInf ? 0.f : mx;
+    if (__builtin_amdgcn_ballot_w64(redo) == 0) break;
+  }
+  // A bad block is seen by one wave: all of them learn of it here.
+  __shared__ int any_bad;
+  if (threadIdx.x == 0) any_bad = 0;
+  __syncthreads();
+  if (bad) any_bad = 1;
+  // The waves' states through LDS, sixteen threads to a row (as in
+  // attn_kernel).
+  auto slot = [&](int w) { return comb + w * G::comb_floats; };
+  st.l = xlane_sum16(st.l);
+  if (!(st.l > 0.f)) st.m = kNegInf;
+  if (mine > 0) {
+    float* c = slot(wave);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt)
+      *reinterpret_cast<f32x4*>(c + ln * G::comb_row + 16 * dt + 4 * lq) = st.o[dt];
+    if (lq == 0) {
+      c[kTok * G::comb_row + ln] = st.m;
+      c[kTok * G::comb_row + kTok + ln] = st.l;
+    }
+  }
+  __syncthreads();
+  bad = any_bad != 0;
+  constexpr int kEl = D / 16;
+  const int row = static_cast<int>(threadIdx.x) >> 4;
+  float mx, l;
+  f32x4 o[kEl / 4];
+  combine_row<D, KV, kPagedWaves>(slot, nq < kPagedWaves ? nq : kPagedWaves, row, ln, o, mx, l);
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float qnan = __builtin_nanf("");
+  if (p.paged_nsplit == 1) {
+    // Whole sequence in this unit: the normalised result.
+    if (row < p.g) {
+      const int64_t orow = (static_cast<int64_t>(b) * p.hq + kvh * p.g + row) * D;
+#pragma unroll
+      for (int e = 0; e < kEl / 4; ++e) {
+        f32x4 x = o[e] * inv;
+        if (bad) x = f32x4{qnan, qnan, qnan, qnan};
+        store_out4(p.out, p.out_bf16 != 0, orow + 16 * ((ln & 3) * (kEl / 4) + e) + 4 * (ln >> 2), x);
+      }
+    }
+  } else {
+    const int64_t prow = (static_cast<int64_t>(b) * p.paged_nsplit + split) * p.hq + kvh * p.g + row;
+    store_partial_row<D, KV>(p.part_o, p.part_ml, prow, o, bad ? qnan : mx, l, inv, ln, row < p.g);
+  }
+}
+
 // Exact merge of the partial softmax states of each (beam, query head), in
 // the order of the beam's slot list. With M = max_k m_k over the states
 // that saw tokens (l_k > 0), w_k = l_k 2^(m_k - M), and e_k the stored
@@ -2059,9 +2262,13 @@ static hipError_t launch_paged_t(AttnParams p, hipStream_t stream) {
     const int64_t n = left < most ? left : most;
     p.num_seqs = static_cast<int32_t>(n);
     const unsigned grid = static_cast<unsigned>(n * per);
-    if (small)
-      hipLaunchKernelGGL((paged_kernel<D, KV>), dim3((grid + kXcds - 1) / kXcds * kXcds), dim3(threads), 0, stream, p);
-    else
+    const dim3 dealt((grid + kXcds - 1) / kXcds * kXcds);
+    if constexpr (KV == kKvMx4) {
+      if (small) hipLaunchKernelGGL((paged_mx4_kernel<D>), dealt, dim3(threads), 0, stream, p);
+    } else {
+      if (small) hipLaunchKernelGGL((paged_kernel<D, KV>), dealt, dim3(threads), 0, stream, p);
+    }
+    if (!small)
       hipLaunchKernelGGL((attn_kernel<D, KV, false, true>), dim3(grid), dim3(threads), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
