@@ -307,29 +307,35 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
     // Values past the last token seen are unused slots; those that some rows
     // see and others do not may hold infinities or NaN, which a zero
     // probability would not keep out.
-    const bool edge = (tile + 1) * G::tokens > seen, hidden = (tile + 1) * G::tokens - 1 > all_see;
+    const bool hidden = (tile + 1) * G::tokens - 1 > all_see;
+    auto each = [&](auto hidden_c) {
 #pragma unroll
-    for (int i = 0; i < G::pieces; ++i) {
-      const int piece = tid + kPfThreads * i;
-      const int blk = piece / G::blk_pieces, at = piece % G::blk_pieces;
-      const int dim = at / G::vcols, vcol = blk * G::vcols + at % G::vcols;
-      uint4 k, v;
-      if constexpr (KV == kKvMx4) {
-        k = mx4x8_to_bf16x8(r.k[i], mx_scale<0>(r.ks[i]));
-        v = mx4x8_to_bf16x8(r.v[i], r.vs[i]);
-      } else {
-        k = staged<KV>(r.k[i]);
-        v = staged<KV>(r.v[i]);
+      for (int i = 0; i < G::pieces; ++i) {
+        const int piece = tid + kPfThreads * i;
+        const int blk = piece / G::blk_pieces, at = piece % G::blk_pieces;
+        const int dim = at / G::vcols, vcol = blk * G::vcols + at % G::vcols;
+        uint4 k, v;
+        if constexpr (KV == kKvMx4) {
+          k = mx4x8_to_bf16x8(r.k[i], mx_scale<0>(r.ks[i]));
+          v = mx4x8_to_bf16x8(r.v[i], r.vs[i]);
+        } else {
+          k = staged<KV>(r.k[i]);
+          v = staged<KV>(r.v[i]);
+        }
+        if constexpr (decltype(hidden_c)::value) {
+          const int tok = tile * G::tokens + vcol * G::per;  // V piece's first token
+          keep_first<G::f32>(v, seen - tok);
+          const int at_bad = drop_nonfinite<G::f32>(v);
+          if (at_bad < 8) atomicMin(&bad_dim[dim], tok + at_bad);
+        }
+        *reinterpret_cast<uint4*>(buf + k_place<D, KV>(blk * kTok + at / G::kcols, at % G::kcols)) = k;
+        *reinterpret_cast<uint4*>(buf + G::tensor_bytes + v_place<D, KV>(dim, vcol)) = v;
       }
-      const int tok = tile * G::tokens + vcol * G::per;  // V piece's first token
-      if (edge) keep_first<G::f32>(v, seen - tok);
-      if (hidden) {
-        const int at_bad = drop_nonfinite<G::f32>(v);
-        if (at_bad < 8) atomicMin(&bad_dim[dim], tok + at_bad);
-      }
-      *reinterpret_cast<uint4*>(buf + k_place<D, KV>(blk * kTok + at / G::kcols, at % G::kcols)) = k;
-      *reinterpret_cast<uint4*>(buf + G::tensor_bytes + v_place<D, KV>(dim, vcol)) = v;
-    }
+    };
+    if (hidden)
+      each(std::true_type{});
+    else
+      each(std::false_type{});
   };
 
   f32x16 o[D / 32];
@@ -377,22 +383,29 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
             }
           }
         }
-        // Scores in log2 units; hidden tokens -inf.
-        const bool partly = t0 + G::tokens - 1 > first_lim;
-        const int left = lim - t0 - half * (G::f32 ? 4 : 8);
+        // fp8: the blocks' K scales.
+        if constexpr (KV == kKvFp8) {
+#pragma unroll
+          for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] *= scales.k[(32 * t + reg_token<G::f32>(i)) / kTok];
+        }
+        // Hidden tokens: -inf. (The empty asm keeps this a branch: as selects
+        // it would cost every tile two instructions per score.)
+        if (t0 + G::tokens - 1 > first_lim) {
+          asm volatile("");
+          const int left = lim - t0 - half * (G::f32 ? 4 : 8);
+#pragma unroll
+          for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = 32 * t + reg_token<G::f32>(i) <= left ? s[t][i] : kNegInf;
+        }
         float mx = kNegInf;
 #pragma unroll
         for (int t = 0; t < G::tokens / 32; ++t)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int tok = 32 * t + reg_token<G::f32>(i);
-            float sc = p.scale_log2;
-            if constexpr (KV == kKvFp8) sc *= scales.k[tok / kTok];
-            s[t][i] *= sc;
-            if (partly) s[t][i] = tok <= left ? s[t][i] : kNegInf;
-            mx = fmaxf(mx, s[t][i]);
-          }
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;  // (the scale is positive)
         if (__builtin_amdgcn_ballot_w64(mx > ref + kRefSlack || (ref == kNegInf && mx > kNegInf)) != 0) {
           const float now = mx > ref ? mx : ref;
           const float f = ref == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ref - now);
@@ -406,7 +419,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
         for (int t = 0; t < G::tokens / 32; ++t)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - sub);
+            s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], p.scale_log2, -sub));
             sum += s[t][i];
           }
 #pragma unroll
