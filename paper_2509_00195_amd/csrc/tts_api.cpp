@@ -696,12 +696,23 @@ tts_status tts_prefix_decode_merge(const tts_attn_desc* d, const tts_prefix_meta
 
 // ---- ragged prefill ------------------------------------------------------------
 
+// Rows of a workgroup: the wide kind where a sequence has as many on average.
+static int32_t prefill_rows_per(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens) {
+  const int64_t g = d->num_q_heads / d->num_kv_heads;
+#ifdef TTS_NO_WIDE
+  return tts::kPrefillRows;
+#endif
+  const bool wide = d->kv_dtype != TTS_F32 && num_tokens * g >= static_cast<int64_t>(num_seqs) * tts::kPrefillWideRows;
+  return wide ? tts::kPrefillWideRows : tts::kPrefillRows;
+}
+
 // Splits of every tile of rows over its tokens: as many as fill the card's
-// 256 compute units with two workgroups each.
+// 256 compute units with eight waves each.
 static int32_t prefill_nsplit(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens, int32_t max_seq_len) {
   const int64_t g = d->num_q_heads / d->num_kv_heads;
-  const int64_t units = tts::prefill_items(num_seqs, num_tokens, g) * d->num_kv_heads;
-  const int64_t fill = units > 0 ? 512 / units : 1;
+  const int32_t rows = prefill_rows_per(d, num_seqs, num_tokens);
+  const int64_t units = tts::prefill_items(num_seqs, num_tokens, g, rows) * d->num_kv_heads;
+  const int64_t fill = units > 0 ? 65536 / rows / units : 1;
   const int64_t fit = max_seq_len / tts::kPrefillSplitTokens;
   const int64_t n = std::min({fill, fit, static_cast<int64_t>(tts::kPrefillMaxSplit)});
   return n < 1 ? 1 : static_cast<int32_t>(n);
@@ -763,6 +774,7 @@ tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int3
   p.hkv = d->num_kv_heads;
   p.g = d->num_q_heads / d->num_kv_heads;
   p.nsplit = prefill_nsplit(d, num_seqs, num_tokens, max_seq_len);
+  p.tile_rows = prefill_rows_per(d, num_seqs, num_tokens);
   p.out_bf16 = d->out_dtype == TTS_BF16;
   p.scale_log2 = scale_log2(d);
   if (p.nsplit > 1) {

@@ -35,13 +35,14 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kPfWaves = kPrefillRows / 32;
-constexpr int kPfThreads = 64 * kPfWaves;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kRefSlack = 16.f;  // log2 units
 
-template <int D, int KV>
+template <int D, int KV, int kThreads>
 struct PfGeo {
+  // A piece as it comes from the cache.
+  typedef typename std::conditional<
+      KV == kKvMx4, uint32_t, typename std::conditional<KV == kKvFp8, uint2, uint4>::type>::type Raw;
   static constexpr bool f32 = KV == kKvF32;
   static constexpr int eb = f32 ? 4 : 2;                 // bytes of a staged element
   static constexpr int tokens = f32 ? 32 : 64;           // of a tile
@@ -50,9 +51,8 @@ struct PfGeo {
   static constexpr int kcols = D / per;                  // pieces of a K row
   static constexpr int vcols = kTok / per;               // pieces of a V row
   static constexpr int blk_pieces = kTok * kcols;        // of K, and of V, in a block
-  static constexpr int pieces = blocks * blk_pieces / kPfThreads;  // per thread and tensor
+  static constexpr int pieces = blocks * blk_pieces / kThreads;  // per thread and tensor
   static constexpr int tensor_bytes = tokens * D * eb;
-  static constexpr int buf_bytes = 2 * tensor_bytes;
   static constexpr int ksteps = kcols / 2;               // fragments of 32 tokens of K
   static constexpr int vsteps = tokens / (2 * per);      // fragments of 32 dims of V
 };
@@ -72,29 +72,16 @@ __host__ __device__ constexpr int reg_token(int r) {
 
 // Byte of the LDS place of K piece (token of the tile, column) and V piece
 // (dim, column of the tile's tokens).
-template <int D, int KV>
+template <typename G>
 __device__ __forceinline__ int k_place(int tok, int col) {
-  using G = PfGeo<D, KV>;
   const int m = row_of_token<G::f32>(tok & 31);
   return ((tok >> 5) * G::ksteps + (col >> 1)) * 1024 + (col & 1) * 512 + ((m ^ (col & 15)) << 4);
 }
-template <int D, int KV>
+template <typename G>
 __device__ __forceinline__ int v_place(int dim, int col) {
-  using G = PfGeo<D, KV>;
   return ((dim >> 5) * G::vsteps + (col >> 1)) * 1024 + (col & 1) * 512 +
          (((dim & 31) ^ ((col & (G::vcols - 1)) * (16 / G::vcols))) << 4);
 }
-
-// A thread's pieces of a tile on their way from the cache.
-template <int D, int KV>
-struct PfRegs {
-  typedef typename std::conditional<
-      KV == kKvMx4, uint32_t, typename std::conditional<KV == kKvFp8, uint2, uint4>::type>::type T;
-  T k[PfGeo<D, KV>::pieces], v[PfGeo<D, KV>::pieces];
-  // 4-bit caches: scale bytes.
-  uint32_t ks[KV == kKvMx4 ? PfGeo<D, KV>::pieces : 1];
-  uint2 vs[KV == kKvMx4 ? PfGeo<D, KV>::pieces : 1];
-};
 
 template <int KV, typename T>
 __device__ __forceinline__ uint4 staged(T raw) {
@@ -142,6 +129,22 @@ __device__ __forceinline__ int drop_nonfinite(uint4& x) {
   return first;
 }
 
+// The larger of a lane's value and that of the same lane of the other half.
+__device__ __forceinline__ float halves_max(float x) {
+  // (In assembly: of the exchange builtin's two results this compiler keeps
+  // one. The wait states are those it puts before the instruction.)
+  float a = x, b = x;
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+  return fmaxf(a, b);
+}
+
+// A value at a uniform address that the kernel does not write.
+template <typename T>
+__device__ __forceinline__ T scalar(const T* at) {
+  typedef const T __attribute__((address_space(4))) * P;
+  return *(P)(reinterpret_cast<uintptr_t>(at));
+}
+
 struct PfItem {
   int seq, n, len;  // its new tokens and its length
   int row0;         // first row (token x g + head of the group) of the tile
@@ -150,9 +153,10 @@ struct PfItem {
 
 // The sequence of an item (as in the rotating append: every wave alone, in
 // bounds whatever the offsets hold).
+template <int kRows>
 __device__ __forceinline__ PfItem prefill_item(const PrefillParams& p, int64_t item) {
   const int lane = threadIdx.x & 63;
-  auto first = [&](int64_t b) { return static_cast<int64_t>(p.tok_offsets[b]) * p.g / kPrefillRows + b; };
+  auto first = [&](int64_t b) { return static_cast<int64_t>(p.tok_offsets[b]) * p.g / kRows + b; };
   int64_t lo = 0, hi = p.num_seqs;
   while (hi - lo > 1) {
     const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
@@ -166,29 +170,54 @@ __device__ __forceinline__ PfItem prefill_item(const PrefillParams& p, int64_t i
   it.tok0 = t0;
   it.n = t1 - t0;
   it.len = p.seq_lens[it.seq];
-  const int64_t row0 = (item - first(it.seq)) * kPrefillRows;
+  const int64_t row0 = (item - first(it.seq)) * kRows;
   if (t0 < 0 || t1 < t0 || t1 > p.num_tokens || row0 < 0 || row0 >= static_cast<int64_t>(it.n) * p.g) it.n = 0;
   it.row0 = static_cast<int>(row0);
   return it;
 }
 
-template <int D, int KV>
-__global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p) {
-  using G = PfGeo<D, KV>;
+// Schedule of kFrags fragments, each one LDS read and kProducts products: the
+// reads go kAhead ahead (left to itself the compiler issues one or two, and
+// every product waits for its operand: the LDS takes longer than a product).
+#ifndef TTS_AHEAD
+#define TTS_AHEAD 6
+#endif
+template <int kFrags, int kProducts>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int kAhead = TTS_AHEAD;
+  constexpr int kMfma = 0x008, kRead = 0x100;
+  __builtin_amdgcn_sched_group_barrier(kRead, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < kFrags - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, kProducts, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kMfma, kProducts * kAhead, 0);
+}
+
+// kWaves 4: the waves take a tile's steps together. kWaves 8: two to a SIMD,
+// in turns (see the header).
+template <int D, int KV, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 1 : 2) void prefill_kernel(PrefillParams p) {
+  constexpr bool kTurns = kWaves == 8;
+  constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
+  using G = PfGeo<D, KV, kThreads>;
   using C = KvGeo<D, KV>;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * G::buf_bytes];
+  // K and V buffers of even and odd tiles.
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * G::tensor_bytes];
   __shared__ int bad_dim[D];  // first token whose value in this dim is not finite (tiles with hidden tokens)
+  __shared__ int bad_tok;     // first token of a block that is not in the pool
 
   // Units in the order (tile of rows, split, KV head), the last tiles of a
   // call (which see the most tokens) first: KV heads side by side, so that
   // the XCDs (workgroups are dealt to them in turn) read few heads each.
   const int64_t unit = p.units - 1 - (p.unit0 + blockIdx.x);
   const int kvh = static_cast<int>(unit % p.hkv), split = static_cast<int>(unit / p.hkv % p.nsplit);
-  const PfItem it = prefill_item(p, unit / p.hkv / p.nsplit);
+  const PfItem it = prefill_item<kRows>(p, unit / p.hkv / p.nsplit);
   if (it.n <= 0) return;
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int nrows = it.n * p.g - it.row0 < kPrefillRows ? it.n * p.g - it.row0 : kPrefillRows;
+  const int nrows = it.n * p.g - it.row0 < kRows ? it.n * p.g - it.row0 : kRows;
   const int row = it.row0 + 32 * wave + ln;  // this lane's row of the sequence
   const bool active = 32 * wave + ln < nrows;
   const int64_t orow = (it.tok0 + row / p.g) * p.hq + kvh * p.g + row % p.g;
@@ -203,11 +232,12 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
   const int wave_lim = 32 * wave < nrows && before >= 0 ? before + last_row / p.g : -1;  // and its last
   const int seen = before >= 0 ? before + (it.row0 + nrows - 1) / p.g + 1 : 0;  // tokens the tile of rows sees
   const int all_see = before >= 0 ? before + it.row0 / p.g : -1;                // the last token that every row sees
-  const int ntiles = (seen + G::tokens - 1) / G::tokens;
+  const int ntiles = p.num_blocks > 0 ? (seen + G::tokens - 1) / G::tokens : 0;
   const int tile0 = static_cast<int>(static_cast<int64_t>(ntiles) * split / p.nsplit);
   const int tile1 = static_cast<int>(static_cast<int64_t>(ntiles) * (split + 1) / p.nsplit);
 
-  for (int i = tid; i < D; i += kPfThreads) bad_dim[i] = 0x7FFFFFFF;
+  for (int i = tid; i < D; i += kThreads) bad_dim[i] = 0x7FFFFFFF;
+  if (tid == 0) bad_tok = p.num_blocks > 0 ? 0x7FFFFFFF : 0;
 
   typedef typename std::conditional<G::f32, f32x4, uint4>::type Frag;
   // Query rows as the B operand.
@@ -224,247 +254,355 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
   const unsigned char* vbase = static_cast<const unsigned char*>(p.v_cache) + static_cast<size_t>(kvh) * C::blk_bytes;
   const int32_t* table = p.block_tables + static_cast<int64_t>(it.seq) * p.max_blocks;
   const int nblk = (seen + kTok - 1) / kTok;
-  int first_bad = 0x7FFFFFFF;  // first token of a block that is not in the pool
-
-  // Block ids of a tile (-1: none to read), uniform over the workgroup.
+  // Ids of the blocks that this wave's pieces of a tile come from, read through
+  // the scalar cache (a vector load's wait would be one for the pieces in
+  // flight too). Behind the last block: that one again. A block that is not in
+  // the pool gives way to block 0: rows that see it are NaN, and to the others
+  // its tokens are hidden ones.
+  // (A vector value rather than an array, so that it stays in registers.)
   struct Ids {
-    int id[G::blocks];
+    int id __attribute__((ext_vector_type(G::pieces)));
   };
+  auto block_in_tile = [&](int i) { return (64 * wave + kThreads * i) / G::blk_pieces; };
   auto load_ids = [&](int tile) {
     Ids x;
 #pragma unroll
-    for (int i = 0; i < G::blocks; ++i) {
-      const int lb = tile * G::blocks + i;
-      x.id[i] = tile < tile1 && lb < nblk ? table[lb] : -1;
+    for (int i = 0; i < G::pieces; ++i) {
+      const int lb = tile * G::blocks + block_in_tile(i);
+      x.id[i] = scalar(table + (lb < nblk ? lb : nblk - 1));
     }
     return x;
   };
   auto check_ids = [&](Ids& x, int tile) {
 #pragma unroll
-    for (int i = 0; i < G::blocks; ++i) {
-      const int lb = tile * G::blocks + i;
-      if (tile < tile1 && lb < nblk && (x.id[i] < 0 || x.id[i] >= p.num_blocks)) {
-        first_bad = first_bad < lb * kTok ? first_bad : lb * kTok;
-        x.id[i] = -1;
+    for (int i = 0; i < G::pieces; ++i)
+      if (x.id[i] < 0 || x.id[i] >= p.num_blocks) {
+        // (A tile behind the last repeats a block that was checked.)
+        atomicMin(&bad_tok, (tile * G::blocks + block_in_tile(i)) * kTok);
+        x.id[i] = 0;
+      }
+  };
+  // fp8: the K scales times the softmax scale, and the V scales, of all of a
+  // tile's blocks. A V scale that is not finite makes every value of its block
+  // infinite or NaN: rows that see the block are NaN, and the others must not
+  // meet it.
+  struct Scales {
+    float k __attribute__((ext_vector_type(G::blocks)));
+    float v __attribute__((ext_vector_type(G::blocks)));
+  };
+  struct AllIds {
+    int id __attribute__((ext_vector_type(G::blocks)));
+  };
+  auto load_all_ids = [&](int tile) {
+    AllIds x;
+    if constexpr (KV == kKvFp8) {
+#pragma unroll
+      for (int i = 0; i < G::blocks; ++i) {
+        const int lb = tile * G::blocks + i;
+        x.id[i] = scalar(table + (lb < nblk ? lb : nblk - 1));
       }
     }
+    return x;
   };
-  struct Scales {  // fp8
-    float k[G::blocks], v[G::blocks];
-  };
-  auto load_scales = [&](const Ids& x) {
+  auto load_scales = [&](const AllIds& x) {
     Scales s;
     if constexpr (KV == kKvFp8) {
 #pragma unroll
       for (int i = 0; i < G::blocks; ++i) {
-        s.k[i] = x.id[i] >= 0 ? p.k_scale[x.id[i]] : 0.f;
-        s.v[i] = x.id[i] >= 0 ? p.v_scale[x.id[i]] : 0.f;
+        const int id = x.id[i] < 0 || x.id[i] >= p.num_blocks ? 0 : x.id[i];
+        s.k[i] = scalar(p.k_scale + id);
+        s.v[i] = scalar(p.v_scale + id);
       }
     }
     return s;
   };
-  // A V scale that is not finite makes every value of its block infinite or
-  // NaN: the rows that see the block are NaN, and the others never meet it.
   auto check_scales = [&](Scales& s, int tile) {
     if constexpr (KV == kKvFp8) {
 #pragma unroll
-      for (int i = 0; i < G::blocks; ++i)
+      for (int i = 0; i < G::blocks; ++i) {
+        s.k[i] *= p.scale_log2;
         if (!(__builtin_fabsf(s.v[i]) < __builtin_inff())) {
-          const int tok = tile * G::tokens + i * kTok;
-          first_bad = first_bad < tok ? first_bad : tok;
+          atomicMin(&bad_tok, tile * G::tokens + i * kTok);
           s.v[i] = 0.f;
         }
+      }
     }
   };
-  auto load_tile = [&](PfRegs<D, KV>& r, const Ids& x) {
-    typedef typename PfRegs<D, KV>::T T;
+
+  // A thread's pieces of a tile on their way from the cache.
+  typedef typename G::Raw T;
+  T kr[G::pieces], vr[G::pieces];
+  uint32_t ks[KV == kKvMx4 ? G::pieces : 1];  // 4-bit caches: scale bytes
+  uint2 vs[KV == kKvMx4 ? G::pieces : 1];
+  auto load_k = [&](const Ids& x) {
 #pragma unroll
     for (int i = 0; i < G::pieces; ++i) {
-      const int piece = tid + kPfThreads * i;
-      const int blk = __builtin_amdgcn_readfirstlane(piece / G::blk_pieces), at = piece % G::blk_pieces;
-      int id = -1;
-#pragma unroll
-      for (int k = 0; k < G::blocks; ++k) id = blk == k ? x.id[k] : id;
-      r.k[i] = T{};
-      r.v[i] = T{};
-      if constexpr (KV == kKvMx4) {
-        r.ks[i] = 0u;
-        r.vs[i] = uint2{0u, 0u};
-      }
-      if (id < 0) continue;  // uniform over the wave
-      const unsigned char* kb = kbase + id * blk_stride;
-      const unsigned char* vb = vbase + id * blk_stride;
-      r.k[i] = *reinterpret_cast<const T*>(kb + at * static_cast<int>(sizeof(T)));
-      r.v[i] = *reinterpret_cast<const T*>(vb + at * static_cast<int>(sizeof(T)));
-      if constexpr (KV == kKvMx4) {
-        r.ks[i] = kb[C::code_bytes + at * 8 / kMxGroup];
-        r.vs[i] = *reinterpret_cast<const uint2*>(vb + C::code_bytes + at / G::vcols / kMxGroup * kTok + 8 * (at % G::vcols));
-      }
+      const unsigned at = (tid + kThreads * i) % G::blk_pieces;
+      const unsigned char* kb = kbase + static_cast<unsigned>(x.id[i]) * blk_stride;
+      kr[i] = *reinterpret_cast<const T*>(kb + at * static_cast<unsigned>(sizeof(T)));
+      if constexpr (KV == kKvMx4) ks[i] = kb[C::code_bytes + at * 8 / kMxGroup];
     }
   };
-  auto store_tile = [&](const PfRegs<D, KV>& r, int tile) {
-    unsigned char* buf = lds + (tile & 1) * G::buf_bytes;
-    // Values past the last token seen are unused slots; those that some rows
-    // see and others do not may hold infinities or NaN, which a zero
-    // probability would not keep out.
-    const bool hidden = (tile + 1) * G::tokens - 1 > all_see;
+  auto load_v = [&](const Ids& x) {
+#pragma unroll
+    for (int i = 0; i < G::pieces; ++i) {
+      const unsigned at = (tid + kThreads * i) % G::blk_pieces;
+      const unsigned char* vb = vbase + static_cast<unsigned>(x.id[i]) * blk_stride;
+      vr[i] = *reinterpret_cast<const T*>(vb + at * static_cast<unsigned>(sizeof(T)));
+      if constexpr (KV == kKvMx4)
+        vs[i] = *reinterpret_cast<const uint2*>(vb + C::code_bytes + at / G::vcols / kMxGroup * kTok + 8 * (at % G::vcols));
+    }
+  };
+  auto kbuf = [&](int tile) { return lds + (tile & 1) * G::tensor_bytes; };
+  auto vbuf = [&](int tile) { return lds + (2 + (tile & 1)) * G::tensor_bytes; };
+  auto store_k = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < G::pieces; ++i) {
+      const int piece = tid + kThreads * i, blk = piece / G::blk_pieces, at = piece % G::blk_pieces;
+      uint4 x;
+      if constexpr (KV == kKvMx4)
+        x = mx4x8_to_bf16x8(kr[i], mx_scale<0>(ks[i]));
+      else
+        x = staged<KV>(kr[i]);
+      *reinterpret_cast<uint4*>(kbuf(tile) + k_place<G>(blk * kTok + at / G::kcols, at % G::kcols)) = x;
+    }
+  };
+  // Values past the last token seen are unused slots; those that some rows
+  // see and others do not may be infinities or NaN, which a zero probability
+  // would not keep out.
+  auto store_v = [&](int tile) {
     auto each = [&](auto hidden_c) {
 #pragma unroll
       for (int i = 0; i < G::pieces; ++i) {
-        const int piece = tid + kPfThreads * i;
-        const int blk = piece / G::blk_pieces, at = piece % G::blk_pieces;
+        const int piece = tid + kThreads * i, blk = piece / G::blk_pieces, at = piece % G::blk_pieces;
         const int dim = at / G::vcols, vcol = blk * G::vcols + at % G::vcols;
-        uint4 k, v;
-        if constexpr (KV == kKvMx4) {
-          k = mx4x8_to_bf16x8(r.k[i], mx_scale<0>(r.ks[i]));
-          v = mx4x8_to_bf16x8(r.v[i], r.vs[i]);
-        } else {
-          k = staged<KV>(r.k[i]);
-          v = staged<KV>(r.v[i]);
-        }
+        uint4 x;
+        if constexpr (KV == kKvMx4)
+          x = mx4x8_to_bf16x8(vr[i], vs[i]);
+        else
+          x = staged<KV>(vr[i]);
         if constexpr (decltype(hidden_c)::value) {
-          const int tok = tile * G::tokens + vcol * G::per;  // V piece's first token
-          keep_first<G::f32>(v, seen - tok);
-          const int at_bad = drop_nonfinite<G::f32>(v);
+          const int tok = tile * G::tokens + vcol * G::per;  // the piece's first token
+          keep_first<G::f32>(x, seen - tok);
+          const int at_bad = drop_nonfinite<G::f32>(x);
           if (at_bad < 8) atomicMin(&bad_dim[dim], tok + at_bad);
         }
-        *reinterpret_cast<uint4*>(buf + k_place<D, KV>(blk * kTok + at / G::kcols, at % G::kcols)) = k;
-        *reinterpret_cast<uint4*>(buf + G::tensor_bytes + v_place<D, KV>(dim, vcol)) = v;
+        *reinterpret_cast<uint4*>(vbuf(tile) + v_place<G>(dim, vcol)) = x;
       }
     };
-    if (hidden)
+    if ((tile + 1) * G::tokens - 1 > all_see)
       each(std::true_type{});
     else
       each(std::false_type{});
   };
 
-  f32x16 o[D / 32];
+  f32x16 o[D / 32], s[G::tokens / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float ref = kNegInf, sum = 0.f;  // reference of the row (both halves alike), this lane's part of the sum
+  uint4 pb[G::f32 ? 1 : G::vsteps];  // a tile's probabilities, the B operand of its value products
+
+  auto scores = [&](int tile) {
+#pragma unroll
+    for (int t = 0; t < G::tokens / 32; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < G::ksteps; ++j) {
+        const Frag k = *reinterpret_cast<const Frag*>(kbuf(tile) + (t * G::ksteps + j) * 1024 + half * 512 +
+                                                      ((ln ^ ((2 * j + half) & 15)) << 4));
+        if constexpr (G::f32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[j][e], s[t], 0, 0, 0);
+        } else {
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
+                                                         __builtin_bit_cast(bf16x8, q[j]), s[t], 0, 0, 0);
+        }
+      }
+    }
+    reads_ahead<G::tokens / 32 * G::ksteps, G::f32 ? 4 : 1>();
+  };
+  auto softmax = [&](int tile, Scales& sc) {
+    const int t0 = tile * G::tokens;
+    if constexpr (KV == kKvFp8) {
+      // What follows takes positive scales; others are multiplied in here.
+      bool positive = true;
+#pragma unroll
+      for (int b = 0; b < G::blocks; ++b) positive = positive && sc.k[b] > 0.f;
+      if (!positive) {
+        asm volatile("");
+#pragma unroll
+        for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] *= sc.k[(32 * t + reg_token<G::f32>(i)) / kTok];
+#pragma unroll
+        for (int b = 0; b < G::blocks; ++b) sc.k[b] = 1.f;
+      }
+    }
+    // Hidden tokens: -inf. (The empty asm keeps this a branch: as selects it
+    // would cost every tile two instructions per score.)
+    if (t0 + G::tokens - 1 > first_lim) {
+      asm volatile("");
+      const int left = lim - t0 - half * (G::f32 ? 4 : 8);
+#pragma unroll
+      for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = 32 * t + reg_token<G::f32>(i) <= left ? s[t][i] : kNegInf;
+    }
+    float mx = kNegInf;
+    if constexpr (KV == kKvFp8) {
+#pragma unroll
+      for (int b = 0; b < G::blocks; ++b) {
+        float m = s[b / 2][8 * (b & 1)];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = fmaxf(m, s[b / 2][8 * (b & 1) + i]);
+        mx = fmaxf(mx, m * sc.k[b]);
+      }
+      mx = halves_max(mx);
+    } else {
+#pragma unroll
+      for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
+      mx = halves_max(mx) * p.scale_log2;  // (the scale is positive)
+    }
+    if (__builtin_amdgcn_ballot_w64(mx > ref + kRefSlack || (ref == kNegInf && mx > kNegInf)) != 0) {
+      const float now = mx > ref ? mx : ref;
+      const float f = ref == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ref - now);
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] *= f;
+      ref = now;
+    }
+    const float sub = ref == kNegInf ? 0.f : ref;
+#pragma unroll
+    for (int t = 0; t < G::tokens / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float f = KV == kKvFp8 ? sc.k[(32 * t + reg_token<G::f32>(i)) / kTok] : p.scale_log2;
+        s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], f, -sub));
+        sum += s[t][i];
+      }
+    if constexpr (!G::f32) {
+#pragma unroll
+      for (int j = 0; j < G::vsteps; ++j) {
+        float pv[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          pv[e] = s[j >> 1][8 * (j & 1) + e];
+          if constexpr (KV == kKvFp8) pv[e] *= sc.v[j];
+        }
+        pb[j] = uint4{pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
+                      pack_bf16x2(pv[6], pv[7])};
+      }
+    }
+  };
+  auto values = [&](int tile) {
+#pragma unroll
+    for (int j = 0; j < G::vsteps; ++j)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+        const Frag v = *reinterpret_cast<const Frag*>(vbuf(tile) + (d * G::vsteps + j) * 1024 + half * 512 +
+                                                      ((ln ^ (((2 * j + half) & (G::vcols - 1)) * (16 / G::vcols))) << 4));
+        if constexpr (G::f32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], s[0][4 * j + e], o[d], 0, 0, 0);
+        } else {
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pb[j]),
+                                                         o[d], 0, 0, 0);
+        }
+      }
+    reads_ahead<G::vsteps * D / 32, G::f32 ? 4 : 1>();
+  };
 
   if (tile0 < tile1) {
-    PfRegs<D, KV> regs;
-    Ids ids = load_ids(tile0);
+    __syncthreads();  // bad_dim and bad_tok are set
+    AllIds all = load_all_ids(tile0);
+    Ids ids = load_ids(tile0), next = load_ids(tile0 + 1);
     check_ids(ids, tile0);
-    load_tile(regs, ids);
-    Scales scales = load_scales(ids), next_scales;
-    ids = load_ids(tile0 + 1);
-    __syncthreads();  // bad_dim is set
-    store_tile(regs, tile0);
-    check_ids(ids, tile0 + 1);
-    load_tile(regs, ids);
-    next_scales = load_scales(ids);
-    ids = load_ids(tile0 + 2);
-    __syncthreads();
-    for (int tile = tile0; tile < tile1; ++tile) {
-      check_scales(scales, tile);
-      const unsigned char* kbuf = lds + (tile & 1) * G::buf_bytes;
-      const unsigned char* vbuf = kbuf + G::tensor_bytes;
-      const int t0 = tile * G::tokens;
-      if (t0 <= wave_lim) {
-        f32x16 s[G::tokens / 32];
-#pragma unroll
-        for (int t = 0; t < G::tokens / 32; ++t) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
-#pragma unroll
-          for (int j = 0; j < G::ksteps; ++j) {
-            const Frag k = *reinterpret_cast<const Frag*>(kbuf + (t * G::ksteps + j) * 1024 + half * 512 +
-                                                          ((ln ^ ((2 * j + half) & 15)) << 4));
-            if constexpr (G::f32) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[j][e], s[t], 0, 0, 0);
-            } else {
-              s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
-                                                             __builtin_bit_cast(bf16x8, q[j]), s[t], 0, 0, 0);
-            }
-          }
-        }
-        // fp8: the blocks' K scales.
-        if constexpr (KV == kKvFp8) {
-#pragma unroll
-          for (int t = 0; t < G::tokens / 32; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] *= scales.k[(32 * t + reg_token<G::f32>(i)) / kTok];
-        }
-        // Hidden tokens: -inf. (The empty asm keeps this a branch: as selects
-        // it would cost every tile two instructions per score.)
-        if (t0 + G::tokens - 1 > first_lim) {
-          asm volatile("");
-          const int left = lim - t0 - half * (G::f32 ? 4 : 8);
-#pragma unroll
-          for (int t = 0; t < G::tokens / 32; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = 32 * t + reg_token<G::f32>(i) <= left ? s[t][i] : kNegInf;
-        }
-        float mx = kNegInf;
-#pragma unroll
-        for (int t = 0; t < G::tokens / 32; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;  // (the scale is positive)
-        if (__builtin_amdgcn_ballot_w64(mx > ref + kRefSlack || (ref == kNegInf && mx > kNegInf)) != 0) {
-          const float now = mx > ref ? mx : ref;
-          const float f = ref == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ref - now);
-          sum *= f;
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d) o[d] *= f;
-          ref = now;
-        }
-        const float sub = ref == kNegInf ? 0.f : ref;
-#pragma unroll
-        for (int t = 0; t < G::tokens / 32; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], p.scale_log2, -sub));
-            sum += s[t][i];
-          }
-#pragma unroll
-        for (int j = 0; j < G::vsteps; ++j) {
-          if constexpr (G::f32) {
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
-              const Frag v = *reinterpret_cast<const Frag*>(
-                  vbuf + (d * G::vsteps + j) * 1024 + half * 512 +
-                  ((ln ^ (((2 * j + half) & (G::vcols - 1)) * (16 / G::vcols))) << 4));
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], s[0][4 * j + e], o[d], 0, 0, 0);
-            }
-          } else {
-            float pv[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              pv[e] = s[j >> 1][8 * (j & 1) + e];
-              if constexpr (KV == kKvFp8) pv[e] *= scales.v[j];
-            }
-            const uint4 pb = {pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
-                              pack_bf16x2(pv[6], pv[7])};
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
-              const Frag v = *reinterpret_cast<const Frag*>(vbuf + (d * G::vsteps + j) * 1024 + half * 512 +
-                                                            ((ln ^ (half * 8)) << 4));
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v),
-                                                             __builtin_bit_cast(bf16x8, pb), o[d], 0, 0, 0);
-            }
-          }
-        }
-      }
-      if (tile + 1 < tile1) {
-        store_tile(regs, tile + 1);
-        scales = next_scales;
-        check_ids(ids, tile + 2);
-        load_tile(regs, ids);
-        next_scales = load_scales(ids);
-        ids = load_ids(tile + 3);
-      }
+    load_k(ids);
+    load_v(ids);
+    Scales sc = load_scales(all), sc_next;
+    all = load_all_ids(tile0 + 1);
+    store_k(tile0);
+    if constexpr (kTurns) {
+      // K of the next tile is on its way with V of this one.
+      Ids ahead = load_ids(tile0 + 2);
+      check_ids(next, tile0 + 1);
+      load_k(next);
       __syncthreads();
+      // stage: K of tile + 1 and V of tile into LDS, then K of tile + 2 and V
+      // of tile + 1 on their way.
+      auto stage = [&](int tile) {
+        if (tile >= tile1) return;
+        if (tile + 1 < tile1) store_k(tile + 1);
+        store_v(tile);
+        if (tile + 1 >= tile1) return;
+        load_v(next);
+        next = ahead;
+        check_ids(next, tile + 2);
+        load_k(next);
+        ahead = load_ids(tile + 3);
+      };
+      auto turn = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      const int group = wave >> 2;
+      if (group != 0) {
+        stage(tile0);
+        turn();
+      }
+      for (int tile = tile0; tile < tile1; ++tile) {
+        const bool sees = tile * G::tokens <= wave_lim;
+        if (sees) scores(tile);
+        if (tile > tile0 && (tile - 1) * G::tokens <= wave_lim) values(tile - 1);
+        turn();
+        sc_next = load_scales(all);
+        all = load_all_ids(tile + 2);
+        check_scales(sc, tile);
+        if (sees) softmax(tile, sc);
+        sc = sc_next;
+        stage(tile + group);
+        if (group == 0 || tile + 1 < tile1) turn();
+      }
+      if ((tile1 - 1) * G::tokens <= wave_lim) values(tile1 - 1);
+    } else {
+      store_v(tile0);
+      check_ids(next, tile0 + 1);
+      load_k(next);
+      load_v(next);
+      next = load_ids(tile0 + 2);
+      __syncthreads();
+      for (int tile = tile0; tile < tile1; ++tile) {
+        sc_next = load_scales(all);
+        all = load_all_ids(tile + 2);
+        check_scales(sc, tile);
+        if (tile * G::tokens <= wave_lim) {
+          scores(tile);
+          softmax(tile, sc);
+          values(tile);
+        }
+        sc = sc_next;
+        if (tile + 1 < tile1) {
+          store_k(tile + 1);
+          store_v(tile + 1);
+          check_ids(next, tile + 2);
+          load_k(next);
+          load_v(next);
+          next = load_ids(tile + 3);
+        }
+        __syncthreads();
+      }
     }
   }
+  __syncthreads();  // bad_dim and bad_tok are whole
   if (!active) return;
+  const int first_bad = bad_tok;
 
   sum += __shfl_xor(sum, 32);
   const float qnan = __builtin_nanf("");
@@ -482,7 +620,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
       x *= f;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (tile0 < tile1 && lim >= bad_dim[dim + e]) x[e] = qnan;
+        if (lim >= bad_dim[dim + e]) x[e] = qnan;
       if (p.nsplit > 1)
         *reinterpret_cast<f32x4*>(p.part_o + part_row * D + dim) = x;
       else
@@ -531,14 +669,14 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillParams p) {
   }
 }
 
-template <int D, int KV>
+template <int D, int KV, int kWaves>
 hipError_t launch_prefill_t(PrefillParams p, hipStream_t stream) {
   // (A launch holds fewer than 2^32 threads.)
-  constexpr int64_t kMost = 0xFFFFFFFFll / kPfThreads;
-  p.units = prefill_items(p.num_seqs, p.num_tokens, p.g) * p.hkv * p.nsplit;
+  constexpr int64_t kMost = 0xFFFFFFFFll / (64 * kWaves);
+  p.units = prefill_items(p.num_seqs, p.num_tokens, p.g, 32 * kWaves) * p.hkv * p.nsplit;
   for (p.unit0 = 0; p.unit0 < p.units; p.unit0 += kMost) {
     const int64_t n = p.units - p.unit0 < kMost ? p.units - p.unit0 : kMost;
-    hipLaunchKernelGGL((prefill_kernel<D, KV>), dim3(static_cast<unsigned>(n)), dim3(kPfThreads), 0, stream, p);
+    hipLaunchKernelGGL((prefill_kernel<D, KV, kWaves>), dim3(static_cast<unsigned>(n)), dim3(64 * kWaves), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -555,13 +693,20 @@ hipError_t launch_prefill_t(PrefillParams p, hipStream_t stream) {
   return hipSuccess;
 }
 
+template <int D, int KV>
+hipError_t launch_prefill_rows(const PrefillParams& p, hipStream_t stream) {
+  if constexpr (KV != kKvF32)
+    if (p.tile_rows == kPrefillWideRows) return launch_prefill_t<D, KV, kPrefillWideRows / 32>(p, stream);
+  return launch_prefill_t<D, KV, kPrefillRows / 32>(p, stream);
+}
+
 template <int D>
 hipError_t launch_prefill_d(const PrefillParams& p, int kv_kind, hipStream_t stream) {
   switch (kv_kind) {
-    case kKvF32: return launch_prefill_t<D, kKvF32>(p, stream);
-    case kKvBf16: return launch_prefill_t<D, kKvBf16>(p, stream);
-    case kKvFp8: return launch_prefill_t<D, kKvFp8>(p, stream);
-    default: return launch_prefill_t<D, kKvMx4>(p, stream);
+    case kKvF32: return launch_prefill_rows<D, kKvF32>(p, stream);
+    case kKvBf16: return launch_prefill_rows<D, kKvBf16>(p, stream);
+    case kKvFp8: return launch_prefill_rows<D, kKvFp8>(p, stream);
+    default: return launch_prefill_rows<D, kKvMx4>(p, stream);
   }
 }
 
