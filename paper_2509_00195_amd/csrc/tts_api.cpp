@@ -696,26 +696,35 @@ tts_status tts_prefix_decode_merge(const tts_attn_desc* d, const tts_prefix_meta
 
 // ---- ragged prefill ------------------------------------------------------------
 
-// Rows of a workgroup: the wide kind where a sequence has as many on average.
-static int32_t prefill_rows_per(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens) {
-  const int64_t g = d->num_q_heads / d->num_kv_heads;
-#ifdef TTS_NO_WIDE
-  return tts::kPrefillRows;
-#endif
-  const bool wide = d->kv_dtype != TTS_F32 && num_tokens * g >= static_cast<int64_t>(num_seqs) * tts::kPrefillWideRows;
-  return wide ? tts::kPrefillWideRows : tts::kPrefillRows;
-}
-
-// Splits of every tile of rows over its tokens: as many as fill the card's
-// 256 compute units with eight waves each.
+// Splits of every tile of rows over its tokens: the number for which a model
+// of the call's time is least. A workgroup takes about `step` us per tile of
+// tokens alone on its compute unit and a third more beside another (512
+// are resident), and 3 us to begin and end; the join costs a launch of 4 us
+// and the states' bytes (written and read at 3.5 TB/s). Measured, bf16: 512
+// tokens of a prompt, 28 heads, one or two splits: 19.6, 24.2 us; 33 tokens
+// over 533, 12 heads, one, two, four, eight: 20.4, 18.0, 15.8, 15.7; 64 tokens
+// over 8,064, 28 heads, one, 15, 31: 177, 29.8, 32.3.
 static int32_t prefill_nsplit(const tts_attn_desc* d, int32_t num_seqs, int32_t num_tokens, int32_t max_seq_len) {
+  if (num_seqs <= 0 || num_tokens <= 0) return 1;
+  const bool f32 = d->kv_dtype == TTS_F32;
   const int64_t g = d->num_q_heads / d->num_kv_heads;
-  const int32_t rows = prefill_rows_per(d, num_seqs, num_tokens);
-  const int64_t units = tts::prefill_items(num_seqs, num_tokens, g, rows) * d->num_kv_heads;
-  const int64_t fill = units > 0 ? 65536 / rows / units : 1;
-  const int64_t fit = max_seq_len / tts::kPrefillSplitTokens;
-  const int64_t n = std::min({fill, fit, static_cast<int64_t>(tts::kPrefillMaxSplit)});
-  return n < 1 ? 1 : static_cast<int32_t>(n);
+  const int64_t units = tts::prefill_items(num_seqs, num_tokens, g) * d->num_kv_heads;
+  // The causal half of a chunk is not seen.
+  const double chunk = std::min<double>(max_seq_len, static_cast<double>(num_tokens) / num_seqs);
+  const double tiles = std::max(1.0, (max_seq_len - 0.5 * chunk) / (f32 ? 32 : 64)), step = f32 ? 2.5 : 1.0;
+  const double state_us = static_cast<double>(num_tokens) * d->num_q_heads * d->head_dim * 8 / 3.5e6;
+  int32_t best = 1;
+  double least = 0;
+  for (int32_t n = 1; n <= tts::kPrefillMaxSplit && n <= tiles; ++n) {
+    const double all = static_cast<double>(units) * n, rounds = std::ceil(all / 512);
+    double us = rounds * (std::ceil(tiles / n) * step * (all > 256 ? 1.3 : 1.0) + 3);
+    if (n > 1) us += 4 + n * state_us;
+    if (n == 1 || us < least) {
+      least = us;
+      best = n;
+    }
+  }
+  return best;
 }
 
 static size_t prefill_rows(const tts_attn_desc* d, int32_t num_tokens) {
@@ -774,7 +783,6 @@ tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int3
   p.hkv = d->num_kv_heads;
   p.g = d->num_q_heads / d->num_kv_heads;
   p.nsplit = prefill_nsplit(d, num_seqs, num_tokens, max_seq_len);
-  p.tile_rows = prefill_rows_per(d, num_seqs, num_tokens);
   p.out_bf16 = d->out_dtype == TTS_BF16;
   p.scale_log2 = scale_log2(d);
   if (p.nsplit > 1) {

@@ -82,6 +82,29 @@ __device__ __forceinline__ uint4 mx4x8_to_bf16x8(uint32_t w, uint2 s) {
                mix(mx4x2_to_bf16x2<3>(w, mx_scale<2>(s.y)), mx4x2_to_bf16x2<3>(w, mx_scale<3>(s.y)))};
 }
 
+// A value at a uniform address that the kernel does not write.
+template <typename T>
+__device__ __forceinline__ T scalar(const T* at) {
+  typedef const T __attribute__((address_space(4))) * P;
+  return *(P)(reinterpret_cast<uintptr_t>(at));
+}
+
+// The sequence whose range of items holds `item`, when sequence b's begins at
+// first(b), increasing with b. Every wave looks for itself, 64 sequences at a
+// step; in bounds and finite whatever the offsets hold.
+template <typename F>
+__device__ __forceinline__ int find_seq(int num_seqs, int64_t item, F first) {
+  const int lane = threadIdx.x & 63;
+  int64_t lo = 0, hi = num_seqs;
+  while (hi - lo > 1) {
+    const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const bool le = lane == 0 || (at < hi && first(at) <= item);
+    lo += (__builtin_popcountll(__builtin_amdgcn_ballot_w64(le)) - 1) * step;
+    hi = hi < lo + step ? hi : lo + step;
+  }
+  return __builtin_amdgcn_readfirstlane(static_cast<int>(lo));
+}
+
 // Four elements of an output row from element `at` on.
 __device__ __forceinline__ void store_out4(void* out, bool bf16, int64_t at, f32x4 x) {
   if (bf16)

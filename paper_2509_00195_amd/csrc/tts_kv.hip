@@ -245,29 +245,17 @@ struct RopeItem {
 // The item's sequence: items [f(b), f(b + 1)) belong to sequence b, with
 // f(b) = offsets[b] / 16 + 2 b. A sequence of n > 0 new tokens touches at
 // most (n + 30) / 16 blocks (rounded down), which is at most
-// f(b + 1) - f(b); the items past its last block are empty. Found by every
-// wave alone in steps of 64 (in bounds and finite whatever the offsets hold).
-__device__ __forceinline__ int64_t first_item(const RopeParams& p, int64_t b) {
-  return (static_cast<int64_t>(p.tok_offsets[b]) >> 4) + 2 * b;
-}
-
+// f(b + 1) - f(b); the items past its last block are empty.
 __device__ __forceinline__ RopeItem rope_item(const RopeParams& p, int64_t item) {
-  const int lane = threadIdx.x & 63;
   RopeItem it{0, 0, 0, 0, 0, -1, false};
   int64_t j = 0;
   int t0, t1;
   if (p.tok_offsets) {
-    int64_t lo = 0, hi = p.num_seqs;
-    while (hi - lo > 1) {
-      const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-      const bool le = lane == 0 || (at < hi && first_item(p, at) <= item);
-      lo += (__builtin_popcountll(__builtin_amdgcn_ballot_w64(le)) - 1) * step;
-      hi = hi < lo + step ? hi : lo + step;
-    }
-    it.seq = __builtin_amdgcn_readfirstlane(static_cast<int>(lo));
+    auto first = [&](int64_t b) { return (static_cast<int64_t>(p.tok_offsets[b]) >> 4) + 2 * b; };
+    it.seq = find_seq(p.num_seqs, item, first);
     t0 = p.tok_offsets[it.seq];
     t1 = p.tok_offsets[it.seq + 1];
-    j = item - ((static_cast<int64_t>(t0) >> 4) + 2 * static_cast<int64_t>(it.seq));
+    j = item - first(it.seq);
     if (t0 < 0 || t1 < t0 || t1 > p.num_tokens || j < 0) return it;
   } else {
     it.seq = static_cast<int>(item);

@@ -8,14 +8,10 @@
 namespace tts {
 
 // Query rows of a workgroup: rows of one sequence and one KV head, token by
-// token with the head's query heads side by side: the first for chunks of few
-// rows and fp32 caches, the second for the others.
+// token with the head's query heads side by side.
 constexpr int kPrefillRows = 128;
-constexpr int kPrefillWideRows = 256;
-// Splits of a tile of rows over the tokens, and the tokens that one is given
-// at least (less, and the joining costs more than it brings).
+// Splits of a tile of rows over the tokens, at most.
 constexpr int kPrefillMaxSplit = 32;
-constexpr int kPrefillSplitTokens = 256;
 
 struct PrefillParams {
   const void* q;
@@ -40,15 +36,14 @@ struct PrefillParams {
   int32_t hkv;
   int32_t g;
   int32_t nsplit;
-  int32_t tile_rows;
   int32_t out_bf16;
   float scale_log2;
 };
 
 // Items (tiles of rows, some empty) of a call: sequence b has items
-// [off[b] * g / tile_rows + b, the same of b + 1).
-inline int64_t prefill_items(int64_t num_seqs, int64_t num_tokens, int64_t g, int64_t tile_rows) {
-  return num_tokens * g / tile_rows + num_seqs;
+// [off[b] * g / kPrefillRows + b, the same of b + 1).
+inline int64_t prefill_items(int64_t num_seqs, int64_t num_tokens, int64_t g) {
+  return num_tokens * g / kPrefillRows + num_seqs;
 }
 
 }  // namespace tts
