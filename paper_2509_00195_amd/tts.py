@@ -186,15 +186,15 @@ def make_desc(num_q_heads, num_kv_heads, head_dim, block_size=16, q_dtype="bf16"
 
 
 def _ptr(x) -> Optional[int]:
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        if not x.is_contiguous():
-            raise ValueError("device tensors must be contiguous")
-        return x.data_ptr()
-    raise TypeError(f"cannot pass {type(x)} as a device pointer")
+    try:
+        contiguous, at = x.is_contiguous(), x.data_ptr()
+    except AttributeError:
+        raise TypeError(f"cannot pass {type(x)} as a device pointer") from None
+    if not contiguous:
+        raise ValueError("device tensors must be contiguous")
+    return at
 
 
 def _stream(stream) -> Optional[int]:
@@ -439,11 +439,12 @@ def tts_rope_tables(rot_dim: int, theta: float, max_pos: int):
 
 def make_rope(cos, sin, interleaved: bool = False) -> tts_rope_desc:
     """The rotation by device tables cos and sin, float32 [max_pos][rot_dim / 2] (which the caller keeps)."""
-    if cos.shape != sin.shape or cos.ndim != 2:
+    shape = cos.shape
+    if len(shape) != 2 or shape != sin.shape:
         raise ValueError("cos and sin must both be [max_pos][rot_dim / 2]")
-    if "float32" not in str(cos.dtype) or "float32" not in str(sin.dtype):
+    if cos.dtype.itemsize != 4 or not cos.dtype.is_floating_point or sin.dtype != cos.dtype:
         raise ValueError("cos and sin must be float32")
-    return tts_rope_desc(2 * int(cos.shape[1]), int(bool(interleaved)), int(cos.shape[0]), _ptr(cos), _ptr(sin))
+    return tts_rope_desc(2 * shape[1], 1 if interleaved else 0, shape[0], _ptr(cos), _ptr(sin))
 
 
 def _rows(x, heads: int, head_dim: int):
@@ -452,11 +453,12 @@ def _rows(x, heads: int, head_dim: int):
         return None, 0
     if isinstance(x, int):
         return x, heads * head_dim
-    if x.ndim != 3 or tuple(x.shape[1:]) != (heads, head_dim):
-        raise ValueError(f"expected rows of [{heads}][{head_dim}], got {tuple(x.shape)}")
-    if x.shape[0] and (x.stride(2) != 1 or x.stride(1) != head_dim):
+    shape, step = x.shape, x.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
+        raise ValueError(f"expected rows of [{heads}][{head_dim}], got {tuple(shape)}")
+    if shape[0] and (step[2] != 1 or step[1] != head_dim):
         raise ValueError("the heads of a token must be contiguous")
-    return x.data_ptr(), int(x.stride(0)) if x.shape[0] > 1 else heads * head_dim
+    return x.data_ptr(), step[0] if shape[0] > 1 else heads * head_dim
 
 
 def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_new, v_new, block_tables,
