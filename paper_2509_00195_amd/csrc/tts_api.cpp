@@ -436,7 +436,7 @@ static int32_t paged_nsplit(const tts_attn_desc* d, int32_t num_seqs, int32_t ma
   // the splits are as many as give the card kMx4Units of them, no smaller than
   // 16 blocks (one step).
   const int64_t pairs = static_cast<int64_t>(num_seqs) * d->num_kv_heads;
-  const int64_t want = pairs > 0 ? (kMx4Units + pairs - 1) / pairs : 1, most = nblk / 16;
+  const int64_t want = pairs > 0 ? (kMx4Units + pairs - 1) / pairs : 1, most = (nblk + 15) / 16;
   const int64_t ns = want < most ? want : most;
   return ns < 1 ? 1 : static_cast<int32_t>(ns);
 }

@@ -1926,8 +1926,6 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_mx4_kernel(AttnPara
   const size_t blk_stride = static_cast<size_t>(p.hkv) * G::blk_bytes;
   const unsigned char* kbase = static_cast<const unsigned char*>(p.k_cache) + kvh * G::blk_bytes;
   const unsigned char* vbase = static_cast<const unsigned char*>(p.v_cache) + kvh * G::blk_bytes;
-  // Split j covers blocks [j * per, (j + 1) * per) of the beam.
-  const int per = (p.paged_max_len + kTok * p.paged_nsplit - 1) / (kTok * p.paged_nsplit);
   const int L = p.seq_lens[b];
   QFrag<D, KV> q;
   {
@@ -1942,6 +1940,10 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_mx4_kernel(AttnPara
     bad = true;
     nb = 0;
   }
+  // Split j covers blocks [j * per, (j + 1) * per) of the beam: equal parts of
+  // its own length, whatever the longest, in steps of one quad for each wave.
+  constexpr int kStep = 4 * kPagedWaves;
+  const int per = kStep * ((nb + kStep * p.paged_nsplit - 1) / (kStep * p.paged_nsplit));
   const int first = split * per;
   int n = nb - first;
   n = n < 0 ? 0 : (n < per ? n : per);
