@@ -191,7 +191,8 @@ static tts_status build_meta_impl(int32_t num_reqs, const int32_t* req_seq_offse
       return fail(TTS_ERR_HIP, "cannot query the device's compute-unit count");
     }
     try {
-      tts::build_work_plan(m->host, {desc->num_q_heads, desc->num_kv_heads, desc->head_dim, kv_bytes(desc), ncu},
+      tts::build_work_plan(m->host, {desc->num_q_heads, desc->num_kv_heads, desc->head_dim, kv_bytes(desc), ncu,
+                                      desc->kv_dtype == TTS_MXFP4},
                            &m->plan, warm);
     } catch (const std::bad_alloc&) {
       delete m;
@@ -376,7 +377,8 @@ tts_status tts_plan_units_host(int32_t num_reqs, const int32_t* req_seq_offsets,
   try {
     const int rc = tts::build_host_meta(in, &host, &err);
     if (rc != 0) return fail(static_cast<tts_status>(rc), err);
-    tts::build_work_plan(host, {desc->num_q_heads, desc->num_kv_heads, desc->head_dim, kv_bytes(desc), num_workgroups},
+    tts::build_work_plan(host, {desc->num_q_heads, desc->num_kv_heads, desc->head_dim, kv_bytes(desc), num_workgroups,
+                                desc->kv_dtype == TTS_MXFP4},
                          &plan);
   } catch (const std::bad_alloc&) {
     return fail(TTS_ERR_NOMEM, "out of host memory");

@@ -86,6 +86,7 @@ struct WorkPlan {
 struct PlanShape {
   int32_t num_q_heads, num_kv_heads, head_dim, kv_bytes;
   int32_t num_bins;  // persistent workgroups (one per compute unit)
+  bool mx4;          // a 4-bit cache (kv_bytes 1, as fp8 ones)
 };
 
 // warm: a plan of an earlier batch of the same shape (e.g. before a fork);

@@ -48,6 +48,11 @@ namespace {
 //   pair): 5.3 us + (0.27 + 0.011 tiles) us per 8 KiB block; more tiles:
 //   5.3 us + (0.12 + 0.029 tiles) us. fp8: 5.3 us + (0.175 + 0.0325 tiles)
 //   us per block, in both forms.
+// * 4-bit: as fp8, with 0.15 us per narrow block and (0.12 + 0.0325 tiles) us
+//   per wide one (whole calls against the fp8 terms: 256 beams over four
+//   trees 37.8 us instead of 42.4, 16 beams 14.6 instead of 15.8, D 64 12.9
+//   instead of 13.4, 64 beams 25.9 instead of 26.2; three more shapes and a
+//   verification the same).
 // * fp32 (16 rows to a wave group, four groups of two waves above 32 rows):
 //   the larger of 0.26 us per 8 KiB of blocks and of the matrix cores' time,
 //   0.24 us per block and row tile (D 128; four times the largest tile's
@@ -62,6 +67,7 @@ constexpr double kHalvesBlockUs = 0.27, kHalvesTileUs = 0.011;
 constexpr double kFullBlockUs = 0.12, kFullTileUs = 0.029;
 constexpr double kFp8NarrowBlockUs = 0.225;
 constexpr double kFp8WideBlockUs = 0.175, kFp8WideTileUs = 0.0325;
+constexpr double kMx4NarrowBlockUs = 0.15, kMx4WideBlockUs = 0.12;
 constexpr double kF32NarrowBlockUs = 0.26, kF32TileBlockUs = 0.24;
 // Where the batch holds many bytes per workgroup the narrow units' blocks
 // come at the rate of the memory, not of one workgroup's round trips: 0.33
@@ -96,7 +102,7 @@ struct NarrowLoad {
 
 struct CostModel {
   double blk_bytes, q_row_bytes, part_row_bytes, d_scale;
-  bool fp8 = false, f32 = false;
+  bool coded = false, mx4 = false, f32 = false;  // coded: fp8 or 4-bit
   double narrow_scale = 1.0;  // kStreamScale where the batch is bound by streaming
   double row_us() const { return kRowUs * (q_row_bytes + part_row_bytes) / 800.0; }
   // Narrow units: the waves split the block pairs, every wave runs every tile.
@@ -112,12 +118,13 @@ struct CostModel {
   double f32_tile_us() const { return kF32TileBlockUs * d_scale; }
   double narrow_block_us() const {
     if (f32) return blk_bytes * (kF32NarrowBlockUs / 8192);
-    return fp8 ? kFp8NarrowBlockUs : narrow_scale * blk_bytes * (kNarrowBlockUs / 8192);
+    if (coded) return mx4 ? kMx4NarrowBlockUs : kFp8NarrowBlockUs;
+    return narrow_scale * blk_bytes * (kNarrowBlockUs / 8192);
   }
   // Wide units: one block, all tiles.
   double wide_block_us(int rows) const {
     const int nt = tiles_of(rows);
-    if (fp8) return kFp8WideBlockUs + nt * kFp8WideTileUs * d_scale;
+    if (coded) return (mx4 ? kMx4WideBlockUs : kFp8WideBlockUs) + nt * kFp8WideTileUs * d_scale;
     if (nt <= kUnitWaves) return blk_bytes * (kHalvesBlockUs / 8192) + nt * kHalvesTileUs * d_scale;
     return blk_bytes * (kFullBlockUs / 8192) + nt * kFullTileUs * d_scale;
   }
@@ -176,7 +183,7 @@ void build_work_plan(const HostMeta& m, const PlanShape& shape, WorkPlan* plan, 
   // Beams per narrow unit: set per candidate row cap below.
   auto narrow_beams = [&](int32_t cap_rows) { return std::max(1, std::min(kMaxUnitBeams, cap_rows / g)); };
   int32_t RB = narrow_beams(kMaxRows);
-  // Beams per wide unit (bf16 and fp8 caches; segments of fp32 caches are cut
+  // Beams per wide unit (all but fp32 caches; segments of fp32 caches are cut
   // into chunks of as many rows as a narrow unit holds, whatever the cap of
   // the narrow list): set per candidate row cap below.
   const bool wide_mode = shape.kv_bytes <= 2;
@@ -195,7 +202,8 @@ void build_work_plan(const HostMeta& m, const PlanShape& shape, WorkPlan* plan, 
   // A partial state is written once and read once by the merge.
   cm.part_row_bytes = 2.0 * (shape.head_dim * (shape.kv_bytes == 4 ? 4.0 : 2.0) + 4 * kPartMl);
   cm.d_scale = shape.head_dim / 128.0;
-  cm.fp8 = shape.kv_bytes == 1;
+  cm.coded = shape.kv_bytes == 1;
+  cm.mx4 = shape.mx4;
   cm.f32 = shape.kv_bytes == 4;
 
   const bool streaming = static_cast<double>(m.unique_blocks) * hkv * cm.blk_bytes > kStreamBytesPerGroup * nbins;
