@@ -592,8 +592,19 @@ __device__ __forceinline__ Probs<KV> tile_probs(const Scores& s, RowState<D>& st
   float p[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(x[i]);
-  st.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
   Probs<KV> out;
+  if constexpr (KV == kKvMx4) {
+    // The sum is that of the rounded probabilities, which the product uses.
+    uint32_t pb[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pb[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+      st.l = add_bf16x2(pb[i], st.l);
+    }
+    out.p = __builtin_bit_cast(bf16x8, uint4{pb[0], pb[1], pb[2], pb[3]});
+    return out;
+  }
+  st.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
   if constexpr (KV == kKvF32) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) out.p[i] = p[i];
@@ -2026,7 +2037,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_mx4_kernel(AttnPara
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             pb[i] = pack_bf16x2(x[8 * h + 2 * i], x[8 * h + 2 * i + 1]);
-            st.l += __builtin_bit_cast(float, pb[i] << 16) + __builtin_bit_cast(float, pb[i] & 0xFFFF0000u);
+            st.l = add_bf16x2(pb[i], st.l);
           }
           const bf16x8 pr = __builtin_bit_cast(bf16x8, uint4{pb[0], pb[1], pb[2], pb[3]});
 #pragma unroll

@@ -48,11 +48,11 @@ namespace {
 //   pair): 5.3 us + (0.27 + 0.011 tiles) us per 8 KiB block; more tiles:
 //   5.3 us + (0.12 + 0.029 tiles) us. fp8: 5.3 us + (0.175 + 0.0325 tiles)
 //   us per block, in both forms.
-// * 4-bit: as fp8, with 0.15 us per narrow block and (0.12 + 0.0325 tiles) us
-//   per wide one (whole calls against the fp8 terms: 256 beams over four
-//   trees 37.8 us instead of 42.4, 16 beams 14.6 instead of 15.8, D 64 12.9
-//   instead of 13.4, 64 beams 25.9 instead of 26.2; three more shapes and a
-//   verification the same).
+// * 4-bit: as fp8, with 0.25 us per narrow block and (0.10 + 0.06 tiles) us
+//   per wide one, whose conversions every row tile pays for again. Whole calls
+//   against the fp8 terms: 256 beams over four trees 37.8 us instead of 42.3,
+//   16 beams 14.7 instead of 15.7, 64 beams 25.8 and 22.1 instead of 26.6 and
+//   23.0, verification of four tokens 22.6 instead of 21.8, D 64 the same.
 // * fp32 (16 rows to a wave group, four groups of two waves above 32 rows):
 //   the larger of 0.26 us per 8 KiB of blocks and of the matrix cores' time,
 //   0.24 us per block and row tile (D 128; four times the largest tile's
@@ -67,7 +67,7 @@ constexpr double kHalvesBlockUs = 0.27, kHalvesTileUs = 0.011;
 constexpr double kFullBlockUs = 0.12, kFullTileUs = 0.029;
 constexpr double kFp8NarrowBlockUs = 0.225;
 constexpr double kFp8WideBlockUs = 0.175, kFp8WideTileUs = 0.0325;
-constexpr double kMx4NarrowBlockUs = 0.15, kMx4WideBlockUs = 0.12;
+constexpr double kMx4NarrowBlockUs = 0.25, kMx4WideBlockUs = 0.10, kMx4WideTileUs = 0.06;
 constexpr double kF32NarrowBlockUs = 0.26, kF32TileBlockUs = 0.24;
 // Where the batch holds many bytes per workgroup the narrow units' blocks
 // come at the rate of the memory, not of one workgroup's round trips: 0.33
@@ -124,7 +124,8 @@ struct CostModel {
   // Wide units: one block, all tiles.
   double wide_block_us(int rows) const {
     const int nt = tiles_of(rows);
-    if (coded) return (mx4 ? kMx4WideBlockUs : kFp8WideBlockUs) + nt * kFp8WideTileUs * d_scale;
+    if (mx4) return kMx4WideBlockUs + nt * kMx4WideTileUs * d_scale;
+    if (coded) return kFp8WideBlockUs + nt * kFp8WideTileUs * d_scale;
     if (nt <= kUnitWaves) return blk_bytes * (kHalvesBlockUs / 8192) + nt * kHalvesTileUs * d_scale;
     return blk_bytes * (kFullBlockUs / 8192) + nt * kFullTileUs * d_scale;
   }

@@ -459,7 +459,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
       for (int i = 0; i < 16; ++i) {
         const float f = KV == kKvFp8 ? sc.k[(32 * t + reg_token<G::f32>(i)) / kTok] : p.scale_log2;
         s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], f, -sub));
-        sum += s[t][i];
+        if constexpr (G::f32 || KV == kKvFp8) sum += s[t][i];
       }
     if constexpr (!G::f32) {
 #pragma unroll
@@ -472,6 +472,13 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
         }
         pb[j] = uint4{pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]),
                       pack_bf16x2(pv[6], pv[7])};
+        // The sum of the rounded probabilities, which the product uses (fp8:
+        // those are multiplied by the V scales).
+        if constexpr (KV != kKvFp8) {
+          const uint32_t w[4] = {pb[j].x, pb[j].y, pb[j].z, pb[j].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum = add_bf16x2(w[e], sum);
+        }
       }
     }
   };
