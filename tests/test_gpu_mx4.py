@@ -215,3 +215,30 @@ def test_long_sequences_past_32_bit_offsets():
     tts_paged_decode_attn(desc, 1, q, *big, None, None, _up(t), t.shape[1], _up(c.lens), 70001, nb, out, ws, size)
     want, tol = reference(c, 0, qv)
     close(out, want, tol)
+
+
+@pytest.mark.parametrize("gain", [1.0, 6.0])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 4, 64), (16, 4, 128)])
+def test_paged_many_unsplit_sequences(hq, hkv, d, gain):
+    """So many sequences that none is split: a wave reads its block ids in several turns; at gain 6 with the repeat."""
+    rng = np.random.default_rng(30)
+    lens = np.full(130, 20)
+    lens[:6] = [5000, 4097, 6000, 0, 1, 1025]
+    c = Cache("mx4", hkv, d, lens, rng, gain=gain)
+    c.poison()
+    q, qv = queries("mx4", (130, hq, d), rng, gain)
+    out = torch.full((130, hq, d), 5.0, device=DEV)
+    _paged(c, desc_of("mx4", hq, hkv, d), q, out)
+    _check(c, out, qv, False)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_paged_bound_far_above_the_lengths(d):
+    """max_seq_len for 20,000 tokens, sequences of none to 300: most splits are empty."""
+    rng = np.random.default_rng(31)
+    c = Cache("mx4", 2, d, [1, 17, 0, 300, 64, 257], rng, cols=1250)
+    c.poison()
+    q, qv = queries("mx4", (6, 10, d), rng)
+    out = torch.full((6, 10, d), 5.0, device=DEV)
+    _paged(c, desc_of("mx4", 10, 2, d), q, out, most=20000)
+    _check(c, out, qv, False)

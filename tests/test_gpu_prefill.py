@@ -205,3 +205,57 @@ def test_offsets_past_32_bits(kind):
     out = torch.zeros((60, 16, 128), device=DEV)
     _call(c, desc_of(kind, 16, 8, 128), [50, 10], q, out, tables=t, caches=(*big, *sc), nb=nb)
     _check(c, [50, 10], out, qv, False)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("hq,hkv,d", [(6, 2, 128), (9, 3, 64)])
+def test_long_chunks(kind, hq, hkv, d):
+    """Several row and token tiles to a sequence, chunk and length not multiples of either."""
+    rng = np.random.default_rng(20)
+    lens, new = [700, 333, 1030, 65], [650, 333, 514, 64]
+    c = Cache(kind, hkv, d, lens, rng)
+    c.poison()
+    q, qv = queries(kind, (sum(new), hq, d), rng, 2.0)
+    out = torch.zeros((sum(new), hq, d), device=DEV)
+    _call(c, desc_of(kind, hq, hkv, d), new, q, out)
+    _check(c, new, out, qv, False)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(7, 1, 128), (2, 2, 64)])
+def test_fp8_scales_of_any_sign(hq, hkv, d):
+    """K and V scales that are zero, negative, tiny and large, one block or several to a tile."""
+    rng = np.random.default_rng(21)
+    lens, new = [200, 77], [150, 77]
+    c = Cache("fp8", hkv, d, lens, rng)
+    t = c.tables
+    c.ks[t[0, 1]], c.ks[t[0, 6]] = 0.0, -c.ks[t[0, 6]]
+    c.vs[t[0, 2]], c.vs[t[0, 5]], c.vs[t[0, 9]] = 0.0, -c.vs[t[0, 5]], 1e-30
+    c.ks[t[1, 0]], c.vs[t[1, 0]], c.vs[t[1, 3]] = 1e-30, 0.0, 3.0
+    q, qv = queries("fp8", (sum(new), hq, d), rng)
+    out = torch.zeros((sum(new), hq, d), device=DEV)
+    _call(c, desc_of("fp8", hq, hkv, d), new, q, out)
+    _check(c, new, out, qv, False)
+
+
+def test_two_streams():
+    """Two calls at once, each with its own workspace and output, give what they give alone."""
+    rng = np.random.default_rng(22)
+    lens, new = [3000, 500, 40], [9, 200, 40]
+    c = Cache("bf16", 2, 128, lens, rng)
+    q, _ = queries("bf16", (sum(new), 8, 128), rng)
+    desc, n, most = desc_of("bf16", 8, 2, 128), len(lens), 3000
+    offs, t, dl = _up(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), _up(c.tables), _up(c.lens)
+    cache = c.device()
+    size = tts_paged_prefill_workspace_size(desc, n, sum(new), most)
+    ws = [torch.zeros(max(size, 1), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    out = [torch.zeros((sum(new), 8, 128), device=DEV) for _ in range(3)]
+    call = lambda i, s, o: tts_paged_prefill_attn(  # noqa: E731
+        desc, n, sum(new), offs, q, *cache, t, t.shape[1], dl, most, c.nb, o, ws[i], size, s)
+    call(0, None, out[2])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            call(i, s, out[i])
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[2])
