@@ -313,9 +313,9 @@ tts_status tts_prefix_verify_attn(const tts_attn_desc* d, const tts_prefix_meta*
  *   q [num_tokens][Hq][D], out [num_tokens][Hq][D]; rows behind the last
  *     sequence's are left as they are; both and the caches aligned to 16 bytes.
  *   max_seq_len: host upper bound on seq_lens.
- *   workspace: at least tts_paged_prefill_workspace_size bytes (chunks of few
- *     rows are split over the tokens; 0 and NULL otherwise). Calls that
- *     overlap in time must not share one.
+ *   workspace: at least tts_paged_prefill_workspace_size bytes, aligned to 16
+ *     (chunks of few rows are split over the tokens; 0 and NULL otherwise).
+ *     Calls that overlap in time must not share one.
  * Device-side errors: a sequence longer than max_seq_len or its table row, or
  * shorter than its new tokens, has NaN rows (seq_len <= 0: zero rows); a block
  * id outside [0, num_blocks) makes the rows that see the block NaN. More than
@@ -333,7 +333,7 @@ tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int3
  * them separately (to overlap the merge with other work, or to time the
  * attention kernel alone). tts_prefix_decode_partials runs the work units
  * and leaves one partial softmax state (reference max, sum, and the output
- * row: for bf16 and fp8 caches in fp16, divided by a power of two, with a
+ * row: for all but fp32 caches in fp16, divided by a power of two, with a
  * factor that takes it to the row normalised by the sum; for fp32 caches
  * normalised, in fp32) per (beam, query head, slot) in the workspace;
  * tts_prefix_decode_merge combines each beam's states, in slot order, into

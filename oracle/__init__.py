@@ -20,6 +20,9 @@ slow and written to be checked by eye against its definitions:
   (DuplicateThenTruncate, Sec. 3.1 and Alg. 1) and the lengths the
   duplicates keep after speculation (truncation drawn around the ratio R,
   Sec. 4.1).
+* ``cached_ops`` -- the steps around cached attention in 64 bits: position
+  rotation, 4-bit blocks (E2M1 codes with E8M0 scales), and the causal
+  attention of a chunk's tokens.
 * ``schedule`` -- dynamic prefix-aware scheduling (Sec. 4.2): the greedy
   shared-prefix order, budgeted batches and the eviction cost.
 * ``kv_alloc`` -- roofline-guided KV allocation (Sec. 4.3): the modelled

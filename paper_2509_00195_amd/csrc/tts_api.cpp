@@ -766,6 +766,8 @@ tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int3
   const size_t need = tts_paged_prefill_workspace_size(d, num_seqs, num_tokens, max_seq_len);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(TTS_ERR_WORKSPACE, "workspace smaller than tts_paged_prefill_workspace_size");
+  if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+    return fail(TTS_ERR_INVALID_ARG, "workspace must be aligned to 16 bytes");
   tts::PrefillParams p{};
   p.q = q;
   p.k_cache = k_cache;

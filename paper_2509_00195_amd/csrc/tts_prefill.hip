@@ -22,6 +22,21 @@
 // the 64 lanes of a wave read for one operand), and inside a fragment at a
 // place XORed with the piece's column, so that neither the stores (rows of
 // the cache, 16 bytes per thread) nor the reads meet in a bank.
+//
+// Rounding: probabilities go to bf16 for the second product; the row's sum is
+// that of the rounded ones (fp8 caches, whose probabilities are multiplied by
+// V scales first: of the unrounded ones; dividing the rounded sum by the scale
+// again, or folding the scale into the exponent, took 2 to 5% longer).
+//
+// Bound by the issue of matrix and vector instructions, which overlap only in
+// part between the two waves of a SIMD: one sequence of 16,384 tokens, 28 over
+// 4 heads of 128, takes 1.95 ms (985 TFLOP/s, 0.72 of a large bf16 matrix
+// product here); eight ragged prompts of 200 to 2048 110 us; chunks over 8,000
+// to 16,000 tokens of an fp8 cache 167 us. Tried: eight waves in two groups
+// that take turns at the matrix cores (4% faster at 16,384 tokens, fp8 chunks
+// 264 us, D 64 98 instead of 78); the exponentials of one half of a tile
+// between the products of the other (2.10 ms); four or eight LDS reads ahead
+// instead of six (the same).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

@@ -75,7 +75,7 @@ static_assert(sizeof(UnitRec) == 32 + 4 * kMaxWideBeams + 16 * kMaxEntries, "Uni
 // Partial softmax state of one query row over a subset of its tokens:
 // the reference maximum m (log2 units), the sum l of 2^(score - m), the
 // row's elements and their factor z, with element x z = o / l (the
-// normalised value average). For bf16 and fp8 caches the elements are o
+// normalised value average). For all but fp32 caches the elements are o
 // divided by a power of two 2^e chosen so that every element lies in
 // [-1, 1], in fp16 (2 bytes per element instead of 4; scaled so, the
 // elements keep fp16's full relative precision and never overflow), and

@@ -82,6 +82,7 @@ def test_prefill_workspace():
     assert need > 0
     assert _status(_prefill, size=need - 1) == T.TTS_ERR_WORKSPACE
     assert _status(_prefill, ws=None) == T.TTS_ERR_WORKSPACE
+    assert _status(_prefill, ws=A + 8) == T.TTS_ERR_INVALID_ARG  # aligned to 16 bytes
     assert T.tts_paged_prefill_workspace_size(d, 2, 40, 200) == 0  # too short to split
     assert T.tts_paged_prefill_workspace_size(d, 64, 1 << 16, 4096) == 0  # rows enough
     assert T.tts_paged_prefill_workspace_size(d, -1, 40, 1000) == 0
