@@ -216,7 +216,8 @@ size_t tts_paged_decode_workspace_size(const tts_attn_desc* d, int32_t num_seqs,
  * exploiting sharing: every beam reads all of its blocks (the non-sharing
  * baseline; paged attention of the serving substrate, Sec. 2.3).
  * max_seq_len: host upper bound on seq_lens (sizes the split of long
- * sequences); beams longer than it get NaN rows.
+ * sequences; MXFP4 caches: 2^31 - 2^16 at most); beams longer than it get NaN
+ * rows.
  * num_blocks: size of the block pool (ids outside it give NaN rows).
  * workspace: device buffer of at least tts_paged_decode_workspace_size
  * bytes (TTS_ERR_WORKSPACE otherwise); NULL allowed when that size is 0.
@@ -312,7 +313,7 @@ tts_status tts_prefix_verify_attn(const tts_attn_desc* d, const tts_prefix_meta*
  * and NaN included, does not reach its row.
  *   q [num_tokens][Hq][D], out [num_tokens][Hq][D]; rows behind the last
  *     sequence's are left as they are; both and the caches aligned to 16 bytes.
- *   max_seq_len: host upper bound on seq_lens.
+ *   max_seq_len: host upper bound on seq_lens, 2^31 - 2^16 at most.
  *   workspace: at least tts_paged_prefill_workspace_size bytes, aligned to 16
  *     (chunks of few rows are split over the tokens; 0 and NULL otherwise).
  *     Calls that overlap in time must not share one.

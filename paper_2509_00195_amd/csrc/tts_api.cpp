@@ -73,6 +73,9 @@ constexpr int32_t kPagedSplitBlocks = 32;
 // to 4096 tokens 34.0, 36.3, 41.3 us; 256 of up to 1100 33.2, 33.3, 47.0; four
 // of 60,000 to 120,000 51.4, 55.9, 63.5.
 constexpr int64_t kMx4Units = 512;
+// Longest sequences of a prefill and of the 4-bit paged path: token indices
+// rounded up to whole tiles stay inside int32.
+constexpr int32_t kMaxSeqLen = 0x7FFF0000;
 // Query heads of a rotating append: the parts of its grid stay below 65,536.
 constexpr int32_t kMaxRopeHeads = 8192;
 
@@ -463,6 +466,7 @@ tts_status tts_paged_decode_attn(const tts_attn_desc* d, int32_t num_seqs, const
     return fail(TTS_ERR_INVALID_ARG, "negative size");
   if (static_cast<int64_t>(max_seq_len) > static_cast<int64_t>(max_blocks_per_seq) * 16)
     return fail(TTS_ERR_INVALID_ARG, "max_seq_len exceeds max_blocks_per_seq * block_size");
+  if (d->kv_dtype == TTS_MXFP4 && max_seq_len > kMaxSeqLen) return fail(TTS_ERR_UNSUPPORTED, "max_seq_len too large");
   if (num_seqs == 0) return ok();
   if (!q || !k_cache || !v_cache || !block_tables || !seq_lens || !out)
     return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
@@ -755,6 +759,7 @@ tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int3
     return fail(TTS_ERR_INVALID_ARG, "negative size");
   if (static_cast<int64_t>(max_seq_len) > static_cast<int64_t>(max_blocks_per_seq) * 16)
     return fail(TTS_ERR_INVALID_ARG, "max_seq_len exceeds max_blocks_per_seq * block_size");
+  if (max_seq_len > kMaxSeqLen) return fail(TTS_ERR_UNSUPPORTED, "max_seq_len too large");
   if (static_cast<int64_t>(num_tokens) * d->num_q_heads > 0x7FFFFFFF)
     return fail(TTS_ERR_UNSUPPORTED, "more than 2^31 - 1 query rows");
   if (num_seqs == 0 || num_tokens == 0) return ok();

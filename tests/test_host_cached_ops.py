@@ -89,6 +89,13 @@ def test_prefill_workspace():
     assert _status(_prefill, n=(1 << 31) // 8) == T.TTS_ERR_UNSUPPORTED
 
 
+def test_sequences_whose_tiles_would_pass_int32():
+    most, cols = (1 << 31) - 1, 1 << 27
+    assert _status(_prefill, most=most, cols=cols) == T.TTS_ERR_UNSUPPORTED
+    d = T.make_desc(8, 2, 64, kv_dtype="mx4")
+    assert _status(T.tts_paged_decode_attn, d, 2, A, A, A, None, None, A, cols, A, most, 8, A, A, 1 << 60) == T.TTS_ERR_UNSUPPORTED
+
+
 @pytest.mark.parametrize("args", [
     dict(q_dtype="f32", kv_dtype="mx4"), dict(q_dtype="bf16", kv_dtype="f32"), dict(out_dtype=2), dict(out_dtype=3),
     dict(kv_dtype=4), dict(head_dim=96), dict(block_size=32),
