@@ -34,16 +34,17 @@ METRIC = "beam-tokens/s per decode step + % HBM peak (unique KV bytes), 1 MI355X
 HBM_PEAK_GBS = 8000.0
 KERNEL_SRC = os.path.join(ROOT, "paper_2509_00195_amd", "csrc", "tts_kernels.hip")
 PLANNER_SRC = os.path.join(ROOT, "paper_2509_00195_amd", "csrc", "tts_plan.cpp")
+DEVICE_HDR = os.path.join(ROOT, "paper_2509_00195_amd", "csrc", "tts_device.h")
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "traffic.json")
 
 
 def kernel_sha() -> str:
-    """Hash of the attention kernel's source, the work planner's source and the device compile flags (a traffic
+    """Hash of the attention kernel's sources, the work planner's source and the device compile flags (a traffic
     record is valid only for the code and the plans it was measured on)."""
     from paper_2509_00195_amd.build import DEVICE
 
     h = hashlib.sha256()
-    for src in (KERNEL_SRC, PLANNER_SRC):
+    for src in (KERNEL_SRC, DEVICE_HDR, PLANNER_SRC):
         with open(src, "rb") as f:
             h.update(f.read())
     h.update(" ".join(DEVICE).encode())
