@@ -126,6 +126,15 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // holds dimensions 16 t + 4 lq + j of row ln in o[t][j]; the four lanes of
 // a row call together.
 //
+// state_ref: the reference that a state is stored with. A state without
+// tokens (l = 0) takes no part in the merge's maximum; a NaN m (a bad row)
+// makes the row NaN there, and so must a NaN sum (a NaN key or query), which
+// is not an empty one.
+__device__ __forceinline__ float state_ref(float m, float l) {
+  if (l > 0.f) return m;
+  return (l != l || m != m) ? __builtin_nanf("") : kNegInf;
+}
+
 // partial_exp: the exponent e with every |o| / 2^e below 1, reduced across
 // the row's lanes (every lane of the wave must call it). This and
 // store_partial serve wide units, which fp32 caches do not have.
@@ -160,11 +169,8 @@ __device__ __forceinline__ void store_partial(void* part_o, float* part_ml, int6
   uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(part_o) + prow * D + (D / 4) * lq);
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) dst[c] = uint4{w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]};
-  // A state without tokens (l = 0) takes no part in the merge's maximum; a
-  // NaN m (a bad row) is kept.
-  const float m_out = (l > 0.f || m != m) ? m : kNegInf;
   if (lq == 0)
-    *reinterpret_cast<f32x4*>(part_ml + prow * kPartMl) = f32x4{m_out, l, __builtin_ldexpf(inv, e), 0.f};
+    *reinterpret_cast<f32x4*>(part_ml + prow * kPartMl) = f32x4{state_ref(m, l), l, __builtin_ldexpf(inv, e), 0.f};
 }
 
 // Largest value over the sixteen lanes of a DPP row (rotations within it).
@@ -217,8 +223,7 @@ __device__ __forceinline__ void store_partial_row(void* part_o, float* part_ml, 
 #pragma unroll
     for (int e = 0; e < kEl / 4; ++e) dst[e] = o[e] * inv;
   }
-  const float m_out = (l > 0.f || m != m) ? m : kNegInf;
-  if (active && c == 0) *reinterpret_cast<f32x4*>(part_ml + prow * kPartMl) = f32x4{m_out, l, z, 0.f};
+  if (active && c == 0) *reinterpret_cast<f32x4*>(part_ml + prow * kPartMl) = f32x4{state_ref(m, l), l, z, 0.f};
 }
 
 __device__ __forceinline__ int rl(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
@@ -1384,7 +1389,7 @@ __global__ __launch_bounds__(kThreads, 1) void attn_kernel(AttnParams p) {
             const f32x2 ml = *reinterpret_cast<const f32x2*>(c + 16 * D + 2 * lane);
             // A half that saw no token of the row must not set the reference.
             const float l1 = xlane_sum16(x.l), l2 = xlane_sum16(ml.y);
-            const float m1 = l1 > 0.f ? x.m : kNegInf, m2 = l2 > 0.f ? ml.x : kNegInf;
+            const float m1 = l1 == 0.f ? kNegInf : x.m, m2 = l2 == 0.f ? kNegInf : ml.x;
             const float mx = fmaxf(m1, m2);
             const float f1 = m1 == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m1 - mx);
             const float f2 = m2 == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m2 - mx);
@@ -1684,7 +1689,7 @@ __global__ __launch_bounds__(kThreads, 1) void attn_kernel(AttnParams p) {
     // scores all lie far below it would lose every weight to underflow.
 #pragma unroll
     for (int i = 0; i < kNt; ++i)
-      if (!(st[i].l > 0.f)) st[i].m = kNegInf;
+      if (st[i].l == 0.f) st[i].m = kNegInf;
 #pragma unroll
     for (int i = 0; i < kNt; ++i) {
       if (wave_has && 16 * (ws.grp * kNt + i) < nrows) {
@@ -1870,7 +1875,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, KV == kKvF32 && D == 128 ? 2 : 3)
   // attn_kernel).
   auto slot = [&](int w) { return comb + w * G::comb_floats; };
   st.l = xlane_sum16(st.l);
-  if (!(st.l > 0.f)) st.m = kNegInf;
+  if (st.l == 0.f) st.m = kNegInf;
   if (wave < np) {
     float* c = slot(wave);
 #pragma unroll
@@ -2082,7 +2087,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_mx4_kernel(AttnPara
   // attn_kernel).
   auto slot = [&](int w) { return comb + w * G::comb_floats; };
   st.l = xlane_sum16(st.l);
-  if (!(st.l > 0.f)) st.m = kNegInf;
+  if (st.l == 0.f) st.m = kNegInf;
   if (mine > 0) {
     float* c = slot(wave);
 #pragma unroll
