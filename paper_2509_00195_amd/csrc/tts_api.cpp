@@ -108,6 +108,11 @@ int64_t block_bytes(const tts_attn_desc* d) {
   return elems * kv_bytes(d);
 }
 
+// Table columns that a kernel may read: none where the pool has no block, so
+// that a sequence with tokens is longer than its row, whose answer is NaN, and
+// no kernel takes block 0 in place of a bad one.
+int32_t readable_cols(int32_t max_blocks_per_seq, int32_t num_blocks) { return num_blocks > 0 ? max_blocks_per_seq : 0; }
+
 float scale_log2(const tts_attn_desc* d) {
   const double s = d->scale > 0.f ? d->scale : 1.0 / std::sqrt(static_cast<double>(d->head_dim));
   return static_cast<float>(s * 1.4426950408889634);
@@ -489,7 +494,7 @@ tts_status tts_paged_decode_attn(const tts_attn_desc* d, int32_t num_seqs, const
   p.part_ml = ns > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + part_o_bytes(d, rows))
                      : nullptr;
 
-  p.max_blocks = max_blocks_per_seq;
+  p.max_blocks = readable_cols(max_blocks_per_seq, num_blocks);
   p.num_blocks = num_blocks;
   p.num_seqs = num_seqs;
   p.hq = d->num_q_heads;
@@ -575,7 +580,7 @@ tts_status prefix_params(const tts_attn_desc* d, const tts_prefix_meta* m, const
   p->recs = reinterpret_cast<const tts::UnitRec*>(dev + m->off_recs);
   p->build_len = reinterpret_cast<const int32_t*>(dev + m->off_build);
   p->rows_per_head = m->plan.rows_per_head;
-  p->max_blocks = max_blocks_per_seq;
+  p->max_blocks = readable_cols(max_blocks_per_seq, num_blocks);
   p->num_blocks = num_blocks;
   p->num_seqs = S;
   p->hq = d->num_q_heads;

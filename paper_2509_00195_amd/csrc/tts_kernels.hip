@@ -1819,7 +1819,6 @@ __global__ __launch_bounds__(64 * kPagedWaves, KV == kKvF32 && D == 128 ? 2 : 3)
     v = 0;
   }
   bad = __builtin_amdgcn_ballot_w64(bad) != 0;
-  if (p.num_blocks <= 0) n = 0;  // no block to read at all
   Window win;
   win.id = id;
   win.w = win_word(0, p.g, v);
@@ -2014,7 +2013,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_mx4_kernel(AttnPara
     st.m = m_exact;
     st.l = 0.f;
     st.seen = kNegInf;
-    if (mine > 0 && p.num_blocks > 0) {
+    if (mine > 0) {
       Mx4Quad<D> next;
       int ids = load_ids(0);
       load_quad(next, ids, 0);
