@@ -209,7 +209,8 @@ tts_status tts_plan_units_host(int32_t num_reqs, const int32_t* req_seq_offsets,
                                int32_t num_workgroups, int32_t* out_rows, int64_t cap, int64_t* n_rows,
                                int64_t* num_units);
 
-/* Workspace bytes needed by tts_paged_decode_attn for these sizes. */
+/* Workspace bytes needed by tts_paged_decode_attn for these sizes; they
+ * suffice for every smaller num_seqs and max_seq_len too. */
 size_t tts_paged_decode_workspace_size(const tts_attn_desc* d, int32_t num_seqs, int32_t max_seq_len);
 
 /* Decode attention of every beam over its own paged sequence, without
@@ -220,7 +221,8 @@ size_t tts_paged_decode_workspace_size(const tts_attn_desc* d, int32_t num_seqs,
  * rows.
  * num_blocks: size of the block pool (ids outside it give NaN rows).
  * workspace: device buffer of at least tts_paged_decode_workspace_size
- * bytes (TTS_ERR_WORKSPACE otherwise); NULL allowed when that size is 0.
+ * bytes (a call that needs more than it is given is TTS_ERR_WORKSPACE); NULL
+ * allowed when that size is 0.
  * Calls that overlap in time must not share a workspace. More than
  * 2^31 - 1 partial rows (num_seqs x splits x query heads) is
  * TTS_ERR_UNSUPPORTED. */
@@ -316,7 +318,10 @@ tts_status tts_prefix_verify_attn(const tts_attn_desc* d, const tts_prefix_meta*
  *   max_seq_len: host upper bound on seq_lens, 2^31 - 2^16 at most.
  *   workspace: at least tts_paged_prefill_workspace_size bytes, aligned to 16
  *     (chunks of few rows are split over the tokens; 0 and NULL otherwise).
- *     Calls that overlap in time must not share one.
+ *     The size is that of these counts alone: fewer tokens or sequences may
+ *     be split into more parts and need more. Ask for every call's counts (a
+ *     host computation of a few microseconds) and keep the largest, or ask
+ *     before each call. Calls that overlap in time must not share one.
  * Device-side errors: a sequence longer than max_seq_len or its table row, or
  * shorter than its new tokens, has NaN rows (seq_len <= 0: zero rows); a block
  * id outside [0, num_blocks) makes the rows that see the block NaN. More than

@@ -451,12 +451,25 @@ static int32_t paged_nsplit(const tts_attn_desc* d, int32_t num_seqs, int32_t ma
   return ns < 1 ? 1 : static_cast<int32_t>(ns);
 }
 
-size_t tts_paged_decode_workspace_size(const tts_attn_desc* d, int32_t num_seqs, int32_t max_seq_len) {
-  if (!d || check_desc(d) != TTS_OK || num_seqs < 0 || max_seq_len < 0) return 0;
+// Bytes that a call of these sizes uses.
+static size_t paged_bytes(const tts_attn_desc* d, int32_t num_seqs, int32_t max_seq_len) {
   const int32_t ns = paged_nsplit(d, num_seqs, max_seq_len);
   if (ns == 1) return 0;
   const size_t rows = static_cast<size_t>(num_seqs) * ns * d->num_q_heads;
   return part_o_bytes(d, rows) + align256(rows * tts::kPartMl * 4);
+}
+
+size_t tts_paged_decode_workspace_size(const tts_attn_desc* d, int32_t num_seqs, int32_t max_seq_len) {
+  if (!d || check_desc(d) != TTS_OK || num_seqs < 0 || max_seq_len < 0) return 0;
+  size_t most = paged_bytes(d, num_seqs, max_seq_len);
+  if (d->kv_dtype != TTS_MXFP4) return most;
+  // 4-bit caches: fewer sequences are split into more parts, so that a smaller
+  // batch may use more (none is split from kMx4Units pairs on). The size is
+  // that of the worst of them: a workspace for a program's largest batch
+  // serves its smaller ones.
+  const int64_t last = std::min<int64_t>(num_seqs, kMx4Units / d->num_kv_heads);
+  for (int32_t n = 1; n <= last; ++n) most = std::max(most, paged_bytes(d, n, max_seq_len));
+  return most;
 }
 
 tts_status tts_paged_decode_attn(const tts_attn_desc* d, int32_t num_seqs, const void* q, const void* k_cache,
@@ -476,7 +489,7 @@ tts_status tts_paged_decode_attn(const tts_attn_desc* d, int32_t num_seqs, const
   if (!q || !k_cache || !v_cache || !block_tables || !seq_lens || !out)
     return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
   const int32_t ns = paged_nsplit(d, num_seqs, max_seq_len);
-  const size_t need = tts_paged_decode_workspace_size(d, num_seqs, max_seq_len);
+  const size_t need = paged_bytes(d, num_seqs, max_seq_len);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(TTS_ERR_WORKSPACE, "workspace smaller than tts_paged_decode_workspace_size");
   const size_t rows = static_cast<size_t>(num_seqs) * ns * d->num_q_heads;
