@@ -312,7 +312,9 @@ tts_status tts_prefix_verify_attn(const tts_attn_desc* d, const tts_prefix_meta*
  * stored the chunk's keys and values): query i of sequence b, row
  * tok_offsets[b] + i, is token seq_lens[b] - n_b + i and attends to the tokens
  * 0 .. itself. What is stored at tokens that a query does not see, infinities
- * and NaN included, does not reach its row.
+ * and NaN included, does not reach its row; values that it sees enter as the
+ * formula has them (an infinity makes the dim infinite, both signs or a NaN
+ * make it NaN).
  *   q [num_tokens][Hq][D], out [num_tokens][Hq][D]; rows behind the last
  *     sequence's are left as they are; both and the caches aligned to 16 bytes.
  *   max_seq_len: host upper bound on seq_lens, 2^31 - 2^16 at most.

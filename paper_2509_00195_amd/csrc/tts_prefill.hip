@@ -120,30 +120,45 @@ __device__ __forceinline__ void keep_first(uint4& x, int keep) {
       w[i] &= (2 * i < keep ? 0xFFFFu : 0u) | (2 * i + 1 < keep ? 0xFFFF0000u : 0u);
   }
 }
-// Zeroes elements that are not finite; the first one's place (or 8).
+// What an element that is not finite adds to the rows that see it.
+enum : int { kBadNan = 0, kBadPos = 1, kBadNeg = 2, kBadKinds = 3 };
+
+// Whether an element is not finite: its exponent is all ones. (Two bf16
+// exponents at once: 0x8000 less what an exponent lacks keeps bit 15 only
+// where nothing is lacking.)
 template <bool F32>
-__device__ __forceinline__ int drop_nonfinite(uint4& x) {
-  uint32_t* w = reinterpret_cast<uint32_t*>(&x);
-  int first = 8;
+__device__ __forceinline__ bool any_nonfinite(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t all = 0u;
+  bool any = false;
 #pragma unroll
-  for (int i = 3; i >= 0; --i) {
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F32)
+      any = any || (w[i] & 0x7F800000u) == 0x7F800000u;
+    else
+      all |= 0x80008000u - (~w[i] & 0x7F807F80u);
+  }
+  return F32 ? any : (all & 0x80008000u) != 0u;
+}
+
+// Zeroes elements that are not finite, after f(place, kind) for each.
+template <bool F32, typename F>
+__device__ __forceinline__ void drop_nonfinite(uint4& x, F f) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+  auto each = [&](uint32_t bits, int at) {  // bits: as fp32
+    if ((bits & 0x7F800000u) != 0x7F800000u) return false;
+    f(at, bits & 0x007FFFFFu ? kBadNan : (bits >> 31 ? kBadNeg : kBadPos));
+    return true;
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     if constexpr (F32) {
-      if ((w[i] & 0x7F800000u) == 0x7F800000u) {
-        w[i] = 0u;
-        first = i;
-      }
+      if (each(w[i], i)) w[i] = 0u;
     } else {
-      if ((w[i] & 0x7F800000u) == 0x7F800000u) {
-        w[i] &= 0xFFFFu;
-        first = 2 * i + 1;
-      }
-      if ((w[i] & 0x7F80u) == 0x7F80u) {
-        w[i] &= 0xFFFF0000u;
-        first = 2 * i;
-      }
+      if (each(w[i] << 16, 2 * i)) w[i] &= 0xFFFF0000u;
+      if (each(w[i] & 0xFFFF0000u, 2 * i + 1)) w[i] &= 0xFFFFu;
     }
   }
-  return first;
 }
 
 // The larger of a lane's value and that of the same lane of the other half.
@@ -196,7 +211,9 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
   using C = KvGeo<D, KV>;
   // K and V buffers of even and odd tiles.
   __shared__ __attribute__((aligned(16))) unsigned char lds[4 * G::tensor_bytes];
-  __shared__ int bad_dim[D];  // first token whose value in this dim is not finite (tiles with hidden tokens)
+  // First token whose value in this dim is NaN, +inf, -inf (tiles with hidden tokens).
+  __shared__ int bad_dim[kBadKinds][D];
+  __shared__ int any_bad;  // whether there is one
   __shared__ int bad_tok;     // first token of a block that is not in the pool
 
   // Units in the order (tile of rows, split, KV head), the last tiles of a
@@ -227,8 +244,11 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
   const int tile0 = static_cast<int>(static_cast<int64_t>(ntiles) * split / p.nsplit);
   const int tile1 = static_cast<int>(static_cast<int64_t>(ntiles) * (split + 1) / p.nsplit);
 
-  for (int i = tid; i < D; i += kPfThreads) bad_dim[i] = 0x7FFFFFFF;
-  if (tid == 0) bad_tok = p.num_blocks > 0 ? 0x7FFFFFFF : 0;
+  for (int i = tid; i < kBadKinds * D; i += kPfThreads) (&bad_dim[0][0])[i] = 0x7FFFFFFF;
+  if (tid == 0) {
+    bad_tok = p.num_blocks > 0 ? 0x7FFFFFFF : 0;
+    any_bad = 0;
+  }
 
   typedef typename std::conditional<G::f32, f32x4, uint4>::type Frag;
   // Query rows as the B operand.
@@ -360,7 +380,9 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
   };
   // Values past the last token seen are unused slots; those that some rows
   // see and others do not may be infinities or NaN, which a zero probability
-  // would not keep out.
+  // would not keep out: they are taken out here and added, at the end, to the
+  // rows that see them (whose probability of them counts as above 0, though it
+  // may have underflowed).
   auto store_v = [&](int tile) {
     auto each = [&](auto hidden_c) {
 #pragma unroll
@@ -375,8 +397,10 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
         if constexpr (decltype(hidden_c)::value) {
           const int tok = tile * G::tokens + vcol * G::per;  // the piece's first token
           keep_first<G::f32>(x, seen - tok);
-          const int at_bad = drop_nonfinite<G::f32>(x);
-          if (at_bad < 8) atomicMin(&bad_dim[dim], tok + at_bad);
+          if (any_nonfinite<G::f32>(x)) {
+            drop_nonfinite<G::f32>(x, [&](int e, int kind) { atomicMin(&bad_dim[kind][dim], tok + e); });
+            any_bad = 1;
+          }
         }
         *reinterpret_cast<uint4*>(vbuf(tile) + v_place<G>(dim, vcol)) = x;
       }
@@ -556,6 +580,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
   __syncthreads();  // bad_dim and bad_tok are whole
   if (!active) return;
   const int first_bad = bad_tok;
+  const bool add_bad = any_bad != 0;
 
   sum += __shfl_xor(sum, 32);
   const float qnan = __builtin_nanf("");
@@ -571,9 +596,14 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
       const int dim = 32 * d + 8 * i + 4 * half;
       f32x4 x = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
       x *= f;
+      if (add_bad) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (lim >= bad_dim[dim + e]) x[e] = qnan;
+        for (int e = 0; e < 4; ++e) {
+          if (lim >= bad_dim[kBadPos][dim + e]) x[e] += __builtin_inff();
+          if (lim >= bad_dim[kBadNeg][dim + e]) x[e] -= __builtin_inff();
+          if (lim >= bad_dim[kBadNan][dim + e]) x[e] = qnan;
+        }
+      }
       if (p.nsplit > 1)
         *reinterpret_cast<f32x4*>(p.part_o + part_row * D + dim) = x;
       else
