@@ -314,7 +314,8 @@ tts_status tts_prefix_verify_attn(const tts_attn_desc* d, const tts_prefix_meta*
  * 0 .. itself. What is stored at tokens that a query does not see, infinities
  * and NaN included, does not reach its row; values that it sees enter as the
  * formula has them (an infinity makes the dim infinite, both signs or a NaN
- * make it NaN).
+ * make it NaN), but that an fp8 block whose K or V scale is not finite makes
+ * the rows that see it NaN.
  *   q [num_tokens][Hq][D], out [num_tokens][Hq][D]; rows behind the last
  *     sequence's are left as they are; both and the caches aligned to 16 bytes.
  *   max_seq_len: host upper bound on seq_lens, 2^31 - 2^16 at most.

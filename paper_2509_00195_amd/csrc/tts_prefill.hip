@@ -294,9 +294,9 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
       }
   };
   // fp8: the K scales times the softmax scale, and the V scales, of all of a
-  // tile's blocks. A V scale that is not finite makes every value of its block
+  // tile's blocks. A scale that is not finite makes every element of its block
   // infinite or NaN: rows that see the block are NaN, and the others must not
-  // meet it.
+  // meet it (K scales: see the softmax).
   struct Scales {
     float k __attribute__((ext_vector_type(G::blocks)));
     float v __attribute__((ext_vector_type(G::blocks)));
@@ -442,12 +442,18 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(PrefillParams p)
   auto softmax = [&](int tile, Scales& sc) {
     const int t0 = tile * G::tokens;
     if constexpr (KV == kKvFp8) {
-      // What follows takes positive scales; others are multiplied in here.
+      // What follows takes positive, finite scales; others are multiplied in
+      // here. (An infinite one would turn the negative score of codes of both
+      // signs, whose products with it have no sum, into no weight at all.)
+      constexpr int kPosFinite = 0x080 | 0x100;  // positive: subnormal, normal
       bool positive = true;
 #pragma unroll
-      for (int b = 0; b < G::blocks; ++b) positive = positive && sc.k[b] > 0.f;
+      for (int b = 0; b < G::blocks; ++b) positive = positive && __builtin_amdgcn_classf(sc.k[b], kPosFinite);
       if (!positive) {
         asm volatile("");
+#pragma unroll
+        for (int b = 0; b < G::blocks; ++b)
+          if (!(__builtin_fabsf(sc.k[b]) < __builtin_inff())) atomicMin(&bad_tok, t0 + b * kTok);
 #pragma unroll
         for (int t = 0; t < G::tokens / 32; ++t)
 #pragma unroll

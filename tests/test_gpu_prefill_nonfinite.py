@@ -56,3 +56,19 @@ def test_visible_infinities(kind, d, seqs, length, split):
         assert (f(got) == f(want)).all()
     keep = np.isfinite(want)
     assert (np.abs(got - np.where(keep, want, 0)) <= tol)[keep].all()
+
+
+@pytest.mark.parametrize("scale", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("length", [100, 2600])
+def test_fp8_scales_that_are_not_finite(scale, which, length):
+    """The rows that see the block are NaN, the others as ever."""
+    n, block = 100, length // BS - 2
+    c = Cache("fp8", 1, 128, [length], np.random.default_rng(2))
+    q, qv = queries("fp8", (n, 4, 128), np.random.default_rng(3))
+    want, tol = reference(c, 0, qv)
+    (c.ks if which == "k" else c.vs)[c.tables[0, block]] = scale
+    got, _ = _call(c, 4, [n], q)
+    first = block * BS - (length - n)
+    assert np.isnan(got[first:]).all()
+    assert (np.abs(got - want) <= tol)[:first].all()
