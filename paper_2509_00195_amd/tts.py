@@ -447,27 +447,39 @@ def make_rope(cos, sin, interleaved: bool = False) -> tts_rope_desc:
     return tts_rope_desc(2 * shape[1], 1 if interleaved else 0, shape[0], _ptr(cos), _ptr(sin))
 
 
-def _rows(x, heads: int, head_dim: int):
-    """(address, elements between tokens) of [tokens][heads][head_dim] rows whose tokens may lie apart."""
+def _rows(x, heads: int, head_dim: int, tokens: int = 0, itemsize: int = 0):
+    """(address, elements between tokens) of [tokens][heads][head_dim] rows whose tokens may lie apart; at least `tokens`
+    of them, of elements of `itemsize` bytes (0: any)."""
     if x is None:
         return None, 0
     if isinstance(x, int):
         return x, heads * head_dim
-    shape, step = x.shape, x.stride()
+    shape = x.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"expected rows of [{heads}][{head_dim}], got {tuple(shape)}")
-    if shape[0] and (step[2] != 1 or step[1] != head_dim):
+    n = shape[0]
+    if n < tokens:
+        raise ValueError(f"expected {tokens} tokens, got {n}")
+    if itemsize and x.itemsize != itemsize:
+        raise ValueError(f"expected elements of {itemsize} bytes, got {x.dtype}")
+    token, head, dim = x.stride()
+    if n and (dim != 1 or head != head_dim):
         raise ValueError("the heads of a token must be contiguous")
-    return x.data_ptr(), step[0] if shape[0] > 1 else heads * head_dim
+    return x.data_ptr(), token if n > 1 else heads * head_dim
 
 
 def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_new, v_new, block_tables,
                        max_blocks_per_seq: int, seq_lens, num_blocks: int, k_cache, v_cache, k_scale=None, v_scale=None,
                        rope: Optional[tts_rope_desc] = None, q=None, q_out=None, tok_offsets=None, positions=None,
                        stream=None):
-    """q, k_new and v_new: [tokens][heads][head_dim], possibly views of one projection's output."""
-    hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
-    (qp, qs), (kp, ks), (vp, vs) = _rows(q, hq, d), _rows(k_new, hkv, d), _rows(v_new, hkv, d)
+    """q, k_new and v_new: [tokens][heads][head_dim], possibly views of one projection's output, of num_tokens tokens at
+    least."""
+    hq, hkv, d, size = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, 4 if desc.q_dtype == TTS_F32 else 2
+    qp, qs = _rows(q, hq, d, num_tokens, size)
+    kp, ks = _rows(k_new, hkv, d, num_tokens, size)
+    vp, vs = _rows(v_new, hkv, d, num_tokens, size)
+    if q_out is not None and not isinstance(q_out, int) and q_out.nbytes < num_tokens * hq * d * size:
+        raise ValueError(f"q_out is smaller than {num_tokens} tokens of [{hq}][{d}]")
     _check(load().tts_rope_append_kv(
         C.byref(desc), C.byref(rope) if rope is not None else None, num_seqs, num_tokens, _ptr(tok_offsets),
         _ptr(positions), qp, qs, kp, ks, vp, vs, _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens), num_blocks,

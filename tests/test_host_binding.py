@@ -1,0 +1,33 @@
+"""Checks of the binding on tensors (CPU: nothing is launched)."""
+
+import pytest
+import torch
+
+from paper_2509_00195_amd import tts as T
+
+A = 1 << 20  # an address that no refused call reads
+
+
+def _append(n=4, q=None, k=None, v=None, q_out=None, kind="bf16"):
+    """A call that the library itself refuses (no tables), unless the binding does so first."""
+    wide = torch.float32 if kind == "f32" else torch.bfloat16
+    rows = lambda heads, m=n: torch.zeros((m, heads, 64), dtype=wide)  # noqa: E731
+    desc = T.make_desc(8, 2, 64, 16, "f32" if kind == "f32" else "bf16", kind)
+    T.tts_rope_append_kv(desc, 4, n, rows(2) if k is None else k, rows(2) if v is None else v, None, 4, A, 8, A, A,
+                         rope=T.tts_rope_desc(64, 0, 16, A, A), q=rows(8) if q is None else q,
+                         q_out=rows(8) if q_out is None else q_out)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mx4"])
+def test_append_refuses_tensors_of_fewer_tokens(kind):
+    wide, other = (torch.float32, torch.bfloat16) if kind == "f32" else (torch.bfloat16, torch.float32)
+    with pytest.raises(T.TTSError):
+        _append(kind=kind)
+    with pytest.raises(T.TTSError):  # more than num_tokens: padded rows
+        _append(k=torch.zeros((9, 2, 64), dtype=wide), kind=kind)
+    for name, heads in (("q", 8), ("k", 2), ("v", 2), ("q_out", 8)):
+        with pytest.raises(ValueError):
+            _append(**{name: torch.zeros((3, heads, 64), dtype=wide)}, kind=kind)
+    for name, heads in (("q", 8), ("k", 2), ("v", 2)):
+        with pytest.raises(ValueError):
+            _append(**{name: torch.zeros((4, heads, 64), dtype=other)}, kind=kind)
