@@ -463,7 +463,7 @@ def _rows(x, heads: int, head_dim: int, tokens: int = 0, itemsize: int = 0):
     if itemsize and x.itemsize != itemsize:
         raise ValueError(f"expected elements of {itemsize} bytes, got {x.dtype}")
     token, head, dim = x.stride()
-    if n and (dim != 1 or head != head_dim):
+    if n and (dim != 1 or (head != head_dim and heads > 1)):
         raise ValueError("the heads of a token must be contiguous")
     return x.data_ptr(), token if n > 1 else heads * head_dim
 

@@ -31,3 +31,13 @@ def test_append_refuses_tensors_of_fewer_tokens(kind):
     for name, heads in (("q", 8), ("k", 2), ("v", 2)):
         with pytest.raises(ValueError):
             _append(**{name: torch.zeros((4, heads, 64), dtype=other)}, kind=kind)
+
+
+def test_rows_of_one_head():
+    """The stride of a dimension of size 1 says nothing: a [1][tokens][64] projection, transposed."""
+    x = torch.zeros((1, 5, 64), dtype=torch.bfloat16).transpose(0, 1)
+    assert x.stride(1) != 64
+    assert T._rows(x, 1, 64) == (x.data_ptr(), 64)
+    y = torch.zeros((2, 5, 64), dtype=torch.bfloat16).transpose(0, 1)
+    with pytest.raises(ValueError):
+        T._rows(y, 2, 64)
