@@ -874,7 +874,7 @@ tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope,
   if ((q != nullptr) != (q_out != nullptr)) return fail(TTS_ERR_INVALID_ARG, "q and q_out go together");
   const int64_t kv_token = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
   const int64_t q_token = static_cast<int64_t>(d->num_q_heads) * d->head_dim;
-  if (k_stride < kv_token || v_stride < kv_token || (q && q_stride < q_token))
+  if ((k_new && k_stride < kv_token) || (v_new && v_stride < kv_token) || (q && q_stride < q_token))
     return fail(TTS_ERR_INVALID_ARG, "a token stride is smaller than a token");
   if (q && q == q_out && q_stride != q_token)
     return fail(TTS_ERR_INVALID_ARG, "queries are rotated in place only without gaps (q_stride)");

@@ -41,3 +41,11 @@ def test_rows_of_one_head():
     y = torch.zeros((2, 5, 64), dtype=torch.bfloat16).transpose(0, 1)
     with pytest.raises(ValueError):
         T._rows(y, 2, 64)
+
+
+def test_an_empty_append_takes_null():
+    """As the other calls do."""
+    desc = T.make_desc(8, 2, 64)
+    T.tts_append_kv(desc, 0, None, None, None, 0, None, 0, None, None)
+    T.tts_rope_append_kv(desc, 0, 0, None, None, None, 0, None, 0, None, None)
+    T.tts_rope_append_kv(desc, 3, 0, None, None, A, 4, A, 8, A, A, tok_offsets=A)
