@@ -246,6 +246,9 @@ size_t tts_prefix_decode_workspace_size(const tts_attn_desc* d, const tts_prefix
  * every seq_len is >= its value at build time (beams only appended
  * privately). The ids of the blocks in use at build time are taken from
  * the metadata; blocks appended since are read from block_tables.
+ * Infinities and NaN in the cache reach the rows of the beams (verification:
+ * the tokens) that see them and no others; rows that come out infinite or
+ * NaN are computed a second time, which is slow.
  * block_tables/seq_lens: device copies of the current tables and lengths.
  * workspace: at least tts_prefix_decode_workspace_size bytes (partial
  * softmax states; calls that overlap in time must not share one). A plan
@@ -346,7 +349,9 @@ tts_status tts_paged_prefill_attn(const tts_attn_desc* d, int32_t num_seqs, int3
  * factor that takes it to the row normalised by the sum; for fp32 caches
  * normalised, in fp32) per (beam, query head, slot) in the workspace;
  * tts_prefix_decode_merge combines each beam's states, in slot order, into
- * out. Arguments and rules are those of tts_prefix_decode_attn; the merge
+ * out. Arguments and rules are those of tts_prefix_decode_attn, but that the
+ * merge, which has no cache at hand, computes no row a second time: a value
+ * that is not finite may reach other beams' rows. The merge
  * must follow the partials call on the same workspace in stream order, with
  * the same metadata and seq_lens. */
 tts_status tts_prefix_decode_partials(const tts_attn_desc* d, const tts_prefix_meta* m, const void* q,

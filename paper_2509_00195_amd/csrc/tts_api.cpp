@@ -630,6 +630,16 @@ tts_status launch_prefix_merge(const tts_attn_desc* d, const tts_prefix_meta* m,
   mp.q_len = p.q_len;
   mp.rows_per_head = p.rows_per_head;
   mp.out_bf16 = p.out_bf16;
+  mp.q = p.q;
+  mp.k_cache = p.k_cache;
+  mp.v_cache = p.v_cache;
+  mp.k_scale = p.k_scale;
+  mp.v_scale = p.v_scale;
+  mp.block_tables = p.block_tables;
+  mp.max_blocks = p.max_blocks;
+  mp.num_blocks = p.num_blocks;
+  mp.hkv = p.hkv;
+  mp.scale_log2 = p.scale_log2;
   hipError_t e = tts::launch_merge(mp, d->head_dim, kv_kind(d), stream);
   if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("merge launch: ") + hipGetErrorString(e));
   return TTS_OK;

@@ -2180,7 +2180,114 @@ struct RowElems<64, F16> {
   E v[1];
 };
 
-template <int D, bool F16>
+// Eight elements of a (block, KV head) from element `at` on: dims of a token
+// of K, or (kValues) tokens of a dim of V.
+template <int D, int KV, bool kValues>
+__device__ __forceinline__ void eight_elements(const unsigned char* blk, int at, float (&x)[8]) {
+  if constexpr (KV == kKvF32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 t = reinterpret_cast<const f32x4*>(blk)[at / 4 + h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * h + i] = t[i];
+    }
+  } else {
+    uint4 w;
+    if constexpr (KV == kKvBf16) {
+      w = reinterpret_cast<const uint4*>(blk)[at / 8];
+    } else if constexpr (KV == kKvFp8) {
+      w = fp8x8_to_bf16x8(reinterpret_cast<const uint2*>(blk)[at / 8]);
+    } else {
+      const uint32_t codes = reinterpret_cast<const uint32_t*>(blk)[at / 8];
+      const unsigned char* scales = blk + Geo<D, KV>::code_bytes;
+      if constexpr (kValues)
+        w = mx4x8_to_bf16x8(codes, *reinterpret_cast<const uint2*>(scales + at / kTok / kMxGroup * kTok + at % kTok));
+      else
+        w = mx4x8_to_bf16x8(codes, mx_scale<0>(scales[at / kMxGroup]));
+    }
+    const uint32_t two[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __builtin_bit_cast(float, two[i] << 16);
+      x[2 * i + 1] = __builtin_bit_cast(float, two[i] & 0xFFFF0000u);
+    }
+  }
+}
+
+// Row (b, h) from its own tokens, by one wave: scores with a lane to a token,
+// the value sum with a lane to its dims (kEl from `dim` on), in fp32, 64
+// tokens at a time.
+template <int D, int KV, int kEl>
+__device__ __forceinline__ void row_alone(const MergeParams& p, int b, int h, int L, int lane, int dim, float (&x)[kEl]) {
+  using G = Geo<D, KV>;
+  typedef typename std::conditional<KV == kKvF32, f32x4, uint32_t>::type Q;  // what q is read by
+  constexpr int kQ = KV == kKvF32 ? 4 : 2;
+  const size_t blk_stride = static_cast<size_t>(p.hkv) * G::blk_bytes, head = static_cast<size_t>(h / p.g) * G::blk_bytes;
+  const unsigned char* kbase = static_cast<const unsigned char*>(p.k_cache) + head;
+  const unsigned char* vbase = static_cast<const unsigned char*>(p.v_cache) + head;
+  const int32_t* table = p.block_tables + static_cast<int64_t>(p.q_len > 1 ? b / p.q_len : b) * p.max_blocks;
+  const Q* q = static_cast<const Q*>(p.q) + (static_cast<int64_t>(b) * p.hq + h) * (D / kQ);
+  bool bad = (L + kTok - 1) / kTok > p.max_blocks;
+  float m = kNegInf, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < kEl; ++e) x[e] = 0.f;
+  for (int t0 = 0; t0 < L && !bad; t0 += 64) {
+    const int t = t0 + lane, n = L - t0 < 64 ? L - t0 : 64;
+    const int id = lane < n ? table[t / kTok] : 0;
+    bad = __builtin_amdgcn_ballot_w64(id < 0 || id >= p.num_blocks) != 0;
+    if (bad) break;
+    float s = kNegInf;
+    if (lane < n) {
+      const unsigned char* blk = kbase + id * blk_stride;
+      s = 0.f;
+#pragma unroll 8
+      for (int d = 0; d < D; d += 8) {
+        float k[8];
+        eight_elements<D, KV, false>(blk, t % kTok * D + d, k);
+#pragma unroll
+        for (int i = 0; i < 8; i += kQ) {
+          const Q w = scalar(q + (d + i) / kQ);
+          if constexpr (KV == kKvF32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s = __builtin_fmaf(k[i + j], w[j], s);
+          } else {
+            s = __builtin_fmaf(k[i], __builtin_bit_cast(float, w << 16), s);
+            s = __builtin_fmaf(k[i + 1], __builtin_bit_cast(float, w & 0xFFFF0000u), s);
+          }
+        }
+      }
+      s *= p.scale_log2 * (KV == kKvFp8 ? p.k_scale[id] : 1.f);
+    }
+    const float now = fmaxf(m, wave_max(s));
+    const float f = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - now);
+    const float w = s == kNegInf ? 0.f : __builtin_amdgcn_exp2f(s - now);
+    l = l * f + wave_sum(w);
+    m = now;
+#pragma unroll
+    for (int e = 0; e < kEl; ++e) x[e] *= f;
+    const float wv = KV == kKvFp8 && lane < n ? w * p.v_scale[id] : w;
+#pragma unroll
+    for (int k = 0; k < 64; k += 8) {
+      if (k >= n) break;  // uniform
+      const unsigned char* blk = vbase + rl(id, k) * blk_stride;
+#pragma unroll
+      for (int e = 0; e < kEl; ++e) {
+        float v[8];
+        eight_elements<D, KV, true>(blk, (dim + e) * kTok + k % kTok, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[e] = __builtin_fmaf(k + i < n ? v[i] : 0.f, rlf(wv, k + i), x[e]);
+      }
+    }
+  }
+  const float inv = bad ? __builtin_nanf("") : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < kEl; ++e) x[e] *= inv;
+}
+
+// KV: the prefix path with its caches of that type at hand (kNoCache: without).
+constexpr int kNoCache = -1;
+
+template <int D, bool F16, int KV>
 __global__ __launch_bounds__(kMergeThreads) void merge_kernel(MergeParams p) {
   using R = RowElems<D, F16>;
   constexpr int kEl = R::kEl;
@@ -2260,14 +2367,29 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(MergeParams p) {
   float* dst = static_cast<float*>(p.out) + at;
   uint16_t* half = static_cast<uint16_t*>(p.out) + at;
   const float q = __builtin_nanf("");
+#pragma unroll
+  for (int e = 0; e < kEl; ++e) acc[e] *= inv;
+  if constexpr (KV != kNoCache) {
+    // A unit's rows meet the values of each other's blocks with a probability
+    // of zero, which does not keep an infinity or NaN out: a row that is not
+    // finite may owe that to another beam's value, and is computed again by
+    // itself. (The test costs 0.05 to 0.2 us a call. 64 beams of up to 4,000
+    // tokens, 28 heads of 128: 240 to 290 us instead of 26 to 33 where one
+    // beam holds a NaN, 400 to 470 where the shared prefix does. Telling such
+    // values apart in the units' own loops spilled registers there.)
+    bool finite = true;
+#pragma unroll
+    for (int e = 0; e < kEl; ++e) finite = finite && __builtin_fabsf(acc[e]) < kInf;
+    if (__builtin_amdgcn_ballot_w64(!finite) != 0 && !nan) row_alone<D, KV>(p, b, h, L, lane, dim, acc);
+  }
   if constexpr (kEl == 2) {
-    const f32x2 x = nan ? f32x2{q, q} : f32x2{acc[0] * inv, acc[1] * inv};
+    const f32x2 x = nan ? f32x2{q, q} : f32x2{acc[0], acc[1]};
     if (p.out_bf16)
       *reinterpret_cast<uint32_t*>(half) = pack_bf16x2(x.x, x.y);
     else
       *reinterpret_cast<f32x2*>(dst) = x;
   } else {
-    const float x = nan ? q : acc[0] * inv;
+    const float x = nan ? q : acc[0];
     if (p.out_bf16)
       *half = static_cast<uint16_t>(pack_bf16x2(x, x));
     else
@@ -2324,7 +2446,7 @@ static hipError_t launch_attn_t(const AttnParams& p, int grid, hipStream_t strea
   return hipGetLastError();
 }
 
-template <int D, bool F16>
+template <int D, bool F16, int KV>
 static hipError_t launch_merge_t(MergeParams p, hipStream_t stream) {
   constexpr int kPer = kMergeThreads / 64;  // rows per workgroup
   // (Whole beams, and whole beams' virtual ones.)
@@ -2334,7 +2456,7 @@ static hipError_t launch_merge_t(MergeParams p, hipStream_t stream) {
     const int64_t n = left < most ? left : most;
     p.num_seqs = static_cast<int32_t>(n);
     const unsigned grid = static_cast<unsigned>((n * p.hq + kPer - 1) / kPer);
-    hipLaunchKernelGGL((merge_kernel<D, F16>), dim3(grid), dim3(kMergeThreads), 0, stream, p);
+    hipLaunchKernelGGL((merge_kernel<D, F16, KV>), dim3(grid), dim3(kMergeThreads), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     p.seq_lens += n / p.q_len;
@@ -2342,6 +2464,10 @@ static hipError_t launch_merge_t(MergeParams p, hipStream_t stream) {
     if (p.slot_tab) {
       p.slot_tab += n * p.slot_stride;
       p.build_len += n;
+      if (p.k_cache) {
+        p.q = static_cast<const char*>(p.q) + n * p.hq * D * (F16 ? 2 : 4);
+        p.block_tables += n / p.q_len * p.max_blocks;
+      }
     } else {
       const int64_t rows = n * p.paged_nsplit * p.hq;
       p.part_o = static_cast<const char*>(p.part_o) + rows * D * (F16 ? 2 : 4);
@@ -2351,10 +2477,20 @@ static hipError_t launch_merge_t(MergeParams p, hipStream_t stream) {
   return hipSuccess;
 }
 
+template <int D>
+static hipError_t launch_merge_d(const MergeParams& p, int kv_kind, hipStream_t stream) {
+  if (!p.k_cache)
+    return kv_kind == kKvF32 ? launch_merge_t<D, false, kNoCache>(p, stream) : launch_merge_t<D, true, kNoCache>(p, stream);
+  switch (kv_kind) {
+    case kKvF32: return launch_merge_t<D, false, kKvF32>(p, stream);
+    case kKvBf16: return launch_merge_t<D, true, kKvBf16>(p, stream);
+    case kKvFp8: return launch_merge_t<D, true, kKvFp8>(p, stream);
+    default: return launch_merge_t<D, true, kKvMx4>(p, stream);
+  }
+}
+
 hipError_t launch_merge(const MergeParams& p, int head_dim, int kv_kind, hipStream_t stream) {
-  const bool f16 = kv_kind != kKvF32;
-  if (head_dim == 128) return f16 ? launch_merge_t<128, true>(p, stream) : launch_merge_t<128, false>(p, stream);
-  return f16 ? launch_merge_t<64, true>(p, stream) : launch_merge_t<64, false>(p, stream);
+  return head_dim == 128 ? launch_merge_d<128>(p, kv_kind, stream) : launch_merge_d<64>(p, kv_kind, stream);
 }
 
 hipError_t launch_attn(const AttnParams& p, int grid, int head_dim, int kv_kind, hipStream_t stream) {

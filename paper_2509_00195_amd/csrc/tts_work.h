@@ -143,6 +143,18 @@ struct MergeParams {
   int32_t rows_per_head;
   int32_t paged_nsplit;
   int32_t q_len;  // as in AttnParams (lengths of virtual beams)
+  // Prefix path: what a row is computed from when it is computed again by
+  // itself; k_cache is null in calls that have no caches.
+  const void* q;
+  const void* k_cache;
+  const void* v_cache;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* block_tables;
+  int32_t max_blocks;
+  int32_t num_blocks;
+  int32_t hkv;
+  float scale_log2;
 };
 
 }  // namespace tts
