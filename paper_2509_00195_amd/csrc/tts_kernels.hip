@@ -200,7 +200,10 @@ __device__ __forceinline__ void store_partial_row(void* part_o, float* part_ml, 
 #pragma unroll
       for (int j = 0; j < 4; ++j) amax = fmaxf(amax, __builtin_fabsf(o[e][j]));
     amax = row16_max(amax);
-    const int e2 = (amax > 0.f && amax <= 3.0e38f) ? __builtin_amdgcn_frexp_expf(amax) : 0;
+    // (An infinite element stays one; the others are then scaled by the sum,
+    // so that they are of the values' size.)
+    const float top = amax <= 3.0e38f ? amax : l;
+    const int e2 = top > 0.f ? __builtin_amdgcn_frexp_expf(top) : 0;
     uint32_t w[kEl / 2];
 #pragma unroll
     for (int e = 0; e < kEl / 4; ++e)

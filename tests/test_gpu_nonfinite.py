@@ -137,3 +137,24 @@ def test_nan_queries_in_verification(kind):
         qb = np.where(nan[b][..., None], 0.0, qv[b])
         want, tol = reference(c, b, qb)
         assert (np.abs(got[b] - want) <= tol)[~nan[b]].all(), b
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hkv", [(6, 2), (36, 2)])
+@pytest.mark.parametrize("gain", [1.0, 2.5, 6.0])
+def test_infinite_values_in_split_calls(kind, hq, hkv, gain):
+    """An infinite value makes its dim infinite and leaves the others, in rows of small and large sums."""
+    make = lambda: Cache(kind, hkv, 64, [40, 700], np.random.default_rng(10), cols=256, gain=gain)  # noqa: E731
+    c, clean = make(), make()
+    for b, token in ((0, 3), (1, 650)):
+        c.v[c.tables[b, token // BS], 1, 9, token % BS] = np.inf if kind == "f32" else 0x7F80
+    q, qv = queries(kind, (2, hq, 64), np.random.default_rng(11), gain)
+    got = _paged(c, q, torch.zeros((2, hq, 64), device=DEV), hq, 4096)
+    for b in range(2):
+        want, tol = reference(clean, b, qv[b][None])
+        # (a probability below fp32's least normal, 2^-126 of the largest, may be held as 0, and 0 x inf is NaN)
+        score = clean.dense(b)[0][1] @ qv[b, hq // 2:].T / 8.0
+        seen = score[3 if b == 0 else 650] - score.max(0) > -125 * np.log(2)
+        assert np.isposinf(got[b, hq // 2:, 9][seen]).all() and not np.isfinite(got[b, hq // 2:, 9]).any()
+        got[b, hq // 2:, 9] = want[0, hq // 2:, 9]
+        assert (np.abs(got[b] - want[0]) <= tol[0]).all()
