@@ -84,7 +84,14 @@ typedef enum { TTS_F32 = 0, TTS_BF16 = 1, TTS_FP8_E4M3 = 2, TTS_MXFP4 = 3 } tts_
 /* Attention shape. Supported: Hq % Hkv == 0, head_dim 64 or 128,
  * block_size 16; (q, kv) dtypes (F32, F32), (BF16, BF16), (BF16, FP8_E4M3),
  * (BF16, MXFP4); out_dtype F32 or BF16 (rounded once from fp32). scale <= 0
- * selects 1/sqrt(head_dim). */
+ * selects 1/sqrt(head_dim).
+ * Precision: scores, softmax statistics and sums are fp32. But for F32 caches
+ * the probabilities (FP8_E4M3: times the V scale) are rounded to bf16, by 2^-8
+ * of each at most, for the value product, and states that are joined are
+ * stored in fp16 (scaled to the row's largest element); the prefill joins fp32
+ * states. The sum is that of the rounded probabilities in
+ * the prefill (but for FP8_E4M3) and over MXFP4 caches, of the unrounded ones
+ * elsewhere. */
 typedef struct {
   int32_t num_q_heads;
   int32_t num_kv_heads;
@@ -311,8 +318,8 @@ tts_status tts_prefix_verify_attn(const tts_attn_desc* d, const tts_prefix_meta*
  * Causal attention of a chunk of every sequence's last tokens over its paged
  * cache, of any length: the prompts and reasoning steps that a verifier reads
  * (its requests are prefills, Sec. 2.2 and 4.3) and a generator's prompts.
- * tok_offsets, num_tokens and seq_lens as for tts_rope_append_kv (which has
- * stored the chunk's keys and values): query i of sequence b, row
+ * tok_offsets (not NULL here), num_tokens and seq_lens as for
+ * tts_rope_append_kv (which has stored the chunk's keys and values): query i of sequence b, row
  * tok_offsets[b] + i, is token seq_lens[b] - n_b + i and attends to the tokens
  * 0 .. itself. What is stored at tokens that a query does not see, infinities
  * and NaN included, does not reach its row; values that it sees enter as the
@@ -440,8 +447,8 @@ tts_status tts_rope_tables(int32_t rot_dim, double theta, int32_t max_pos, float
  * token per sequence it is the same.
  * A sequence with seq_len <= 0 is idle: none of its rows is read or written.
  * Device-side errors: a sequence shorter than its new tokens stores nothing
- * and its queries are NaN; a position outside [0, max_pos) makes its token's
- * queries NaN and stores nothing of it; a block index past the table row or a
+ * and its queries are NaN; where rot_dim > 0, a position outside [0, max_pos)
+ * makes its token's queries NaN and stores nothing of it; a block index past the table row or a
  * block id outside [0, num_blocks) stores nothing. As for tts_append_kv, the
  * blocks that new tokens go to belong to one sequence each. The caches are
  * aligned to 16 bytes. Rows of 16-byte alignment (and rot_dim a multiple of

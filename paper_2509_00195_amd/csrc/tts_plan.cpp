@@ -49,10 +49,13 @@ namespace {
 //   5.3 us + (0.12 + 0.029 tiles) us. fp8: 5.3 us + (0.175 + 0.0325 tiles)
 //   us per block, in both forms.
 // * 4-bit: as fp8, with 0.25 us per narrow block and (0.10 + 0.06 tiles) us
-//   per wide one, whose conversions every row tile pays for again. Whole calls
-//   against the fp8 terms: 256 beams over four trees 37.8 us instead of 42.3,
-//   16 beams 14.7 instead of 15.7, 64 beams 25.8 and 22.1 instead of 26.6 and
-//   23.0, verification of four tokens 22.6 instead of 21.8, D 64 the same.
+//   per wide one. Fitted to the times of whole calls (60 sets of terms over
+//   seven shapes), not to single units: a wide unit converts each block once,
+//   when it is staged, as an fp8 one does, so that the doubled term per tile
+//   stands for no work of its own. Whole calls against the fp8 terms: 256
+//   beams over four trees 37.8 us instead of 42.3, 16 beams 14.7 instead of
+//   15.7, 64 beams 25.8 and 22.1 instead of 26.6 and 23.0, but verification of
+//   four tokens 22.6 instead of 21.8; D 64 the same.
 // * fp32 (16 rows to a wave group, four groups of two waves above 32 rows):
 //   the larger of 0.26 us per 8 KiB of blocks and of the matrix cores' time,
 //   0.24 us per block and row tile (D 128; four times the largest tile's
