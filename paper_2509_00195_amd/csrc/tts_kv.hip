@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kKvThreads) void append_kernel(AppendParams p) {
 // dim-major V row) has one writer and no atomics. Parts: the K rows of
 // `heads_per` heads, the V rows of as many, kRopeTasks pieces of the query
 // rows. Bound by memory for chunks (eight of 256 to 2,048 tokens, 28 over 4 heads of
-// 128, 4-bit cache: 30.2 us, the time of a copy of as many bytes), by the round
+// 128, 4-bit cache: 30.9 us, a copy of as many bytes 30.2), by the round
 // trips (offsets, length, table and table rows, token) for a step's single
 // tokens (16 sequences 4.9 us; 512 over an fp8 cache, whose earlier codes may
 // have to be read and encoded again, 10.1 us).

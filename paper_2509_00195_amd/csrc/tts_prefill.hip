@@ -30,9 +30,9 @@
 //
 // Bound by the issue of matrix and vector instructions, which overlap only in
 // part between the two waves of a SIMD: one sequence of 16,384 tokens, 28 over
-// 4 heads of 128, takes 1.95 ms (985 TFLOP/s, 0.72 of a large bf16 matrix
-// product here); eight ragged prompts of 200 to 2048 110 us; chunks over 8,000
-// to 16,000 tokens of an fp8 cache 167 us. Tried: eight waves in two groups
+// 4 heads of 128, takes 1.98 ms (972 TFLOP/s, 0.71 of a large bf16 matrix
+// product here; cards differ by 5%); eight ragged prompts of 200 to 2048 111
+// us; chunks over 8,000 to 16,000 tokens of an fp8 cache 166 us. Tried: eight waves in two groups
 // that take turns at the matrix cores (4% faster at 16,384 tokens, fp8 chunks
 // 264 us, D 64 98 instead of 78); the exponentials of one half of a tile
 // between the products of the other (2.10 ms); four or eight LDS reads ahead
