@@ -468,6 +468,12 @@ def _rows(x, heads: int, head_dim: int, tokens: int = 0, itemsize: int = 0):
     return x.data_ptr(), token if n > 1 else heads * head_dim
 
 
+def _holds(x, nbytes: int, name: str) -> None:
+    """Refuses a tensor of fewer bytes than a call reads or writes of it."""
+    if x is not None and not isinstance(x, int) and x.nbytes < nbytes:
+        raise ValueError(f"{name} holds {x.nbytes} bytes, the call takes {nbytes}")
+
+
 def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_new, v_new, block_tables,
                        max_blocks_per_seq: int, seq_lens, num_blocks: int, k_cache, v_cache, k_scale=None, v_scale=None,
                        rope: Optional[tts_rope_desc] = None, q=None, q_out=None, tok_offsets=None, positions=None,
@@ -478,8 +484,7 @@ def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_ne
     qp, qs = _rows(q, hq, d, num_tokens, size)
     kp, ks = _rows(k_new, hkv, d, num_tokens, size)
     vp, vs = _rows(v_new, hkv, d, num_tokens, size)
-    if q_out is not None and not isinstance(q_out, int) and q_out.nbytes < num_tokens * hq * d * size:
-        raise ValueError(f"q_out is smaller than {num_tokens} tokens of [{hq}][{d}]")
+    _holds(q_out, num_tokens * hq * d * size, "q_out")
     _check(load().tts_rope_append_kv(
         C.byref(desc), C.byref(rope) if rope is not None else None, num_seqs, num_tokens, _ptr(tok_offsets),
         _ptr(positions), qp, qs, kp, ks, vp, vs, _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens), num_blocks,
@@ -493,6 +498,9 @@ def tts_paged_prefill_workspace_size(desc: tts_attn_desc, num_seqs: int, num_tok
 def tts_paged_prefill_attn(desc: tts_attn_desc, num_seqs: int, num_tokens: int, tok_offsets, q, k_cache, v_cache,
                            k_scale, v_scale, block_tables, max_blocks_per_seq: int, seq_lens, max_seq_len: int,
                            num_blocks: int, out, workspace, workspace_bytes: int, stream=None):
+    elems = num_tokens * desc.num_q_heads * desc.head_dim
+    _holds(q, elems * (4 if desc.q_dtype == TTS_F32 else 2), "q")
+    _holds(out, elems * (4 if desc.out_dtype == TTS_F32 else 2), "out")
     _check(load().tts_paged_prefill_attn(
         C.byref(desc), num_seqs, num_tokens, _ptr(tok_offsets), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
         _ptr(v_scale), _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens), max_seq_len, num_blocks, _ptr(out),

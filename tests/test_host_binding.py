@@ -49,3 +49,23 @@ def test_an_empty_append_takes_null():
     T.tts_append_kv(desc, 0, None, None, None, 0, None, 0, None, None)
     T.tts_rope_append_kv(desc, 0, 0, None, None, None, 0, None, 0, None, None)
     T.tts_rope_append_kv(desc, 3, 0, None, None, A, 4, A, 8, A, A, tok_offsets=A)
+
+
+@pytest.mark.parametrize("kind,out_t", [("f32", "f32"), ("bf16", "f32"), ("fp8", "bf16")])
+def test_prefill_refuses_tensors_of_fewer_tokens(kind, out_t):
+    desc = T.make_desc(8, 2, 64, 16, "f32" if kind == "f32" else "bf16", kind, out_t)
+    wide = torch.float32 if kind == "f32" else torch.bfloat16
+    out = torch.float32 if out_t == "f32" else torch.bfloat16
+    scale = A if kind == "fp8" else None
+
+    def call(nq, no):
+        """The library itself refuses the call (no tables)."""
+        T.tts_paged_prefill_attn(desc, 2, 40, A, torch.zeros((nq, 8, 64), dtype=wide), A, A, scale, scale, None, 64, A, 1000, 200,
+                                 torch.zeros((no, 8, 64), dtype=out), A, 1 << 40)
+
+    for nq, no in ((40, 40), (45, 41)):
+        with pytest.raises(T.TTSError):
+            call(nq, no)
+    for nq, no in ((39, 40), (40, 39)):
+        with pytest.raises(ValueError):
+            call(nq, no)
