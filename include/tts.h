@@ -461,6 +461,29 @@ tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope,
                               int32_t num_blocks, void* q_out, void* k_cache, void* v_cache, float* k_scale,
                               float* v_scale, hipStream_t stream);
 
+/* Norms of the heads before the rotation: every query and key head's row x is
+ * replaced by
+ *   x[i] * r * weight[i],  r = 1 / sqrt(mean of x^2 + eps),
+ * mean and root in 64 bits, r rounded to fp32 and each product too. */
+typedef struct {
+  float eps;            /* finite, >= 0 (0: a head of zeros becomes NaN) */
+  const void* q_weight; /* device, [head_dim] in q's type; NULL: ones */
+  const void* k_weight;
+} tts_head_norm_desc;
+
+/* tts_rope_append_kv with head norms: queries and keys are normalised, rotated
+ * and stored in one pass; values are stored as they are. Arguments, rules and
+ * errors are those of tts_rope_append_kv, but that rope NULL (norms without a
+ * rotation; positions is NULL then) takes queries too. norm is not NULL. An
+ * infinity in a head makes its finite elements 0 and itself NaN, a NaN makes
+ * the head NaN, as the formula has it. */
+tts_status tts_norm_rope_append_kv(const tts_attn_desc* d, const tts_head_norm_desc* norm, const tts_rope_desc* rope,
+                                   int32_t num_seqs, int32_t num_tokens, const int32_t* tok_offsets,
+                                   const int32_t* positions, const void* q, int64_t q_stride, const void* k_new,
+                                   int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* block_tables,
+                                   int32_t max_blocks_per_seq, const int32_t* seq_lens, int32_t num_blocks, void* q_out,
+                                   void* k_cache, void* v_cache, float* k_scale, float* v_scale, hipStream_t stream);
+
 /* Copy whole blocks: for each i < num_pairs, K and V of every KV head of
  * block pairs[2i] into block pairs[2i + 1] (and the fp8 scales). pairs is a
  * device int32 array. Pairs naming a block outside [0, num_blocks), or a
@@ -508,6 +531,73 @@ tts_status tts_fork_tables(int32_t num_parents, const int32_t* parent_tables, in
 tts_status tts_truncated_lengths(int32_t num_children, const int32_t* child_parent, const int32_t* parent_lens,
                                  const int32_t* parent_spec, int32_t num_parents, double ratio, double sigma,
                                  const double* z, int32_t* child_lens);
+
+/* ---- A layer's products and norm --------------------------------------------
+ *
+ * What stands before and behind the cached attention in every decoder layer
+ * whose decode step and prefill the library serves (Sec. 2.2, 3.2.3): the norm
+ * of the hidden states, the projections, the feed-forward block. Rows are
+ * tokens: one beam's, a step's, a verification's or a prefill's. Rows lie
+ * x_stride (w_stride, ...) elements apart, at least as many as a row has, and
+ * start at any multiple of an element; rows of x and of the weights that all
+ * start at multiples of 16 bytes are fastest. A row of the output depends on
+ * the same row of x alone, whatever the others hold. */
+
+typedef enum { TTS_ACT_NONE = 0, TTS_ACT_RELU = 1, TTS_ACT_SILU = 2, TTS_ACT_GELU = 3, TTS_ACT_GELU_TANH = 4 } tts_act;
+
+/* SiLU: y / (1 + exp(-y)); GELU: y Phi(y), Phi the normal distribution's
+ * integral; its tanh form: y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) / 2. */
+typedef struct {
+  int32_t in_features;  /* K, 1 .. 2^28 */
+  int32_t out_features; /* N, 1 .. 2^26 */
+  tts_dtype dtype;      /* x, weights, biases: F32 or BF16 */
+  tts_dtype out_dtype;  /* out, residual: F32 or BF16, whatever dtype is */
+  tts_act act;
+} tts_linear_desc;
+
+/* Workspace bytes needed by tts_linear and tts_gated_linear; they suffice for
+ * every smaller num_rows too. */
+size_t tts_linear_workspace_size(const tts_linear_desc* d, int32_t num_rows);
+size_t tts_gated_linear_workspace_size(const tts_linear_desc* d, int32_t num_rows);
+
+/* out[m][n] = act(sum_k x[m][k] w[n][k] + bias[n]) + residual[m][n], sums in
+ * fp32, rounded once.
+ *   x [num_rows][K], w [N][K], bias [N] or NULL, residual [num_rows][N] or
+ *   NULL, out [num_rows][N]. out may be the residual itself (same stride), and
+ *   otherwise overlaps no input.
+ *   workspace: at least tts_linear_workspace_size bytes, aligned to 16 (a call
+ *   that needs more than it is given is TTS_ERR_WORKSPACE); NULL allowed when
+ *   that size is 0. Calls that overlap in time must not share one.
+ * The order of the sums depends on the sizes and on the rows' alignment, not
+ * on the values, and a call repeats itself bit for bit. Outputs whose tiles
+ * pass one launch (2^32 threads) are TTS_ERR_UNSUPPORTED. */
+tts_status tts_linear(const tts_linear_desc* d, int32_t num_rows, const void* x, int64_t x_stride, const void* w,
+                      int64_t w_stride, const void* bias, const void* residual, int64_t residual_stride, void* out,
+                      int64_t out_stride, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The first half of a gated feed-forward block, both projections read in one
+ * pass over x, nothing of them stored:
+ *   out[m][n] = act(sum_k x[m][k] w_gate[n][k] + bias_gate[n])
+ *               * (sum_k x[m][k] w_up[n][k] + bias_up[n]).
+ * w_gate and w_up [N][K], w_stride elements between the rows of each (they may
+ * be the halves of one tensor); each bias may be NULL. Otherwise as tts_linear. */
+tts_status tts_gated_linear(const tts_linear_desc* d, int32_t num_rows, const void* x, int64_t x_stride,
+                            const void* w_gate, const void* w_up, int64_t w_stride, const void* bias_gate,
+                            const void* bias_up, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream);
+
+typedef struct {
+  int32_t row_len;     /* >= 1 */
+  tts_dtype dtype;     /* x, weight: F32 or BF16 */
+  tts_dtype out_dtype; /* F32 or BF16 */
+  float eps;           /* finite, >= 0 (0: a row of zeros becomes NaN) */
+} tts_norm_desc;
+
+/* out[m][i] = x[m][i] / sqrt(mean of x[m]^2 + eps) * weight[i], in fp32,
+ * rounded once. x, out [num_rows][row_len]; weight [row_len] or NULL (ones).
+ * out may be x itself (same type and stride), and otherwise does not overlap it. */
+tts_status tts_rms_norm(const tts_norm_desc* d, int32_t num_rows, const void* x, int64_t x_stride, const void* weight,
+                        void* out, int64_t out_stride, hipStream_t stream);
 
 /* ---- Roofline-guided KV allocation (Sec. 4.3) -------------------------------
  *

@@ -12,6 +12,9 @@ from .tts import (  # noqa: F401
     PrefixMeta,
     load,
     make_desc,
+    make_head_norm,
+    make_linear,
+    make_norm,
     make_rope,
     tts_append_kv,
     tts_build_prefix_meta,
@@ -19,9 +22,15 @@ from .tts import (  # noqa: F401
     tts_copy_blocks,
     tts_fork_prefix_meta,
     tts_fork_tables,
+    tts_gated_linear,
+    tts_gated_linear_workspace_size,
     tts_kv_alloc_search,
     tts_kv_alloc_time,
+    tts_linear,
+    tts_linear_workspace_size,
+    tts_norm_rope_append_kv,
     tts_prefix_schedule,
+    tts_rms_norm,
     tts_truncated_lengths,
     tts_prefix_verify_attn,
     tts_paged_decode_attn,

@@ -31,8 +31,9 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{os.path.join(ROOT, 'include')}", f"
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 
-SOURCES_HIP = ["tts_kernels.hip", "tts_kv.hip", "tts_prefill.hip"]
-SOURCES_HOST = ["tts_meta.cpp", "tts_plan.cpp", "tts_alloc.cpp", "tts_sched.cpp", "tts_api.cpp"]
+SOURCES_HIP = ["tts_kernels.hip", "tts_kv.hip", "tts_prefill.hip", "tts_linear.hip"]
+SOURCES_HOST = ["tts_meta.cpp", "tts_plan.cpp", "tts_alloc.cpp", "tts_sched.cpp", "tts_linear.cpp",
+                "tts_api.cpp"]
 
 
 def _run(cmd):

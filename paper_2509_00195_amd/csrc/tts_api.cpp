@@ -12,6 +12,7 @@
 
 #include "tts.h"
 #include "tts_kv.h"
+#include "tts_linear.h"
 #include "tts_meta.h"
 #include "tts_prefill.h"
 #include "tts_work.h"
@@ -20,7 +21,9 @@ namespace tts {
 hipError_t launch_attn(const AttnParams& p, int grid, int head_dim, int kv_kind, hipStream_t stream);
 hipError_t launch_merge(const MergeParams& p, int head_dim, int kv_kind, hipStream_t stream);
 hipError_t scratch_buffer(void** ptr, size_t* bytes);
-hipError_t launch_rope_append(RopeParams p, int kv_kind, hipStream_t stream);
+hipError_t launch_rope_append(RopeParams p, int kv_kind, bool norm, hipStream_t stream);
+hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, bool gated, bool aligned, hipStream_t stream);
+hipError_t launch_rms(const RmsParams& p, hipStream_t stream);
 hipError_t launch_prefill(const PrefillParams& p, int head_dim, int kv_kind, hipStream_t stream);
 hipError_t launch_append(const void* k_new, const void* v_new, const int32_t* block_tables, const int32_t* seq_lens,
                          void* k_cache, void* v_cache, float* k_scale, float* v_scale, int num_seqs, int max_blocks,
@@ -78,6 +81,13 @@ constexpr int64_t kMx4Units = 512;
 constexpr int32_t kMaxSeqLen = 0x7FFF0000;
 // Query heads of a rotating append: the parts of its grid stay below 65,536.
 constexpr int32_t kMaxRopeHeads = 8192;
+// Products: bytes of a row and 128-byte chunks stay inside int32, tiles of 512
+// threads inside one launch.
+constexpr int32_t kMaxInFeatures = 1 << 28;
+constexpr int32_t kMaxOutFeatures = 1 << 26;
+constexpr int64_t kMaxStride = int64_t{1} << 31;
+constexpr int64_t kMaxTileStride = int64_t{1} << 22;  // bytes; 256 rows of it and one more stay below 2^31
+constexpr int64_t kMaxLinearGroups = (int64_t{1} << 32) / 512 - 1;
 
 tts_status check_desc(const tts_attn_desc* d) {
   if (!d) return fail(TTS_ERR_INVALID_ARG, "desc is NULL");
@@ -860,12 +870,13 @@ tts_status tts_append_kv(const tts_attn_desc* d, int32_t num_seqs, const void* k
   return ok();
 }
 
-tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope, int32_t num_seqs, int32_t num_tokens,
-                              const int32_t* tok_offsets, const int32_t* positions, const void* q, int64_t q_stride,
-                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
-                              const int32_t* block_tables, int32_t max_blocks_per_seq, const int32_t* seq_lens,
-                              int32_t num_blocks, void* q_out, void* k_cache, void* v_cache, float* k_scale,
-                              float* v_scale, hipStream_t stream) {
+// tts_rope_append_kv, and with head norms (norm not NULL) tts_norm_rope_append_kv.
+static tts_status rope_append(const tts_attn_desc* d, const tts_head_norm_desc* norm, const tts_rope_desc* rope,
+                              int32_t num_seqs, int32_t num_tokens, const int32_t* tok_offsets,
+                              const int32_t* positions, const void* q, int64_t q_stride, const void* k_new,
+                              int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* block_tables,
+                              int32_t max_blocks_per_seq, const int32_t* seq_lens, int32_t num_blocks, void* q_out,
+                              void* k_cache, void* v_cache, float* k_scale, float* v_scale, hipStream_t stream) {
   tts_status s = check_desc(d);
   if (s != TTS_OK) return s;
   if ((s = check_scales(d, k_scale, v_scale)) != TTS_OK) return s;
@@ -882,7 +893,12 @@ tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope,
       return fail(TTS_ERR_INVALID_ARG, "interleaved must be 0 or 1");
   }
   const bool turned = rope && rope->rot_dim > 0;
-  if (!rope && (q || q_out || positions))
+  if (norm && !(norm->eps >= 0 && std::isfinite(norm->eps)))
+    return fail(TTS_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  const uintptr_t elem = d->q_dtype == TTS_F32 ? 4 : 2;
+  if (norm && (reinterpret_cast<uintptr_t>(norm->q_weight) % elem != 0 || reinterpret_cast<uintptr_t>(norm->k_weight) % elem != 0))
+    return fail(TTS_ERR_INVALID_ARG, "head norm weights must be aligned to an element");
+  if (!rope && (positions || (!norm && (q || q_out))))
     return fail(TTS_ERR_INVALID_ARG, "queries and positions need a rotation (rope is NULL)");
   if ((q != nullptr) != (q_out != nullptr)) return fail(TTS_ERR_INVALID_ARG, "q and q_out go together");
   const int64_t kv_token = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
@@ -927,8 +943,162 @@ tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope,
     p.cos = rope->cos;
     p.sin = rope->sin;
   }
-  const hipError_t e = tts::launch_rope_append(p, kv_kind(d), stream);
+  if (norm) {
+    p.q_weight = norm->q_weight;
+    p.k_weight = norm->k_weight;
+    p.eps = norm->eps;
+  }
+  const hipError_t e = tts::launch_rope_append(p, kv_kind(d), norm != nullptr, stream);
   if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("append launch: ") + hipGetErrorString(e));
+  return ok();
+}
+
+tts_status tts_rope_append_kv(const tts_attn_desc* d, const tts_rope_desc* rope, int32_t num_seqs, int32_t num_tokens,
+                              const int32_t* tok_offsets, const int32_t* positions, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                              const int32_t* block_tables, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                              int32_t num_blocks, void* q_out, void* k_cache, void* v_cache, float* k_scale,
+                              float* v_scale, hipStream_t stream) {
+  return rope_append(d, nullptr, rope, num_seqs, num_tokens, tok_offsets, positions, q, q_stride, k_new, k_stride, v_new,
+                     v_stride, block_tables, max_blocks_per_seq, seq_lens, num_blocks, q_out, k_cache, v_cache, k_scale,
+                     v_scale, stream);
+}
+
+tts_status tts_norm_rope_append_kv(const tts_attn_desc* d, const tts_head_norm_desc* norm, const tts_rope_desc* rope,
+                                   int32_t num_seqs, int32_t num_tokens, const int32_t* tok_offsets,
+                                   const int32_t* positions, const void* q, int64_t q_stride, const void* k_new,
+                                   int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* block_tables,
+                                   int32_t max_blocks_per_seq, const int32_t* seq_lens, int32_t num_blocks, void* q_out,
+                                   void* k_cache, void* v_cache, float* k_scale, float* v_scale, hipStream_t stream) {
+  if (!norm) return fail(TTS_ERR_INVALID_ARG, "norm is NULL");
+  return rope_append(d, norm, rope, num_seqs, num_tokens, tok_offsets, positions, q, q_stride, k_new, k_stride, v_new,
+                     v_stride, block_tables, max_blocks_per_seq, seq_lens, num_blocks, q_out, k_cache, v_cache, k_scale,
+                     v_scale, stream);
+}
+
+static tts_status check_type(tts_dtype in, tts_dtype out) {
+  if ((in != TTS_F32 && in != TTS_BF16) || (out != TTS_F32 && out != TTS_BF16))
+    return fail(TTS_ERR_UNSUPPORTED, "types must be F32 or BF16");
+  return TTS_OK;
+}
+
+static tts_status check_linear(const tts_linear_desc* d) {
+  if (!d) return fail(TTS_ERR_INVALID_ARG, "desc is NULL");
+  if (d->in_features < 1 || d->out_features < 1) return fail(TTS_ERR_INVALID_ARG, "features must be at least 1");
+  if (d->act < TTS_ACT_NONE || d->act > TTS_ACT_GELU_TANH) return fail(TTS_ERR_INVALID_ARG, "unknown activation");
+  if (d->in_features > kMaxInFeatures || d->out_features > kMaxOutFeatures)
+    return fail(TTS_ERR_UNSUPPORTED, "more than 2^28 input or 2^26 output features");
+  return check_type(d->dtype, d->out_dtype);
+}
+
+static size_t linear_size(const tts_linear_desc* d, int32_t num_rows, bool gated) {
+  if (check_linear(d) != TTS_OK || num_rows <= 0) return 0;
+  const bool f32 = d->dtype == TTS_F32;
+  return tts::linear_workspace(num_rows, d->out_features, d->in_features * (f32 ? 4 : 2), f32, gated);
+}
+
+size_t tts_linear_workspace_size(const tts_linear_desc* d, int32_t num_rows) { return linear_size(d, num_rows, false); }
+
+size_t tts_gated_linear_workspace_size(const tts_linear_desc* d, int32_t num_rows) {
+  return linear_size(d, num_rows, true);
+}
+
+// Both products; w1 NULL: tts_linear.
+static tts_status linear(const tts_linear_desc* d, int32_t num_rows, const void* x, int64_t x_stride, const void* w0,
+                         const void* w1, int64_t w_stride, const void* b0, const void* b1, const void* residual,
+                         int64_t residual_stride, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                         bool gated, hipStream_t stream) {
+  const tts_status s = check_linear(d);
+  if (s != TTS_OK) return s;
+  if (num_rows < 0) return fail(TTS_ERR_INVALID_ARG, "negative num_rows");
+  if (num_rows == 0) return ok();
+  if (!x || !w0 || (gated && !w1) || !out) return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
+  if (x_stride < d->in_features || w_stride < d->in_features || out_stride < d->out_features ||
+      (residual && residual_stride < d->out_features))
+    return fail(TTS_ERR_INVALID_ARG, "a row stride is smaller than a row");
+  if (residual == out && residual_stride != out_stride)
+    return fail(TTS_ERR_INVALID_ARG, "a residual is added in place only at the output's own stride");
+  const bool f32 = d->dtype == TTS_F32;
+  const int elem = f32 ? 4 : 2, out_elem = d->out_dtype == TTS_F32 ? 4 : 2;
+  const auto at = [](const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; };
+  if (!at(x, elem) || !at(w0, elem) || !at(w1, elem) || !at(b0, elem) || !at(b1, elem) || !at(out, out_elem) ||
+      !at(residual, out_elem))
+    return fail(TTS_ERR_INVALID_ARG, "pointers must be aligned to an element");
+  if (x_stride > kMaxStride || w_stride > kMaxStride || out_stride > kMaxStride || (residual && residual_stride > kMaxStride))
+    return fail(TTS_ERR_UNSUPPORTED, "a row stride of more than 2^31 elements");
+  tts::LinearParams p{};
+  p.x = x;
+  p.w[0] = w0;
+  p.w[1] = w1;
+  p.bias[0] = b0;
+  p.bias[1] = b1;
+  p.residual = residual;
+  p.out = out;
+  p.part = static_cast<float*>(workspace);
+  p.x_stride = x_stride * elem;
+  p.w_stride = w_stride * elem;
+  p.residual_stride = residual_stride;
+  p.out_stride = out_stride;
+  p.rows = num_rows;
+  p.n = d->out_features;
+  p.k_bytes = d->in_features * elem;
+  p.act = d->act;
+  p.in_bf16 = !f32;
+  p.out_bf16 = d->out_dtype == TTS_BF16;
+  // Loads into LDS take 16 bytes from a multiple of 16, at 32-bit offsets into a tile's rows.
+  const bool aligned = at(x, 16) && at(w0, 16) && at(w1, 16) && p.x_stride % 16 == 0 && p.w_stride % 16 == 0 &&
+                       p.k_bytes % 16 == 0 && p.x_stride < kMaxTileStride && p.w_stride < kMaxTileStride;
+  const tts::LinearPlan plan = tts::linear_plan(num_rows, p.n, p.k_bytes, f32, gated, aligned);
+  if (plan.groups > kMaxLinearGroups) return fail(TTS_ERR_UNSUPPORTED, "more tiles than one launch takes");
+  if (plan.workspace > 0) {
+    if (!workspace || workspace_bytes < plan.workspace)
+      return fail(TTS_ERR_WORKSPACE, "workspace too small: need " + std::to_string(plan.workspace) + " bytes");
+    if (!at(workspace, 16)) return fail(TTS_ERR_INVALID_ARG, "workspace must be aligned to 16 bytes");
+  }
+  const hipError_t e = tts::launch_linear(p, plan, gated, aligned, stream);
+  if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("linear launch: ") + hipGetErrorString(e));
+  return ok();
+}
+
+tts_status tts_linear(const tts_linear_desc* d, int32_t num_rows, const void* x, int64_t x_stride, const void* w,
+                      int64_t w_stride, const void* bias, const void* residual, int64_t residual_stride, void* out,
+                      int64_t out_stride, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return linear(d, num_rows, x, x_stride, w, nullptr, w_stride, bias, nullptr, residual, residual_stride, out, out_stride,
+                workspace, workspace_bytes, false, stream);
+}
+
+tts_status tts_gated_linear(const tts_linear_desc* d, int32_t num_rows, const void* x, int64_t x_stride,
+                            const void* w_gate, const void* w_up, int64_t w_stride, const void* bias_gate,
+                            const void* bias_up, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream) {
+  return linear(d, num_rows, x, x_stride, w_gate, w_up, w_stride, bias_gate, bias_up, nullptr, 0, out, out_stride, workspace,
+                workspace_bytes, true, stream);
+}
+
+tts_status tts_rms_norm(const tts_norm_desc* d, int32_t num_rows, const void* x, int64_t x_stride, const void* weight,
+                        void* out, int64_t out_stride, hipStream_t stream) {
+  if (!d) return fail(TTS_ERR_INVALID_ARG, "desc is NULL");
+  if (d->row_len < 1) return fail(TTS_ERR_INVALID_ARG, "row_len must be at least 1");
+  if (!(d->eps >= 0 && std::isfinite(d->eps))) return fail(TTS_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  const tts_status s = check_type(d->dtype, d->out_dtype);
+  if (s != TTS_OK) return s;
+  if (num_rows < 0) return fail(TTS_ERR_INVALID_ARG, "negative num_rows");
+  if (num_rows == 0) return ok();
+  if (!x || !out) return fail(TTS_ERR_INVALID_ARG, "NULL device pointer");
+  if (x_stride < d->row_len || out_stride < d->row_len)
+    return fail(TTS_ERR_INVALID_ARG, "a row stride is smaller than a row");
+  if (x == out && (x_stride != out_stride || d->dtype != d->out_dtype))
+    return fail(TTS_ERR_INVALID_ARG, "rows are normalised in place only at one stride and type");
+  const int elem = d->dtype == TTS_F32 ? 4 : 2, out_elem = d->out_dtype == TTS_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(x) % elem != 0 || reinterpret_cast<uintptr_t>(weight) % elem != 0 ||
+      reinterpret_cast<uintptr_t>(out) % out_elem != 0)
+    return fail(TTS_ERR_INVALID_ARG, "pointers must be aligned to an element");
+  if (x_stride > kMaxStride || out_stride > kMaxStride)
+    return fail(TTS_ERR_UNSUPPORTED, "a row stride of more than 2^31 elements");
+  const tts::RmsParams p{x, weight, out, x_stride, out_stride, num_rows, d->row_len, d->dtype == TTS_BF16,
+                         d->out_dtype == TTS_BF16, d->eps};
+  const hipError_t e = tts::launch_rms(p, stream);
+  if (e != hipSuccess) return fail(TTS_ERR_HIP, std::string("norm launch: ") + hipGetErrorString(e));
   return ok();
 }
 

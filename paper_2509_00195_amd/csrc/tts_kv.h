@@ -9,6 +9,14 @@ namespace tts {
 constexpr int kRopeTile = 4096;   // elements (tokens x heads x head dims) of a K or V part
 constexpr int kRopeTasks = 1024;  // units of the query rows to a part
 
+// Lanes that a row of so many units takes with head norms: a power of two, at
+// most a wave.
+constexpr int rope_lanes(int units) {
+  int n = 1;
+  while (n < units && n < 64) n *= 2;
+  return n;
+}
+
 struct RopeParams {
   const void* q;  // null: no queries
   const void* k_new;
@@ -19,12 +27,15 @@ struct RopeParams {
   const int32_t* positions;              // null: the token's index in its sequence
   const int32_t* block_tables;
   const int32_t* seq_lens;
+  const void* q_weight;                  // head norms: null for ones
+  const void* k_weight;
   const float* cos;
   const float* sin;
   void* k_cache;
   void* v_cache;
   float* k_scale;
   float* v_scale;
+  double eps;
   int64_t item0;  // set by the launch, as is what follows max_pos
   int32_t num_seqs;
   int32_t num_tokens;

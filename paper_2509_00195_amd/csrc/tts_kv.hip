@@ -346,22 +346,38 @@ __device__ __forceinline__ int rope_units(const RopeParams& p) {
   return (p.interleaved && W > 1 ? p.rot / W : p.rot / 2 / W) + passed;
 }
 
-template <int W, typename E>
-__device__ __forceinline__ RopeUnit<W> rope_unit(const RopeParams& p, const E* src, int u, const float* cos,
-                                                 const float* sin) {
+// Elements `at` .. + W of a row, of a normalised one its `scale` and weights applied.
+template <int W, bool NORM, typename E>
+__device__ __forceinline__ void load_row(const E* src, const E* weight, float scale, int at, float (&x)[W]) {
+#pragma clang fp contract(off)
+  load_elems<W>(src + at, x);
+  if constexpr (NORM) {
+    float w[W];
+    if (weight) load_elems<W>(weight + at, w);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      x[i] = x[i] * scale;
+      if (weight) x[i] = x[i] * w[i];
+    }
+  }
+}
+
+template <int W, bool NORM, typename E>
+__device__ __forceinline__ RopeUnit<W> rope_unit(const RopeParams& p, const E* src, const E* weight, float scale, int u,
+                                                 const float* cos, const float* sin) {
 #pragma clang fp contract(off)
   RopeUnit<W> r;
   const int half = p.rot / 2, turned = p.interleaved && W > 1 ? p.rot / W : half / W;
   if (u >= turned) {
     r.parts = 1;
     r.at[0] = p.rot + (u - turned) * W;
-    load_elems<W>(src + r.at[0], r.x[0]);
+    load_row<W, NORM>(src, weight, scale, r.at[0], r.x[0]);
   } else if (W > 1 && p.interleaved) {
     constexpr int kPairs = W > 1 ? W / 2 : 1;
     r.parts = 1;
     r.at[0] = u * W;
     float x[W], c[kPairs], s[kPairs];
-    load_elems<W>(src + u * W, x);
+    load_row<W, NORM>(src, weight, scale, u * W, x);
     load_elems<kPairs>(cos + u * kPairs, c);
     load_elems<kPairs>(sin + u * kPairs, s);
 #pragma unroll
@@ -375,8 +391,8 @@ __device__ __forceinline__ RopeUnit<W> rope_unit(const RopeParams& p, const E* s
     r.at[0] = p.interleaved ? 2 * u : u * W;
     r.at[1] = p.interleaved ? 2 * u + 1 : half + u * W;
     float x[W], y[W], c[W], s[W];
-    load_elems<W>(src + r.at[0], x);
-    load_elems<W>(src + r.at[1], y);
+    load_row<W, NORM>(src, weight, scale, r.at[0], x);
+    load_row<W, NORM>(src, weight, scale, r.at[1], y);
     load_elems<W>(cos + u * W, c);
     load_elems<W>(sin + u * W, s);
 #pragma unroll
@@ -387,6 +403,31 @@ __device__ __forceinline__ RopeUnit<W> rope_unit(const RopeParams& p, const E* s
     }
   }
   return r;
+}
+
+// Head norms: x[i] / sqrt(mean of x^2 + eps) * weight[i] over a head's row.
+// Mean and root are taken in 64 bits and rounded to fp32 once, and the two
+// products round one by one, as those of the rotation behind them do: what is
+// stored in 8 and 4 bits then follows from the formula, whatever the order of
+// the sum.
+template <int W, typename E>
+__device__ __forceinline__ double squares(const E* src, int at) {
+  float x[W];
+  load_elems<W>(src + at, x);
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < W; ++i) s += static_cast<double>(x[i]) * static_cast<double>(x[i]);
+  return s;
+}
+
+// The sum of the squares of a unit's elements.
+template <int W, typename E>
+__device__ __forceinline__ double rope_squares(const RopeParams& p, const E* src, int u) {
+  const int half = p.rot / 2, turned = p.interleaved && W > 1 ? p.rot / W : half / W;
+  if (u >= turned) return squares<W>(src, p.rot + (u - turned) * W);
+  if (W > 1 && p.interleaved) return squares<W>(src, u * W);
+  return p.interleaved ? squares<W>(src, 2 * u) + squares<W>(src, 2 * u + 1)
+                       : squares<W>(src, u * W) + squares<W>(src, half + u * W);
 }
 
 __device__ __forceinline__ int64_t rope_pos(const RopeParams& p, const RopeItem& it, int i) {
@@ -406,22 +447,43 @@ __device__ __forceinline__ uint32_t rope_tokens(const RopeParams& p, const RopeI
 
 // Calls f(token, head - h0, unit) for the units of heads h0 .. h1 of the
 // item's good tokens, with the unit rotated.
-template <int W, typename E, typename F>
+//
+// With head norms (`weight`: null for ones) a row's units go to adjacent
+// lanes, as many as rope_lanes() has, and `first` and `last` count lanes: its
+// sum of squares is then a sum over them, of what they hold in registers.
+template <int W, bool NORM, typename E, typename F>
 __device__ __forceinline__ void rope_each(const RopeParams& p, const RopeItem& it, uint32_t good, const E* src,
-                                          int64_t stride, int h0, int h1, int first, int last, F f) {
-  const int units = rope_units<W>(p), heads = h1 - h0, total = it.n * heads * units;
-  const int end = last < total ? last : total;
+                                          int64_t stride, const E* weight, int h0, int h1, int first, int last, F f) {
+  const int units = rope_units<W>(p), heads = h1 - h0;
+  if constexpr (NORM) {
+    const int lanes = rope_lanes(units), all = it.n * heads * lanes, stop = last < all ? last : all;
+    for (int i = first + static_cast<int>(threadIdx.x); i < stop; i += kRopeThreads) {
+      const int lane = i % lanes, h = i / lanes % heads, t = i / lanes / heads;
+      if (!((good >> t) & 1u)) continue;  // (all of a row's lanes)
+      const int64_t at = p.rot > 0 ? rope_pos(p, it, t) * (p.rot / 2) : 0;
+      const E* row = src + (it.row + t) * stride + static_cast<int64_t>(h0 + h) * p.head_dim;
+      double sum = lane < units ? rope_squares<W>(p, row, lane) : 0.0;
+      if (W == 1 && lane + lanes < units) sum += rope_squares<W>(p, row, lane + lanes);
+      for (int o = lanes / 2; o > 0; o /= 2) sum += __shfl_xor(sum, o);
+      const float scale = static_cast<float>(1.0 / sqrt(sum / p.head_dim + p.eps));
+      if (lane < units) f(t, h, rope_unit<W, true>(p, row, weight, scale, lane, p.cos + at, p.sin + at));
+      if (W == 1 && lane + lanes < units)
+        f(t, h, rope_unit<W, true>(p, row, weight, scale, lane + lanes, p.cos + at, p.sin + at));
+    }
+    return;
+  }
+  const int total = it.n * heads * units, end = last < total ? last : total;
   for (int i = first + static_cast<int>(threadIdx.x); i < end; i += kRopeThreads) {
     const int u = i % units, h = i / units % heads, t = i / units / heads;
     if (!((good >> t) & 1u)) continue;
     const int64_t at = p.rot > 0 ? rope_pos(p, it, t) * (p.rot / 2) : 0;
-    f(t, h, rope_unit<W>(p, src + (it.row + t) * stride + static_cast<int64_t>(h0 + h) * p.head_dim, u, p.cos + at,
-                         p.sin + at));
+    f(t, h, rope_unit<W, false>(p, src + (it.row + t) * stride + static_cast<int64_t>(h0 + h) * p.head_dim, weight, 1.f, u,
+                                p.cos + at, p.sin + at));
   }
 }
 
 // Query rows: pieces [first, first + kRopeTasks) of the item's.
-template <int W, typename E>
+template <int W, bool NORM, typename E>
 __device__ __forceinline__ void rope_query(const RopeParams& p, const RopeItem& it, uint32_t good, int part) {
   E* out = static_cast<E*>(p.q_out);
   const int first = part * kRopeTasks;
@@ -435,8 +497,8 @@ __device__ __forceinline__ void rope_query(const RopeParams& p, const RopeItem& 
           store_elems<1>(out + static_cast<int64_t>(it.row + t) * row + i, qnan);
     if (it.bad) return;
   }
-  rope_each<W>(p, it, good, static_cast<const E*>(p.q), p.q_stride, 0, p.hq, first, first + kRopeTasks,
-               [&](int t, int h, const RopeUnit<W>& r) {
+  rope_each<W, NORM>(p, it, good, static_cast<const E*>(p.q), p.q_stride, static_cast<const E*>(p.q_weight), 0, p.hq, first,
+                     first + kRopeTasks, [&](int t, int h, const RopeUnit<W>& r) {
                  E* dst = out + (static_cast<int64_t>(it.row + t) * p.hq + h) * p.head_dim;
                  store_elems<W>(dst + r.at[0], r.x[0]);
                  if (r.parts == 2) store_elems<W>(dst + r.at[1], r.x[1]);
@@ -491,15 +553,16 @@ __device__ __forceinline__ uint32_t mx_quantise(const float (&x)[8], uint32_t* s
 }
 
 // K rows of heads h0 .. h1.
-template <int KV, int W, typename E>
+template <int KV, int W, bool NORM, typename E>
 __device__ __forceinline__ void rope_keys(const RopeParams& p, const RopeItem& it, uint32_t good, int h0, int h1,
                                           void* lds, float* red) {
   const int D = p.head_dim;
   const E* src = static_cast<const E*>(p.k_new);
+  const E* weight = static_cast<const E*>(p.k_weight);
   constexpr int kAll = 0x7FFFFFFF;
   if constexpr (KV == kKvF32 || KV == kKvBf16) {
     E* blk = static_cast<E*>(p.k_cache) + (static_cast<int64_t>(it.blk) * p.hkv + h0) * kSlots * D;
-    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
+    rope_each<W, NORM>(p, it, good, src, p.k_stride, weight, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
       E* dst = blk + (h * kSlots + it.slot + t) * D;
       store_elems<W>(dst + r.at[0], r.x[0]);
       if (r.parts == 2) store_elems<W>(dst + r.at[1], r.x[1]);
@@ -508,7 +571,7 @@ __device__ __forceinline__ void rope_keys(const RopeParams& p, const RopeItem& i
     uint8_t* lut = static_cast<uint8_t*>(lds);
     const float old = p.k_scale[it.blk];
     float top = 0.f;
-    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int, int, const RopeUnit<W>& r) {
+    rope_each<W, NORM>(p, it, good, src, p.k_stride, weight, h0, h1, 0, kAll, [&](int, int, const RopeUnit<W>& r) {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -525,7 +588,7 @@ __device__ __forceinline__ void rope_keys(const RopeParams& p, const RopeItem& i
         *x = map_codes(*x, lut, 16, -1, 0);
       }
     }
-    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
+    rope_each<W, NORM>(p, it, good, src, p.k_stride, weight, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
       uint8_t* dst = blk + (h * kSlots + it.slot + t) * D;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -545,7 +608,7 @@ __device__ __forceinline__ void rope_keys(const RopeParams& p, const RopeItem& i
     // Rotated rows in LDS, then four lanes to a group of 32 dims.
     float* tile = static_cast<float*>(lds);
     const int heads = h1 - h0;
-    rope_each<W>(p, it, good, src, p.k_stride, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
+    rope_each<W, NORM>(p, it, good, src, p.k_stride, weight, h0, h1, 0, kAll, [&](int t, int h, const RopeUnit<W>& r) {
       float* dst = tile + (t * heads + h) * D;
       store_elems<W>(dst + r.at[0], r.x[0]);
       if (r.parts == 2) store_elems<W>(dst + r.at[1], r.x[1]);
@@ -699,7 +762,7 @@ __device__ __forceinline__ void rope_values(const RopeParams& p, const RopeItem&
   }
 }
 
-template <int KV>
+template <int KV, bool NORM>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeParams p) {
   typedef typename std::conditional<KV == kKvF32, float, uint16_t>::type E;
   // 4-bit K: rotated rows in fp32; 4-bit V: codes; fp8: the codes' table.
@@ -711,18 +774,18 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeParams p)
   const uint32_t good = rope_tokens(p, it);
   if (part >= 2 * p.kv_parts) {
     if (p.q_wide)
-      rope_query<8, E>(p, it, good, part - 2 * p.kv_parts);
+      rope_query<8, NORM, E>(p, it, good, part - 2 * p.kv_parts);
     else
-      rope_query<1, E>(p, it, good, part - 2 * p.kv_parts);
+      rope_query<1, NORM, E>(p, it, good, part - 2 * p.kv_parts);
     return;
   }
   if (it.blk < 0 || good == 0) return;
   const int h0 = part / 2 * p.heads_per, h1 = h0 + p.heads_per < p.hkv ? h0 + p.heads_per : p.hkv;
   if (part % 2 == 0) {
     if (p.k_wide)
-      rope_keys<KV, 8, E>(p, it, good, h0, h1, lds, red);
+      rope_keys<KV, 8, NORM, E>(p, it, good, h0, h1, lds, red);
     else
-      rope_keys<KV, 1, E>(p, it, good, h0, h1, lds, red);
+      rope_keys<KV, 1, NORM, E>(p, it, good, h0, h1, lds, red);
   } else {
     if (p.v_wide)
       rope_values<KV, 2, E>(p, it, good, h0, h1, lds, red);
@@ -809,13 +872,25 @@ static bool rows_at(const void* ptr, int64_t stride, int elem, int bytes) {
   return reinterpret_cast<uintptr_t>(ptr) % bytes == 0 && stride * elem % bytes == 0;
 }
 
-hipError_t launch_rope_append(RopeParams p, int kv_kind, hipStream_t stream) {
+template <bool NORM>
+static void launch_rope_t(const RopeParams& p, int kv_kind, dim3 grid, hipStream_t stream) {
+  const dim3 block(kRopeThreads);
+  switch (kv_kind) {
+    case kKvF32: hipLaunchKernelGGL((rope_append_kernel<kKvF32, NORM>), grid, block, 0, stream, p); break;
+    case kKvBf16: hipLaunchKernelGGL((rope_append_kernel<kKvBf16, NORM>), grid, block, 0, stream, p); break;
+    case kKvFp8: hipLaunchKernelGGL((rope_append_kernel<kKvFp8, NORM>), grid, block, 0, stream, p); break;
+    default: hipLaunchKernelGGL((rope_append_kernel<kKvMx4, NORM>), grid, block, 0, stream, p); break;
+  }
+}
+
+hipError_t launch_rope_append(RopeParams p, int kv_kind, bool norm, hipStream_t stream) {
   const int elem = kv_kind == kKvF32 ? 4 : 2, half = p.rot / 2;
   // Eight elements at a time where rows, tables and the rotated part allow it.
   const bool parts8 = p.interleaved ? p.rot % 8 == 0 : half % 8 == 0;
   const bool tables8 = p.rot == 0 || (rows_at(p.cos, half, 4, 16) && rows_at(p.sin, half, 4, 16));
-  p.q_wide = p.q && parts8 && tables8 && rows_at(p.q, p.q_stride, elem, 16) && rows_at(p.q_out, 0, elem, 16);
-  p.k_wide = parts8 && tables8 && rows_at(p.k_new, p.k_stride, elem, 16);
+  p.q_wide = p.q && parts8 && tables8 && rows_at(p.q, p.q_stride, elem, 16) && rows_at(p.q_out, 0, elem, 16) &&
+             rows_at(p.q_weight, 0, elem, 16);
+  p.k_wide = parts8 && tables8 && rows_at(p.k_new, p.k_stride, elem, 16) && rows_at(p.k_weight, 0, elem, 16);
   p.v_wide = rows_at(p.v_new, p.v_stride, elem, 2 * elem);
   const int most_tokens = p.tok_offsets ? kSlots : 1;
   // fp8: one scale for all heads of a block, so one part.
@@ -823,7 +898,8 @@ hipError_t launch_rope_append(RopeParams p, int kv_kind, hipStream_t stream) {
   if (kv_kind == kKvFp8 || p.heads_per > p.hkv) p.heads_per = p.hkv;
   p.kv_parts = (p.hkv + p.heads_per - 1) / p.heads_per;
   const int width = p.q_wide ? 8 : 1;
-  const int64_t units = (p.interleaved && p.q_wide ? p.rot / width : half / width) + (p.head_dim - p.rot) / width;
+  const int row = (p.interleaved && p.q_wide ? p.rot / width : half / width) + (p.head_dim - p.rot) / width;
+  const int64_t units = norm ? rope_lanes(row) : row;
   const int64_t q_parts = p.q ? (most_tokens * p.hq * units + kRopeTasks - 1) / kRopeTasks : 0;
   const int64_t parts = 2 * static_cast<int64_t>(p.kv_parts) + q_parts;
   if (parts > kMaxGridY) return hipErrorInvalidValue;
@@ -834,12 +910,10 @@ hipError_t launch_rope_append(RopeParams p, int kv_kind, hipStream_t stream) {
     const int64_t n = items - done < most ? items - done : most;
     p.item0 = done;
     const dim3 grid(static_cast<unsigned>(n), static_cast<unsigned>(parts));
-    switch (kv_kind) {
-      case kKvF32: hipLaunchKernelGGL(rope_append_kernel<kKvF32>, grid, dim3(kRopeThreads), 0, stream, p); break;
-      case kKvBf16: hipLaunchKernelGGL(rope_append_kernel<kKvBf16>, grid, dim3(kRopeThreads), 0, stream, p); break;
-      case kKvFp8: hipLaunchKernelGGL(rope_append_kernel<kKvFp8>, grid, dim3(kRopeThreads), 0, stream, p); break;
-      default: hipLaunchKernelGGL(rope_append_kernel<kKvMx4>, grid, dim3(kRopeThreads), 0, stream, p); break;
-    }
+    if (norm)
+      launch_rope_t<true>(p, kv_kind, grid, stream);
+    else
+      launch_rope_t<false>(p, kv_kind, grid, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

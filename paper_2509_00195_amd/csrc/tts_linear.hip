@@ -1,0 +1,654 @@
+// Products with trained weights, and the norm before them.
+//
+// out[m][n] = act(sum_k x[m][k] w[n][k] + bias[n]) + residual[m][n], and the
+// gated form act(gate) * up of two such sums. Both operands have the inner
+// dimension contiguous. The weights are the matrix instructions' first
+// operand and x the second, so that a lane ends with four consecutive columns
+// of one row of the output. All of it is done in pieces of 16 bytes (8 bf16
+// values, one 16x16x32 instruction; 4 fp32 values, four 16x16x4 ones): which
+// value of a step lies in which lane group does not matter as long as both
+// operands agree. Sums are fp32, the result is rounded once.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "tts_device.h"
+#include "tts_linear.h"
+
+namespace tts {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// Loads and stores at the addresses of a caller's rows, which need only the
+// alignment of an element (the hardware takes them, an instruction each).
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+template <typename E>
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (sizeof(E) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                   0);
+  } else {
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+    return c;
+  }
+}
+
+// 16 bytes of a row of `end` bytes from byte `at`; what lies behind the end is zero and is not read.
+template <typename E>
+__device__ __forceinline__ u32x4 load_piece(const char* row, int at, int end) {
+  if (at + 16 <= end) return *reinterpret_cast<const u32x4u*>(row + at);
+  u32x4 r = {0u, 0u, 0u, 0u};
+  if constexpr (sizeof(E) == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (at + 2 * i < end)
+        r[i / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(row + at + 2 * i)) << (16 * (i % 2));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + 4 * i < end) r[i] = *reinterpret_cast<const uint32_t*>(row + at + 4 * i);
+  }
+  return r;
+}
+
+__device__ __forceinline__ float activate(float y, int act) {
+  switch (act) {
+    case kActRelu: return y < 0.f ? 0.f : y;  // (NaN stays)
+    case kActSilu: return y / (1.f + __expf(-y));
+    case kActGelu: return 0.5f * y * erfcf(-0.70710678118654752f * y);
+    case kActGeluTanh: {  // 1 + tanh z = 2 / (1 + exp(-2 z))
+      const float z = 0.79788456080286536f * (y + 0.044715f * y * y * y);
+      return y / (1.f + __expf(-2.f * z));
+    }
+    default: return y;
+  }
+}
+
+// `count` (at most 4) values from element i of an array of bf16 or fp32.
+__device__ __forceinline__ f32x4 load_row4(const void* p, int64_t i, int count, bool is_bf16) {
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+  if (is_bf16) {
+    const __bf16* s = static_cast<const __bf16*>(p) + i;
+    if (count == 4) return __builtin_convertvector(*reinterpret_cast<const bf16x4u*>(s), f32x4);
+    for (int j = 0; j < 3; ++j)
+      if (j < count) r[j] = static_cast<float>(s[j]);
+  } else {
+    const float* s = static_cast<const float*>(p) + i;
+    if (count == 4) return *reinterpret_cast<const f32x4u*>(s);
+    for (int j = 0; j < 3; ++j)
+      if (j < count) r[j] = s[j];
+  }
+  return r;
+}
+
+// The finished columns n .. n + 3 (those below p.n) of row m from their sums.
+template <bool GATED>
+__device__ __forceinline__ void finish(const LinearParams& p, int m, int n, f32x4 y, f32x4 up) {
+  const int count = p.n - n < 4 ? p.n - n : 4;
+  if (p.bias[0]) y += load_row4(p.bias[0], n, count, p.in_bf16);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = activate(y[j], p.act);
+  if constexpr (GATED) {
+    if (p.bias[1]) up += load_row4(p.bias[1], n, count, p.in_bf16);
+    y *= up;
+  }
+  if (p.residual) y += load_row4(p.residual, m * p.residual_stride + n, count, p.out_bf16);
+  const int64_t at = m * p.out_stride + n;
+  if (p.out_bf16) {
+    __bf16* o = static_cast<__bf16*>(p.out) + at;
+    const bf16x4 r = __builtin_convertvector(y, bf16x4);
+    if (count == 4)
+      *reinterpret_cast<bf16x4u*>(o) = r;
+    else
+      for (int j = 0; j < 3; ++j)
+        if (j < count) o[j] = r[j];
+  } else {
+    float* o = static_cast<float*>(p.out) + at;
+    if (count == 4)
+      *reinterpret_cast<f32x4u*>(o) = y;
+    else
+      for (int j = 0; j < 3; ++j)
+        if (j < count) o[j] = y[j];
+  }
+}
+
+// Partial sums of a split, columns n .. n + 3 of row m of plane 0 (gate) or 1 (up).
+__device__ __forceinline__ int64_t part_at(const LinearParams& p, int split, int plane, int planes, int m, int n) {
+  return ((static_cast<int64_t>(split) * planes + plane) * p.rows + m) * p.n + n;
+}
+
+__device__ __forceinline__ void store_part(float* dst, int count, f32x4 y) {
+  if (count == 4)
+    *reinterpret_cast<f32x4u*>(dst) = y;
+  else
+    for (int j = 0; j < 3; ++j)
+      if (j < count) dst[j] = y[j];
+}
+
+template <bool GATED>
+__device__ __forceinline__ void emit(const LinearParams& p, int split, int m, int n, f32x4 y, f32x4 up) {
+  if (m >= p.rows || n >= p.n) return;
+  if (p.splits == 1) {
+    finish<GATED>(p, m, n, y, up);
+    return;
+  }
+  constexpr int kPlanes = GATED ? 2 : 1;
+  const int count = p.n - n < 4 ? p.n - n : 4;
+  store_part(p.part + part_at(p, split, 0, kPlanes, m, n), count, y);
+  if constexpr (GATED) store_part(p.part + part_at(p, split, 1, kPlanes, m, n), count, up);
+}
+
+// ---- few rows ----------------------------------------------------------------
+
+constexpr int kFewWaves = 8;
+constexpr int kFewThreads = 64 * kFewWaves;
+
+// MT tiles of 16 rows of x, NT tiles of 16 rows of weights (gated: the first
+// half gate, the second up, of the same columns). Bound by the weights'
+// bytes: each is read once, straight into registers, 128 bytes of a row at a
+// time. The workgroup's chunks of the inner dimension go to its waves in turn,
+// and the waves' sums are added in LDS in the order of the waves.
+template <typename E, int MT, int NT, bool GATED, int U>
+__global__ __launch_bounds__(kFewThreads) void few_rows_kernel(LinearParams p) {
+  __shared__ __attribute__((aligned(16))) f32x4 sums[kFewWaves][NT * MT][64];
+  const int wave = static_cast<int>(threadIdx.x) / 64, lane = static_cast<int>(threadIdx.x) % 64;
+  const int row = lane & 15, group = lane >> 4;
+  constexpr int kCols = (GATED ? NT / 2 : NT) * 16;
+  const int n0 = static_cast<int>(blockIdx.x) * kCols;
+  const char* wp[NT];
+  const char* xp[MT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int plane = GATED && t >= NT / 2, local = GATED ? t % (NT / 2) : t;
+    int n = n0 + 16 * local + row;
+    n = n < p.n ? n : p.n - 1;
+    wp[t] = static_cast<const char*>(p.w[plane]) + n * p.w_stride + 32 * group;
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    int m = 16 * t + row;
+    m = m < p.rows ? m : p.rows - 1;
+    xp[t] = static_cast<const char*>(p.x) + m * p.x_stride + 32 * group;
+  }
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int whole = p.k_bytes / kLinearChunk, total = (p.k_bytes + kLinearChunk - 1) / kLinearChunk;
+  const int first = static_cast<int>(blockIdx.y) * p.chunks;
+  const int end = first + p.chunks < total ? first + p.chunks : total;
+  const int full = end < whole ? end : whole;
+  int c = first + wave;
+  for (; c + (U - 1) * kFewWaves < full; c += U * kFewWaves) {
+    u32x4 a[U][NT][2], b[U][MT][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = static_cast<int64_t>(c + u * kFewWaves) * kLinearChunk;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) a[u][t][h] = *reinterpret_cast<const u32x4u*>(wp[t] + at + 16 * h);
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) b[u][t][h] = *reinterpret_cast<const u32x4u*>(xp[t] + at + 16 * h);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int j = 0; j < MT; ++j) acc[i][j] = mma<E>(a[u][i][h], b[u][j][h], acc[i][j]);
+  }
+  for (; c < end; c += kFewWaves) {
+    const int at = c * kLinearChunk, left = p.k_bytes - 32 * group;  // (bytes of the row from this lane's pointer)
+    u32x4 a[NT][2], b[MT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) a[t][h] = load_piece<E>(wp[t], at + 16 * h, left);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) b[t][h] = load_piece<E>(xp[t], at + 16 * h, left);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = mma<E>(a[i][h], b[j][h], acc[i][j]);
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) sums[wave][i * MT + j][lane] = acc[i][j];
+  __syncthreads();
+  constexpr int kItems = (GATED ? NT / 2 : NT) * MT * 64;
+  for (int i = threadIdx.x; i < kItems; i += kFewThreads) {
+    const int l = i % 64, t = i / 64, m = 16 * (t % MT) + (l & 15);
+    if (m >= p.rows) continue;
+    f32x4 y = sums[0][t][l], up = y;
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) y += sums[w][t][l];
+    if constexpr (GATED) {
+      up = sums[0][t + kItems / 64][l];
+#pragma unroll
+      for (int w = 1; w < kFewWaves; ++w) up += sums[w][t + kItems / 64][l];
+    }
+    emit<GATED>(p, static_cast<int>(blockIdx.y), m, n0 + 16 * (t / MT) + 4 * (l >> 4), y, up);
+  }
+}
+
+// ---- tiles -------------------------------------------------------------------
+
+constexpr uint32_t kOutside = 0x80000000u;  // behind the end of every tile's buffer: reads as zero
+
+// A buffer whose loads are checked against its size, and its loads into LDS (16
+// bytes to a lane, lane after lane from `lds`). The builtins are known to the
+// device's compilation alone.
+struct Rows {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ void set(const char* base, uint32_t bytes) {
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00020000);
+  }
+  __device__ __forceinline__ void load(char* lds, uint32_t offset, int at) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)lds, 16, offset, at, 0, 0);
+  }
+#else
+  __device__ void set(const char*, uint32_t) {}
+  __device__ void load(char*, uint32_t, int) const {}
+#endif
+};
+
+// Waits for this wave's loads into LDS: a barrier behind it then means that all
+// waves' have landed (the barrier alone waits for none).
+__device__ __forceinline__ void landed() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
+
+// A tile's rows lie in LDS 128 bytes each, in eight pieces of 16 whose places
+// are permuted by the row (piece c of row r at c ^ (r & 7)), so that the same
+// piece of 16 rows, which a matrix operand reads, is spread over the banks. The
+// LDS side of a load into LDS is fixed (lane after lane), so the lanes' global
+// addresses carry the permutation.
+template <typename E, int BM, int BN, int WM, int WN, bool GATED, bool ALIGNED>
+__global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
+  constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+  constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 tiles of a wave
+  constexpr int kStage = (BM + BN) * kLinearChunk;
+  constexpr int kLoadsN = BN / 8 / kWaves, kLoadsM = BM / 8 / kWaves;
+  constexpr int kPlanes = GATED ? 2 : 1;
+  constexpr int kCols = BN / kPlanes;
+  __shared__ __attribute__((aligned(16))) char stage0[kStage];
+  __shared__ __attribute__((aligned(16))) char stage1[kStage];
+  const int wave = static_cast<int>(threadIdx.x) / 64, lane = static_cast<int>(threadIdx.x) % 64;
+
+  // Tiles in groups of 8 along x's rows; consecutive ones on one XCD, whose L2
+  // then serves the group's shared rows.
+  int id = static_cast<int>(blockIdx.x);
+  const int tiles = p.m_tiles * p.n_tiles;
+  {
+    const int per = tiles / 8, rest = tiles % 8, xcd = id % 8, nth = id / 8;
+    id = xcd * per + (xcd < rest ? xcd : rest) + nth;
+  }
+  constexpr int kGroup = 8;
+  const int in_group = kGroup * p.n_tiles, g0 = id / in_group * kGroup;
+  const int height = p.m_tiles - g0 < kGroup ? p.m_tiles - g0 : kGroup;
+  const int m0 = (g0 + id % in_group % height) * BM, n0 = id % in_group / height * kCols;
+
+  const int split = static_cast<int>(blockIdx.y);
+  const int total = (p.k_bytes + kLinearChunk - 1) / kLinearChunk;
+  const int first = split * p.chunks, end = first + p.chunks < total ? first + p.chunks : total;
+  const int stop = end == total ? p.k_bytes : end * kLinearChunk;  // of a row's bytes
+
+  const int sub = lane >> 3, piece = (lane & 7) ^ sub;  // a load's 8 rows: this lane's row and piece of it
+  const int rows_m = p.rows - m0 < BM ? p.rows - m0 : BM, rows_n = p.n - n0 < kCols ? p.n - n0 : kCols;
+  const char* xb = static_cast<const char*>(p.x) + m0 * p.x_stride;
+  const char* wb[kPlanes];
+#pragma unroll
+  for (int i = 0; i < kPlanes; ++i) wb[i] = static_cast<const char*>(p.w[i]) + n0 * p.w_stride;
+
+  // Rows of load i, within the operand (gated: within its plane).
+  constexpr int kStep = 8 * kWaves;
+  const auto row_n = [&](int i) { return (i % (kLoadsN / kPlanes)) * kStep + wave * 8 + sub; };
+  const auto row_m = [&](int i) { return i * kStep + wave * 8 + sub; };
+
+  // (Rows behind the last one start behind the buffer's end.)
+  Rows xr, wr[kPlanes];
+  xr.set(xb, static_cast<uint32_t>((rows_m - 1) * p.x_stride + p.k_bytes));
+#pragma unroll
+  for (int i = 0; i < kPlanes; ++i) wr[i].set(wb[i], static_cast<uint32_t>((rows_n - 1) * p.w_stride + p.k_bytes));
+  const uint32_t off_n = static_cast<uint32_t>(row_n(0) * p.w_stride + 16 * piece);
+  const uint32_t off_m = static_cast<uint32_t>(row_m(0) * p.x_stride + 16 * piece);
+  u32x4 held[ALIGNED ? 1 : kLoadsN + kLoadsM];
+
+  // Starts the loads of chunk c (aligned: into LDS; else into registers, for put()).
+  auto start = [&](char* stage, int c) {
+    const int at = c * kLinearChunk;
+    if constexpr (ALIGNED) {
+      const bool out = at + 16 * piece >= stop;
+      const uint32_t from_n = out ? kOutside : off_n, from_m = out ? kOutside : off_m;
+      const uint32_t step_n = static_cast<uint32_t>(kStep * p.w_stride), step_m = static_cast<uint32_t>(kStep * p.x_stride);
+#pragma unroll
+      for (int i = 0; i < kLoadsN; ++i)
+        wr[i / (kLoadsN / kPlanes)].load(stage + (i * kWaves + wave) * 1024, from_n + (i % (kLoadsN / kPlanes)) * step_n, at);
+#pragma unroll
+      for (int i = 0; i < kLoadsM; ++i)
+        xr.load(stage + BN * kLinearChunk + (i * kWaves + wave) * 1024, from_m + i * step_m, at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoadsN; ++i)
+        held[i] = load_piece<E>(wb[i / (kLoadsN / kPlanes)] + least(row_n(i), rows_n - 1) * p.w_stride, at + 16 * piece, stop);
+#pragma unroll
+      for (int i = 0; i < kLoadsM; ++i)
+        held[kLoadsN + i] = load_piece<E>(xb + least(row_m(i), rows_m - 1) * p.x_stride, at + 16 * piece, stop);
+    }
+  };
+  auto put = [&](char* stage) {
+    if constexpr (!ALIGNED) {
+#pragma unroll
+      for (int i = 0; i < kLoadsN; ++i)
+        *reinterpret_cast<u32x4*>(stage + (i * kWaves + wave) * 1024 + lane * 16) = held[i];
+#pragma unroll
+      for (int i = 0; i < kLoadsM; ++i)
+        *reinterpret_cast<u32x4*>(stage + BN * kLinearChunk + (i * kWaves + wave) * 1024 + lane * 16) = held[kLoadsN + i];
+    }
+  };
+
+  const int wm = wave % WM, wn = wave / WM, row = lane & 15, group = lane >> 4;
+  f32x4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Operands {
+    u32x4 a[TN], b[TM];
+  };
+  auto read = [&](const char* stage, int step) {
+    Operands o;
+    const char* at = stage + row * kLinearChunk + ((4 * step + group) ^ (row & 7)) * 16;
+#pragma unroll
+    for (int t = 0; t < TN; ++t) {
+      const int r = GATED ? (t >= TN / 2 ? kCols : 0) + wn * (TN / 2 * 16) + t % (TN / 2) * 16 : (wn * TN + t) * 16;
+      o.a[t] = *reinterpret_cast<const u32x4*>(at + r * kLinearChunk);
+    }
+#pragma unroll
+    for (int t = 0; t < TM; ++t) o.b[t] = *reinterpret_cast<const u32x4*>(at + (BN + (wm * TM + t) * 16) * kLinearChunk);
+    return o;
+  };
+  auto multiply = [&](const Operands& o) {
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) acc[i][j] = mma<E>(o.a[i], o.b[j], acc[i][j]);
+  };
+
+  // Each chunk is two steps. The first step's operands of a chunk are read
+  // while the second of the chunk before it is multiplied; the one barrier per
+  // chunk lies between: all waves have read the chunk, and the next one's
+  // loads, started a chunk ago, have landed. Chunks behind the end load
+  // nothing and are zero, so that the loop holds no branch.
+  start(stage0, first);
+  put(stage0);
+  landed();
+  __syncthreads();
+  start(stage1, first + 1);
+  Operands lo = read(stage0, 0), hi;
+  const auto chunk = [&](char* cur, char* next, int c) {
+    __builtin_amdgcn_sched_barrier(0);
+    hi = read(cur, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(lo);
+    __builtin_amdgcn_sched_barrier(0);
+    put(next);
+    landed();
+    __syncthreads();
+    start(cur, c + 2);
+    lo = read(next, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(hi);
+  };
+  for (int c = first; c < end; c += 2) {
+    chunk(stage0, stage1, c);
+    chunk(stage1, stage0, c + 1);
+  }
+
+  // The sums go through LDS, two tiles of rows at a time, so that what is
+  // written is whole runs of columns (and the code of the activations stands
+  // once per pass).
+  constexpr int kWidth = TN * 4, kQuads = GATED ? kWidth / 2 : kWidth;  // four columns each
+  static_assert(kWaves * 32 * kWidth * 16 <= kStage && (kWidth & (kWidth - 1)) == 0, "a wave's part of a stage");
+  f32x4* const tile = reinterpret_cast<f32x4*>(stage0) + wave * (32 * kWidth);
+  const auto place = [&](int r, int q) { return tile + r * kWidth + (q ^ (r & (kWidth - 1))); };  // (spread over the banks)
+#pragma unroll
+  for (int j = 0; j < TM; j += 2) {
+    landed();
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < TN; ++i) *place(16 * h + row, 4 * i + group) = acc[i][j + h];
+    __syncthreads();
+#pragma nounroll
+    for (int i = lane; i < 32 * kQuads; i += 64) {
+      const int r = i / kQuads, q = i % kQuads;
+      emit<GATED>(p, split, m0 + (wm * TM + j) * 16 + r, n0 + (wn * kQuads + q) * 4, *place(r, q),
+                  *place(r, q + (GATED ? kQuads : 0)));
+    }
+  }
+}
+
+// The splits' sums, added in their order, and finished.
+constexpr int kJoinThreads = 256;
+
+template <bool GATED>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(LinearParams p) {
+  constexpr int kPlanes = GATED ? 2 : 1;
+  const int quads = (p.n + 3) / 4;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kJoinThreads + threadIdx.x;
+  if (i >= static_cast<int64_t>(quads) * p.rows) return;
+  const int m = static_cast<int>(i / quads), n = static_cast<int>(i % quads) * 4;
+  const int count = p.n - n < 4 ? p.n - n : 4;
+  f32x4 y[kPlanes];
+#pragma unroll
+  for (int q = 0; q < kPlanes; ++q) {
+    y[q] = load_row4(p.part, part_at(p, 0, q, kPlanes, m, n), count, false);
+    for (int s = 1; s < p.splits; ++s) y[q] += load_row4(p.part, part_at(p, s, q, kPlanes, m, n), count, false);
+  }
+  finish<GATED>(p, m, n, y[0], y[kPlanes - 1]);
+}
+
+// ---- norm --------------------------------------------------------------------
+
+constexpr int kRmsThreads = 256;
+constexpr int kRmsHeld = 4;  // pieces of 8 elements that a thread keeps of a row
+
+// `count` (at most 8) elements; the others are zero.
+template <typename E>
+__device__ __forceinline__ void load_row8(const E* src, int count, float (&x)[8]) {
+  if (count == 8) {
+    if constexpr (sizeof(E) == 2) {
+      const u32x4 w = *reinterpret_cast<const u32x4u*>(src);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+        x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
+      }
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32x4u*>(src), b = *reinterpret_cast<const f32x4u*>(src + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = i < count ? static_cast<float>(src[i]) : 0.f;
+}
+
+template <typename E>
+__device__ __forceinline__ void store_row8(E* dst, int count, const float (&x)[8]) {
+  if (count == 8) {
+    if constexpr (sizeof(E) == 2) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+      *reinterpret_cast<u32x4u*>(dst) = w;
+    } else {
+      *reinterpret_cast<f32x4u*>(dst) = f32x4{x[0], x[1], x[2], x[3]};
+      *reinterpret_cast<f32x4u*>(dst + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < count) dst[i] = static_cast<E>(x[i]);
+}
+
+// out[i] = x[i] / sqrt(mean of x^2 + eps) * weight[i], a workgroup to a row.
+// Each thread keeps its pieces of a row of up to 8192 elements; longer rows
+// are read a second time. Bound by memory, and for few rows by the round trips.
+template <typename E, typename O>
+__global__ __launch_bounds__(kRmsThreads) void rms_kernel(RmsParams p) {
+  __shared__ float red[2][kRmsThreads / 64];
+  const int pieces = (p.len + 7) / 8, tid = static_cast<int>(threadIdx.x);
+  const auto count = [&](int at) { return at + 1 < pieces ? 8 : p.len - 8 * at; };
+  const E* weight = static_cast<const E*>(p.weight);
+  int turn = 0;  // (the sums' place alternates: one barrier per row)
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+    const E* x = static_cast<const E*>(p.x) + row * p.x_stride;
+    O* out = static_cast<O*>(p.out) + row * p.out_stride;
+    float held[kRmsHeld][8], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kRmsHeld; ++i) {
+      const int at = tid + i * kRmsThreads;
+      if (at >= pieces) continue;
+      load_row8(x + 8 * at, count(at), held[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += held[i][j] * held[i][j];
+    }
+#pragma nounroll
+    for (int at = tid + kRmsHeld * kRmsThreads; at < pieces; at += kRmsThreads) {
+      float y[8];
+      load_row8(x + 8 * at, count(at), y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += y[j] * y[j];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if ((tid & 63) == 0) red[turn][tid / 64] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRmsThreads / 64; ++w) sum += red[turn][w];
+    const float scale = 1.f / sqrtf(sum / static_cast<float>(p.len) + p.eps);
+    const auto write = [&](int at, float (&y)[8]) {
+      float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+      if (weight) load_row8(weight + 8 * at, count(at), w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = y[j] * scale * w[j];
+      store_row8(out + 8 * at, count(at), y);
+    };
+#pragma unroll
+    for (int i = 0; i < kRmsHeld; ++i)
+      if (tid + i * kRmsThreads < pieces) write(tid + i * kRmsThreads, held[i]);
+#pragma nounroll
+    for (int at = tid + kRmsHeld * kRmsThreads; at < pieces; at += kRmsThreads) {
+      float y[8];
+      load_row8(x + 8 * at, count(at), y);
+      write(at, y);
+    }
+  }
+}
+
+int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
+
+}  // namespace
+
+template <typename E, bool GATED>
+static void launch_few(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(p.n_tiles), static_cast<unsigned>(p.splits)), block(kFewThreads);
+#define TTS_FEW(MT, NT, U) hipLaunchKernelGGL((few_rows_kernel<E, MT, NT, GATED, U>), grid, block, 0, stream, p)
+  if constexpr (!GATED) {
+    if (plan.bn == 16) {
+      if (plan.bm == 16) TTS_FEW(1, 1, 4);
+      else if (plan.bm == 32) TTS_FEW(2, 1, 4);
+      else TTS_FEW(4, 1, 2);
+      return;
+    }
+  }
+  if (plan.bm == 16) TTS_FEW(1, 2, 4);
+  else if (plan.bm == 32) TTS_FEW(2, 2, 2);
+  else TTS_FEW(4, 2, 2);
+#undef TTS_FEW
+}
+
+template <typename E, bool GATED, bool ALIGNED>
+static void launch_tiles(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles), static_cast<unsigned>(p.splits));
+  if constexpr (ALIGNED && sizeof(E) == 2) {
+    if (plan.tile == 256) {
+      hipLaunchKernelGGL((tile_kernel<E, 256, 256, 2, 4, GATED, true>), grid, dim3(512), 0, stream, p);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((tile_kernel<E, 128, 128, 2, 2, GATED, ALIGNED>), grid, dim3(256), 0, stream, p);
+}
+
+template <typename E, bool GATED>
+static hipError_t launch_linear_t(LinearParams p, const LinearPlan& plan, bool aligned, hipStream_t stream) {
+  p.splits = plan.splits;
+  p.chunks = plan.chunks;
+  p.m_tiles = ceil_div(p.rows, plan.bm);
+  p.n_tiles = ceil_div(static_cast<int64_t>(p.n) * (GATED ? 2 : 1), plan.bn);
+  if (plan.tile == 0)
+    launch_few<E, GATED>(p, plan, stream);
+  else if (aligned)
+    launch_tiles<E, GATED, true>(p, plan, stream);
+  else
+    launch_tiles<E, GATED, false>(p, plan, stream);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const int64_t items = static_cast<int64_t>((p.n + 3) / 4) * p.rows;
+  hipLaunchKernelGGL(join_kernel<GATED>, dim3(static_cast<unsigned>((items + kJoinThreads - 1) / kJoinThreads)),
+                     dim3(kJoinThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, bool gated, bool aligned, hipStream_t stream) {
+  if (p.in_bf16)
+    return gated ? launch_linear_t<uint16_t, true>(p, plan, aligned, stream)
+                 : launch_linear_t<uint16_t, false>(p, plan, aligned, stream);
+  return gated ? launch_linear_t<float, true>(p, plan, aligned, stream)
+               : launch_linear_t<float, false>(p, plan, aligned, stream);
+}
+
+hipError_t launch_rms(const RmsParams& p, hipStream_t stream) {
+  constexpr int kMostGroups = 1 << 20;
+  const dim3 grid(static_cast<unsigned>(p.rows < kMostGroups ? p.rows : kMostGroups)), block(kRmsThreads);
+  if (p.in_bf16 && p.out_bf16)
+    hipLaunchKernelGGL((rms_kernel<__bf16, __bf16>), grid, block, 0, stream, p);
+  else if (p.in_bf16)
+    hipLaunchKernelGGL((rms_kernel<__bf16, float>), grid, block, 0, stream, p);
+  else if (p.out_bf16)
+    hipLaunchKernelGGL((rms_kernel<float, __bf16>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((rms_kernel<float, float>), grid, block, 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace tts

@@ -74,3 +74,78 @@ class PrefixAttention:
             x.v_scale if v_scale is None else v_scale, x.block_tables, int(x.block_tables.shape[1]),
             x.seq_lens if seq_lens is None else seq_lens, self.num_blocks, o, self.ws, self.ws_bytes, stream)
         return o
+
+
+class DecoderLayer:
+    """One decoder layer over a paged cache: norm, projections, head norms with rotation and append, attention, output
+    projection with its residual, norm, gated product, last projection with its residual. Every step is one call of
+    libtts on buffers that are allocated once.
+
+    ``weights``: a mapping of device tensors in the queries' type: ``attn_norm`` [hidden], ``qkv`` [(Hq + 2 Hkv) D][hidden],
+    ``out`` [hidden][Hq D], ``ffn_norm`` [hidden], ``gate`` and ``up`` [ffn][hidden], ``down`` [hidden][ffn], and if
+    wanted ``qkv_bias``, ``q_norm`` and ``k_norm`` [D] (without both, heads are not normalised). ``desc``: its output is of
+    the queries' type."""
+
+    def __init__(self, desc: _t.tts_attn_desc, weights, rope: _t.tts_rope_desc, max_tokens: int, max_seqs: int,
+                 max_seq_len: int, num_blocks: int, eps: float = 1e-6, act: str = "silu"):
+        if desc.out_dtype != desc.q_dtype:
+            raise ValueError("the attention's output must be of the queries' type")
+        w = self.w = dict(weights)
+        self.desc, self.rope, self.max_seq_len, self.num_blocks = desc, rope, int(max_seq_len), int(num_blocks)
+        hq, hkv, d, t = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.q_dtype
+        hidden, ffn = int(w["qkv"].shape[1]), int(w["gate"].shape[0])
+        dev, torch_t = w["qkv"].device, torch.float32 if t == _t.TTS_F32 else torch.bfloat16
+        empty = lambda *shape: torch.empty(shape, dtype=torch_t, device=dev)  # noqa: E731
+        self.normed, self.qkv = empty(max_tokens, hidden), empty(max_tokens, hq + 2 * hkv, d)
+        self.q, self.o, self.ffn = empty(max_tokens, hq, d), empty(max_tokens, hq, d), empty(max_tokens, ffn)
+        self.norm = _t.make_norm(hidden, eps, t, t)
+        self.heads = None
+        if w.get("q_norm") is not None or w.get("k_norm") is not None:
+            self.heads = _t.make_head_norm(w.get("q_norm"), w.get("k_norm"), eps)
+        self.lin_qkv = _t.make_linear(hidden, (hq + 2 * hkv) * d, t, t)
+        self.lin_out = _t.make_linear(hq * d, hidden, t, t)
+        self.lin_ffn = _t.make_linear(hidden, ffn, t, t, act)
+        self.lin_down = _t.make_linear(ffn, hidden, t, t)
+        size = max(_t.tts_linear_workspace_size(x, max_tokens) for x in (self.lin_qkv, self.lin_out, self.lin_down))
+        size = max(size, _t.tts_gated_linear_workspace_size(self.lin_ffn, max_tokens),
+                   _t.tts_paged_decode_workspace_size(desc, max_seqs, self.max_seq_len))
+        self.ws = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
+
+    def __call__(self, x, k_cache, v_cache, block_tables, seq_lens, k_scale=None, v_scale=None, tok_offsets=None,
+                 meta: Optional[_t.PrefixMeta] = None, stream=None):
+        """x [tokens][hidden], replaced by the layer's output. Without ``tok_offsets`` every sequence has one new token,
+        and the attention is the paged call, or with ``meta`` the prefix-shared one; else it is the prefill. A call that
+        needs a larger workspace than the calls before it allocates one: make it once before capturing it."""
+        w, ws, n, s = self.w, self.ws, int(x.shape[0]), int(seq_lens.shape[0])
+        hq, hkv, d = self.desc.num_q_heads, self.desc.num_kv_heads, self.desc.head_dim
+        cols, cache, scales = int(block_tables.shape[1]), (k_cache, v_cache), (k_scale, v_scale)
+        need = 0
+        if tok_offsets is not None:
+            need = _t.tts_paged_prefill_workspace_size(self.desc, s, n, self.max_seq_len)
+        elif meta is not None:
+            need = _t.tts_prefix_decode_workspace_size(self.desc, meta)
+        if need > ws.numel():
+            ws = self.ws = torch.empty(need, dtype=torch.uint8, device=ws.device)
+        size, qkv, q, o, f = ws.numel(), self.qkv[:n], self.q[:n], self.o[:n], self.ffn[:n]
+        _t.tts_rms_norm(self.norm, n, x, w["attn_norm"], self.normed, stream)
+        _t.tts_linear(self.lin_qkv, n, self.normed, w["qkv"], qkv.flatten(1), w.get("qkv_bias"), None, ws, size, stream)
+        args = (s, n, qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], block_tables, cols, seq_lens, self.num_blocks, *cache, *scales)
+        kw = dict(rope=self.rope, q=qkv[:, :hq], q_out=q, tok_offsets=tok_offsets, stream=stream)
+        if self.heads is not None:
+            _t.tts_norm_rope_append_kv(self.desc, self.heads, *args, **kw)
+        else:
+            _t.tts_rope_append_kv(self.desc, *args, **kw)
+        if tok_offsets is not None:
+            _t.tts_paged_prefill_attn(self.desc, s, n, tok_offsets, q, *cache, *scales, block_tables, cols, seq_lens,
+                                      self.max_seq_len, self.num_blocks, o, ws, size, stream)
+        elif meta is not None:
+            _t.tts_prefix_decode_attn(self.desc, meta, q, *cache, *scales, block_tables, cols, seq_lens, self.num_blocks, o,
+                                      ws, size, stream)
+        else:
+            _t.tts_paged_decode_attn(self.desc, s, q, *cache, *scales, block_tables, cols, seq_lens, self.max_seq_len,
+                                     self.num_blocks, o, ws, size, stream)
+        _t.tts_linear(self.lin_out, n, o.flatten(1), w["out"], x, None, x, ws, size, stream)
+        _t.tts_rms_norm(self.norm, n, x, w["ffn_norm"], self.normed, stream)
+        _t.tts_gated_linear(self.lin_ffn, n, self.normed, w["gate"], w["up"], f, None, None, ws, size, stream)
+        _t.tts_linear(self.lin_down, n, f, w["down"], x, None, x, ws, size, stream)
+        return x

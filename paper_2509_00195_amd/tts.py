@@ -32,6 +32,7 @@ STATUS_NAMES = {0: "TTS_OK", -1: "TTS_ERR_INVALID_ARG", -2: "TTS_ERR_UNSUPPORTED
 
 TTS_F32, TTS_BF16, TTS_FP8_E4M3, TTS_MXFP4 = 0, 1, 2, 3
 DTYPES = {"f32": TTS_F32, "bf16": TTS_BF16, "fp8": TTS_FP8_E4M3, "mx4": TTS_MXFP4}
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 
 EXPORTED = [
     "tts_build_prefix_meta", "tts_prefix_meta_destroy", "tts_prefix_meta_export", "tts_prefix_meta_coverage",
@@ -41,7 +42,8 @@ EXPORTED = [
     "tts_prefix_decode_merge", "tts_append_kv", "tts_copy_blocks", "tts_fork_tables", "tts_kv_alloc_time",
     "tts_kv_alloc_search", "tts_prefix_schedule", "tts_build_verify_meta", "tts_prefix_verify_attn",
     "tts_last_error", "tts_fork_prefix_meta", "tts_truncated_lengths", "tts_rope_append_kv", "tts_rope_tables",
-    "tts_paged_prefill_workspace_size", "tts_paged_prefill_attn",
+    "tts_paged_prefill_workspace_size", "tts_paged_prefill_attn", "tts_norm_rope_append_kv", "tts_linear",
+    "tts_linear_workspace_size", "tts_gated_linear", "tts_gated_linear_workspace_size", "tts_rms_norm",
 ]
 
 
@@ -60,6 +62,19 @@ class tts_attn_desc(C.Structure):
 class tts_rope_desc(C.Structure):
     _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("max_pos", C.c_int32), ("cos", C.c_void_p),
                 ("sin", C.c_void_p)]
+
+
+class tts_head_norm_desc(C.Structure):
+    _fields_ = [("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
+class tts_linear_desc(C.Structure):
+    _fields_ = [("in_features", C.c_int32), ("out_features", C.c_int32), ("dtype", C.c_int), ("out_dtype", C.c_int),
+                ("act", C.c_int)]
+
+
+class tts_norm_desc(C.Structure):
+    _fields_ = [("row_len", C.c_int32), ("dtype", C.c_int), ("out_dtype", C.c_int), ("eps", C.c_float)]
 
 
 class tts_model_cost(C.Structure):
@@ -152,6 +167,19 @@ def load() -> C.CDLL:
     lib.tts_rope_append_kv.restype = C.c_int
     lib.tts_rope_append_kv.argtypes = [P(tts_attn_desc), P(tts_rope_desc), I32, I32, VP, VP, VP, I64, VP, I64, VP, I64,
                                        VP, I32, VP, I32, VP, VP, VP, VP, VP, VP]
+    lib.tts_norm_rope_append_kv.restype = C.c_int
+    lib.tts_norm_rope_append_kv.argtypes = [P(tts_attn_desc), P(tts_head_norm_desc),
+                                            *lib.tts_rope_append_kv.argtypes[1:]]
+    for name in ("tts_linear_workspace_size", "tts_gated_linear_workspace_size"):
+        getattr(lib, name).restype = C.c_size_t
+        getattr(lib, name).argtypes = [P(tts_linear_desc), I32]
+    lib.tts_linear.restype = C.c_int
+    lib.tts_linear.argtypes = [P(tts_linear_desc), I32, VP, I64, VP, I64, VP, VP, I64, VP, I64, VP, C.c_size_t, VP]
+    lib.tts_gated_linear.restype = C.c_int
+    lib.tts_gated_linear.argtypes = [P(tts_linear_desc), I32, VP, I64, VP, VP, I64, VP, VP, VP, I64, VP, C.c_size_t,
+                                     VP]
+    lib.tts_rms_norm.restype = C.c_int
+    lib.tts_rms_norm.argtypes = [P(tts_norm_desc), I32, VP, I64, VP, VP, I64, VP]
     lib.tts_rope_tables.restype = C.c_int
     lib.tts_rope_tables.argtypes = [I32, C.c_double, I32, P(C.c_float), P(C.c_float)]
     lib.tts_paged_prefill_workspace_size.restype = C.c_size_t
@@ -489,6 +517,102 @@ def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_ne
         C.byref(desc), C.byref(rope) if rope is not None else None, num_seqs, num_tokens, _ptr(tok_offsets),
         _ptr(positions), qp, qs, kp, ks, vp, vs, _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens), num_blocks,
         _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+
+
+def make_head_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> tts_head_norm_desc:
+    """Head norms with device weights [head_dim] in the queries' type (which the caller keeps; None: ones)."""
+    return tts_head_norm_desc(float(eps), _ptr(q_weight), _ptr(k_weight))
+
+
+def tts_norm_rope_append_kv(desc: tts_attn_desc, norm: tts_head_norm_desc, num_seqs: int, num_tokens: int, k_new, v_new,
+                            block_tables, max_blocks_per_seq: int, seq_lens, num_blocks: int, k_cache, v_cache,
+                            k_scale=None, v_scale=None, rope: Optional[tts_rope_desc] = None, q=None, q_out=None,
+                            tok_offsets=None, positions=None, stream=None):
+    """Tensors as for tts_rope_append_kv."""
+    hq, hkv, d, size = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, 4 if desc.q_dtype == TTS_F32 else 2
+    qp, qs = _rows(q, hq, d, num_tokens, size)
+    kp, ks = _rows(k_new, hkv, d, num_tokens, size)
+    vp, vs = _rows(v_new, hkv, d, num_tokens, size)
+    _holds(q_out, num_tokens * hq * d * size, "q_out")
+    _check(load().tts_norm_rope_append_kv(
+        C.byref(desc), C.byref(norm) if norm is not None else None, C.byref(rope) if rope is not None else None, num_seqs,
+        num_tokens, _ptr(tok_offsets), _ptr(positions), qp, qs, kp, ks, vp, vs, _ptr(block_tables), max_blocks_per_seq,
+        _ptr(seq_lens), num_blocks, _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+        _stream(stream)))
+
+
+def _type(x) -> int:
+    return DTYPES[x] if isinstance(x, str) else int(x)
+
+
+def make_linear(in_features: int, out_features: int, dtype="bf16", out_dtype="bf16", act="none") -> tts_linear_desc:
+    return tts_linear_desc(in_features, out_features, _type(dtype), _type(out_dtype),
+                           ACTS[act] if isinstance(act, str) else int(act))
+
+
+def make_norm(row_len: int, eps: float = 1e-6, dtype="bf16", out_dtype="bf16") -> tts_norm_desc:
+    return tts_norm_desc(row_len, _type(dtype), _type(out_dtype), float(eps))
+
+
+def _matrix(x, rows: int, cols: int, dtype: int, name: str):
+    """(address, elements between rows) of a tensor [rows or more][cols] of a type, whose rows may lie apart; an
+    address is that of rows without gaps."""
+    if x is None or isinstance(x, int):
+        return x, cols
+    shape = x.shape
+    if len(shape) != 2 or shape[1] != cols or shape[0] < rows:
+        raise ValueError(f"{name}: expected [{rows}][{cols}], got {tuple(shape)}")
+    if x.itemsize != (4 if dtype == TTS_F32 else 2):
+        raise ValueError(f"{name}: elements of {x.dtype}")
+    row, col = x.stride()
+    if col != 1 and cols > 1 and shape[0]:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return x.data_ptr(), row if shape[0] > 1 else cols
+
+
+def tts_linear_workspace_size(desc: tts_linear_desc, num_rows: int) -> int:
+    return int(load().tts_linear_workspace_size(C.byref(desc), num_rows))
+
+
+def tts_gated_linear_workspace_size(desc: tts_linear_desc, num_rows: int) -> int:
+    return int(load().tts_gated_linear_workspace_size(C.byref(desc), num_rows))
+
+
+def tts_linear(desc: tts_linear_desc, num_rows: int, x, w, out, bias=None, residual=None, workspace=None,
+               workspace_bytes: int = 0, stream=None):
+    """x [num_rows][in], w [out][in], residual and out [num_rows][out], whose rows may lie apart; bias [out]."""
+    k, n, t, o = desc.in_features, desc.out_features, desc.dtype, desc.out_dtype
+    xp, xs = _matrix(x, num_rows, k, t, "x")
+    wp, ws = _matrix(w, n, k, t, "w")
+    rp, rs = _matrix(residual, num_rows, n, o, "residual")
+    op, os_ = _matrix(out, num_rows, n, o, "out")
+    _holds(bias, n * (4 if t == TTS_F32 else 2), "bias")
+    _check(load().tts_linear(C.byref(desc), num_rows, xp, xs, wp, ws, _ptr(bias), rp, rs, op, os_, _ptr(workspace),
+                             workspace_bytes, _stream(stream)))
+
+
+def tts_gated_linear(desc: tts_linear_desc, num_rows: int, x, w_gate, w_up, out, bias_gate=None, bias_up=None,
+                     workspace=None, workspace_bytes: int = 0, stream=None):
+    """x [num_rows][in], w_gate and w_up [out][in] (of one stride), out [num_rows][out]; biases [out]."""
+    k, n, t = desc.in_features, desc.out_features, desc.dtype
+    xp, xs = _matrix(x, num_rows, k, t, "x")
+    gp, gs = _matrix(w_gate, n, k, t, "w_gate")
+    up, us = _matrix(w_up, n, k, t, "w_up")
+    if gs != us:
+        raise ValueError("w_gate and w_up must have one row stride")
+    op, os_ = _matrix(out, num_rows, n, desc.out_dtype, "out")
+    for b, name in ((bias_gate, "bias_gate"), (bias_up, "bias_up")):
+        _holds(b, n * (4 if t == TTS_F32 else 2), name)
+    _check(load().tts_gated_linear(C.byref(desc), num_rows, xp, xs, gp, up, gs, _ptr(bias_gate), _ptr(bias_up), op, os_,
+                                   _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def tts_rms_norm(desc: tts_norm_desc, num_rows: int, x, weight, out, stream=None):
+    """x and out [num_rows][row_len], whose rows may lie apart; weight [row_len] or None."""
+    xp, xs = _matrix(x, num_rows, desc.row_len, desc.dtype, "x")
+    op, os_ = _matrix(out, num_rows, desc.row_len, desc.out_dtype, "out")
+    _holds(weight, desc.row_len * (4 if desc.dtype == TTS_F32 else 2), "weight")
+    _check(load().tts_rms_norm(C.byref(desc), num_rows, xp, xs, _ptr(weight), op, os_, _stream(stream)))
 
 
 def tts_paged_prefill_workspace_size(desc: tts_attn_desc, num_seqs: int, num_tokens: int, max_seq_len: int) -> int:
