@@ -15,18 +15,19 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
 LinearPlan linear_plan(int32_t rows, int32_t n, int32_t k_bytes, bool f32, bool gated, bool aligned) {
   LinearPlan r{};
-  const int planes = gated ? 2 : 1, total = ceil_div(k_bytes, kLinearChunk);
+  const int planes = gated ? 2 : 1;
   const int64_t cols = static_cast<int64_t>(n) * planes;
   int slots = 2 * kUnits;  // workgroups that run at once
-  if (rows <= kLinearFewRows) {
+  if (rows <= 64) {
     r.tile = 0;
     r.bm = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
-    r.bn = gated || n > 2048 ? 32 : 16;
+    r.bn = cols >= 8192 ? 64 : (gated || cols >= 4096 ? 32 : 16);
   } else {
     const bool wide = aligned && !f32 && static_cast<int64_t>(ceil_div(rows, 256)) * ceil_div(cols, 256) >= kUnits;
     r.tile = r.bm = r.bn = wide ? 256 : 128;
     if (wide) slots = kUnits;
   }
+  const int total = ceil_div(k_bytes, r.tile ? kLinearChunk : kThinChunk);
   const int64_t groups = static_cast<int64_t>(ceil_div(rows, r.bm)) * ceil_div(cols, r.bn);
   int64_t splits = groups >= slots ? 1 : slots / groups;
   if (splits > total / kLeast) splits = total / kLeast;
@@ -47,7 +48,7 @@ size_t linear_workspace(int32_t rows, int32_t n, int32_t k_bytes, bool f32, bool
     for (int aligned = 0; aligned < 2; ++aligned) {
       const LinearPlan plan = linear_plan(m, n, k_bytes, f32, gated, aligned != 0);
       if (plan.workspace > most) most = plan.workspace;
-      if (m > kLinearFewRows && plan.splits == 1) return most;
+      if (m > 64 && plan.splits == 1) return most;
     }
     if (m == rows) return most;
   }

@@ -22,12 +22,12 @@ struct LinearParams {
   int32_t k_bytes;                            // of one row of x or of the weights
   int32_t act;
   int32_t in_bf16, out_bf16;
-  int32_t splits, chunks;                     // parts of the inner dimension, 128-byte chunks to a part
+  int32_t splits, chunks;                     // parts of the inner dimension, chunks to a part
   int32_t m_tiles, n_tiles;
 };
 
-// How a product is launched: `tile` 0: few rows (weights straight into
-// registers, the inner dimension dealt to the waves), else tiles through LDS.
+// How a product is launched: `tile` 0: small tiles, whose workgroup deals the
+// inner dimension to its waves; 128 or 256: large tiles.
 struct LinearPlan {
   int tile;
   int bm, bn;  // rows of x and rows of weights to a workgroup
@@ -36,8 +36,8 @@ struct LinearPlan {
   size_t workspace;
 };
 
-constexpr int kLinearChunk = 128;    // bytes of a row to a step
-constexpr int kLinearFewRows = 64;   // most rows of the few-row kernel
+constexpr int kLinearChunk = 128;  // bytes of a row to a step of the large tiles
+constexpr int kThinChunk = 256;    // and of the small ones
 
 // `aligned`: every row of both operands starts at a multiple of 16 bytes.
 LinearPlan linear_plan(int32_t rows, int32_t n, int32_t k_bytes, bool f32, bool gated, bool aligned);

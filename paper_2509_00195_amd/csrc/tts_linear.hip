@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "tts_device.h"
 #include "tts_linear.h"
@@ -146,110 +147,7 @@ __device__ __forceinline__ void emit(const LinearParams& p, int split, int m, in
   if constexpr (GATED) store_part(p.part + part_at(p, split, 1, kPlanes, m, n), count, up);
 }
 
-// ---- few rows ----------------------------------------------------------------
-
-constexpr int kFewWaves = 8;
-constexpr int kFewThreads = 64 * kFewWaves;
-
-// MT tiles of 16 rows of x, NT tiles of 16 rows of weights (gated: the first
-// half gate, the second up, of the same columns). Bound by the weights'
-// bytes: each is read once, straight into registers, 128 bytes of a row at a
-// time. The workgroup's chunks of the inner dimension go to its waves in turn,
-// and the waves' sums are added in LDS in the order of the waves.
-template <typename E, int MT, int NT, bool GATED, int U>
-__global__ __launch_bounds__(kFewThreads) void few_rows_kernel(LinearParams p) {
-  __shared__ __attribute__((aligned(16))) f32x4 sums[kFewWaves][NT * MT][64];
-  const int wave = static_cast<int>(threadIdx.x) / 64, lane = static_cast<int>(threadIdx.x) % 64;
-  const int row = lane & 15, group = lane >> 4;
-  constexpr int kCols = (GATED ? NT / 2 : NT) * 16;
-  const int n0 = static_cast<int>(blockIdx.x) * kCols;
-  const char* wp[NT];
-  const char* xp[MT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int plane = GATED && t >= NT / 2, local = GATED ? t % (NT / 2) : t;
-    int n = n0 + 16 * local + row;
-    n = n < p.n ? n : p.n - 1;
-    wp[t] = static_cast<const char*>(p.w[plane]) + n * p.w_stride + 32 * group;
-  }
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    int m = 16 * t + row;
-    m = m < p.rows ? m : p.rows - 1;
-    xp[t] = static_cast<const char*>(p.x) + m * p.x_stride + 32 * group;
-  }
-  f32x4 acc[NT][MT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-#pragma unroll
-    for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int whole = p.k_bytes / kLinearChunk, total = (p.k_bytes + kLinearChunk - 1) / kLinearChunk;
-  const int first = static_cast<int>(blockIdx.y) * p.chunks;
-  const int end = first + p.chunks < total ? first + p.chunks : total;
-  const int full = end < whole ? end : whole;
-  int c = first + wave;
-  for (; c + (U - 1) * kFewWaves < full; c += U * kFewWaves) {
-    u32x4 a[U][NT][2], b[U][MT][2];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = static_cast<int64_t>(c + u * kFewWaves) * kLinearChunk;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) a[u][t][h] = *reinterpret_cast<const u32x4u*>(wp[t] + at + 16 * h);
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) b[u][t][h] = *reinterpret_cast<const u32x4u*>(xp[t] + at + 16 * h);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int j = 0; j < MT; ++j) acc[i][j] = mma<E>(a[u][i][h], b[u][j][h], acc[i][j]);
-  }
-  for (; c < end; c += kFewWaves) {
-    const int at = c * kLinearChunk, left = p.k_bytes - 32 * group;  // (bytes of the row from this lane's pointer)
-    u32x4 a[NT][2], b[MT][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) a[t][h] = load_piece<E>(wp[t], at + 16 * h, left);
-#pragma unroll
-      for (int t = 0; t < MT; ++t) b[t][h] = load_piece<E>(xp[t], at + 16 * h, left);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = mma<E>(a[i][h], b[j][h], acc[i][j]);
-  }
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-#pragma unroll
-    for (int j = 0; j < MT; ++j) sums[wave][i * MT + j][lane] = acc[i][j];
-  __syncthreads();
-  constexpr int kItems = (GATED ? NT / 2 : NT) * MT * 64;
-  for (int i = threadIdx.x; i < kItems; i += kFewThreads) {
-    const int l = i % 64, t = i / 64, m = 16 * (t % MT) + (l & 15);
-    if (m >= p.rows) continue;
-    f32x4 y = sums[0][t][l], up = y;
-#pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) y += sums[w][t][l];
-    if constexpr (GATED) {
-      up = sums[0][t + kItems / 64][l];
-#pragma unroll
-      for (int w = 1; w < kFewWaves; ++w) up += sums[w][t + kItems / 64][l];
-    }
-    emit<GATED>(p, static_cast<int>(blockIdx.y), m, n0 + 16 * (t / MT) + 4 * (l >> 4), y, up);
-  }
-}
-
-// ---- tiles -------------------------------------------------------------------
+// ---- loads into LDS ------------------------------------------------------------
 
 constexpr uint32_t kOutside = 0x80000000u;  // behind the end of every tile's buffer: reads as zero
 
@@ -271,15 +169,217 @@ struct Rows {
 #endif
 };
 
-// Waits for this wave's loads into LDS: a barrier behind it then means that all
-// waves' have landed (the barrier alone waits for none).
+// Waits for this wave's loads into LDS, but for the newest N: a barrier behind
+// it then means that all waves' have landed (the barrier alone waits for none).
+template <int N = 0>
 __device__ __forceinline__ void landed() {
+  static_assert(N < 64, "the counter's width");
   __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);  // vmcnt(N)
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// A barrier that waits for no load in flight (__syncthreads waits for all).
+// What a wave has read from LDS before it must have been used: the reads are
+// then over. The empty statements keep the compiler from moving memory
+// accesses across.
+__device__ __forceinline__ void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// f(integral_constant<int, 0>{}), ..., f(integral_constant<int, N - 1>{}).
+template <typename F, int... J>
+__device__ __forceinline__ void each(F f, std::integer_sequence<int, J...>) {
+  (f(std::integral_constant<int, J>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+  each(f, std::make_integer_sequence<int, N>{});
+}
+
 __device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
+
+// Position of a workgroup in the order of its XCD: workgroups go to the eight
+// XCDs in turn, and this gives each a run of consecutive tiles, whose shared
+// rows its L2 then serves.
+__device__ __forceinline__ int tile_of(int id, int tiles) {
+  const int per = tiles / 8, rest = tiles % 8, xcd = id % 8;
+  return xcd * per + (xcd < rest ? xcd : rest) + id / 8;
+}
+
+// ---- small tiles ---------------------------------------------------------------
+
+constexpr int kThinWaves = 4;
+constexpr int kThinThreads = 64 * kThinWaves;
+constexpr int kThinRow = kThinChunk;  // bytes of a row to a stage: a quarter to each wave
+
+// Few rows: bound by the weights' bytes and, where many workgroups read the
+// same rows of x, by what a compute unit draws from its L2. Tiles of BM rows
+// of x and BN rows of weights (gated: half gate, half up, of the same columns)
+// pass through S stages in LDS, S - 1 of them in flight, each row 256 bytes
+// long to a stage in 16 pieces of 16, piece c of row r at c ^ (r & 15). Every
+// wave multiplies the whole tile over its quarter of a stage's inner
+// dimension, so that each byte is read from LDS once; the waves' sums are
+// added at the end, in their order.
+template <typename E, int BM, int BN, int S, bool GATED, bool ALIGNED>
+__global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
+  constexpr int TM = BM / 16, TN = BN / 16, kPlanes = GATED ? 2 : 1, kCols = BN / kPlanes;
+  constexpr int kStage = (BM + BN) * kThinRow, kLoads = TM + TN;
+  static_assert(S >= 2 && S <= 8 && (ALIGNED || S == 2) && kLoads * (S - 2) < 64, "stages");
+  __shared__ __attribute__((aligned(16))) char s0[kStage], s1[kStage], s2[S > 2 ? kStage : 16], s3[S > 3 ? kStage : 16],
+      s4[S > 4 ? kStage : 16], s5[S > 5 ? kStage : 16], s6[S > 6 ? kStage : 16], s7[S > 7 ? kStage : 16];
+  // (An array each, not one: the compiler then knows which of them a load writes.)
+  const auto stage = [&](auto i) -> char* {
+    constexpr int k = decltype(i)::value % S;
+    if constexpr (k == 0) return s0;
+    else if constexpr (k == 1) return s1;
+    else if constexpr (k == 2) return s2;
+    else if constexpr (k == 3) return s3;
+    else if constexpr (k == 4) return s4;
+    else if constexpr (k == 5) return s5;
+    else if constexpr (k == 6) return s6;
+    else return s7;
+  };
+  const int wave = static_cast<int>(threadIdx.x) / 64, lane = static_cast<int>(threadIdx.x) % 64;
+  const int id = tile_of(static_cast<int>(blockIdx.x), p.m_tiles * p.n_tiles), split = static_cast<int>(blockIdx.y);
+  const int m0 = id % p.m_tiles * BM, n0 = id / p.m_tiles * kCols;
+  const int total = (p.k_bytes + kThinRow - 1) / kThinRow;
+  const int first = split * p.chunks, end = first + p.chunks < total ? first + p.chunks : total;
+  const int stop = end == total ? p.k_bytes : end * kThinRow;
+
+  // A load takes four rows to a wave, sixteen to the workgroup.
+  const int sub = wave * 4 + (lane >> 4), piece = (lane & 15) ^ sub;
+  const int rows_m = least(p.rows - m0, BM), rows_n = least(p.n - n0, kCols);
+  const char* xb = static_cast<const char*>(p.x) + m0 * p.x_stride;
+  const char* wb[kPlanes];
+  Rows xr, wr[kPlanes];
+  xr.set(xb, static_cast<uint32_t>((rows_m - 1) * p.x_stride + p.k_bytes));
+#pragma unroll
+  for (int i = 0; i < kPlanes; ++i) {
+    wb[i] = static_cast<const char*>(p.w[i]) + n0 * p.w_stride;
+    wr[i].set(wb[i], static_cast<uint32_t>((rows_n - 1) * p.w_stride + p.k_bytes));
+  }
+  const uint32_t off_n = static_cast<uint32_t>(sub * p.w_stride + 16 * piece);
+  const uint32_t off_m = static_cast<uint32_t>(sub * p.x_stride + 16 * piece);
+  constexpr int kTilesN = TN / kPlanes;  // of a plane
+  u32x4 held[ALIGNED ? 1 : kLoads];
+
+  // Chunk c into a stage (not aligned: into registers, for put()).
+  const auto start = [&](char* to, int c) {
+    const int at = c * kThinRow;
+    if constexpr (ALIGNED) {
+      const bool out = at + 16 * piece >= stop;
+      const uint32_t from_n = out ? kOutside : off_n, from_m = out ? kOutside : off_m;
+      const uint32_t step_n = static_cast<uint32_t>(16 * p.w_stride), step_m = static_cast<uint32_t>(16 * p.x_stride);
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+        wr[i / kTilesN].load(to + (i * 16 + wave * 4) * kThinRow, from_n + (i % kTilesN) * step_n, at);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) xr.load(to + (BN + i * 16 + wave * 4) * kThinRow, from_m + i * step_m, at);
+    } else {
+      const auto fetch = [&](auto whole) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const bool is_x = i >= TN;
+          const int row = is_x ? least((i - TN) * 16 + sub, rows_m - 1) : least(i % kTilesN * 16 + sub, rows_n - 1);
+          const char* src = is_x ? xb + row * p.x_stride : wb[is_x ? 0 : i / kTilesN] + row * p.w_stride;
+          if constexpr (whole.value)
+            held[i] = *reinterpret_cast<const u32x4u*>(src + at + 16 * piece);
+          else
+            held[i] = load_piece<E>(src, at + 16 * piece, stop);
+        }
+      };
+      if (at + kThinRow <= stop)
+        fetch(std::true_type{});
+      else
+        fetch(std::false_type{});
+    }
+  };
+  const auto put = [&](char* to) {
+#pragma unroll
+    for (int i = 0; i < (ALIGNED ? 0 : kLoads); ++i)
+      *reinterpret_cast<u32x4*>(to + (i * 16 + wave * 4) * kThinRow + lane * 16) = held[i];
+  };
+
+  const int row = lane & 15, group = lane >> 4;
+  f32x4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int from = row * kThinRow + ((4 * wave + group) ^ row) * 16;
+  const auto multiply = [&](const char* at) {
+    u32x4 a[TN], b[TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i) a[i] = *reinterpret_cast<const u32x4*>(at + from + i * 16 * kThinRow);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) b[j] = *reinterpret_cast<const u32x4*>(at + from + (BN + j * 16) * kThinRow);
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) acc[i][j] = mma<E>(a[i], b[j], acc[i][j]);
+  };
+
+  // Stage j's chunk has landed once all but the S - 2 newer ones have; behind
+  // the barrier the stage read before it is free for the chunk S - 1 further
+  // on. Chunks behind the end load nothing and are zero.
+  if constexpr (ALIGNED) {
+    each<S - 1>([&](auto j) { start(stage(j), first + decltype(j)::value); });
+  } else {
+    start(s0, first);
+  }
+  const auto step = [&](auto j, int c) {
+    constexpr int k = decltype(j)::value;
+    if constexpr (ALIGNED) {
+      landed<kLoads*(S - 2)>();
+      barrier();
+    } else {
+      put(stage(j));
+      __syncthreads();
+    }
+    start(stage(std::integral_constant<int, k + S - 1>{}), c + (ALIGNED ? S - 1 : 1));
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(stage(j));
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int c = first; c < end; c += S)
+    each<S>([&](auto j) { step(j, c + decltype(j)::value); });
+
+  // The waves' sums, [wave][tile][lane], then whole runs of columns.
+  static_assert(kThinWaves * TN * TM * 1024 <= S * kStage, "the sums' place");
+  landed();
+  __syncthreads();
+  constexpr int kSums = kStage / 1024;  // tiles of sums to a stage
+  const auto sum_at = [&](int i) {  // (wave * tiles + tile)
+    const int k = i / kSums;
+    char* at = k == 0 ? s0 : k == 1 ? s1 : k == 2 ? s2 : s3;
+    return reinterpret_cast<f32x4*>(at + i % kSums * 1024);
+  };
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) sum_at(wave * TN * TM + i * TM + j)[lane] = acc[i][j];
+  __syncthreads();
+  constexpr int kQuads = kCols / 4;
+#pragma nounroll
+  for (int i = threadIdx.x; i < BM * kQuads; i += kThinThreads) {
+    const int r = i / kQuads, q = i % kQuads, l = (r & 15) + 16 * (q & 3), t = q / 4 * TM + r / 16;
+    f32x4 y = sum_at(t)[l], up = y;
+#pragma unroll
+    for (int w = 1; w < kThinWaves; ++w) y += sum_at(w * TN * TM + t)[l];
+    if constexpr (GATED) {
+      up = sum_at(t + kTilesN * TM)[l];
+#pragma unroll
+      for (int w = 1; w < kThinWaves; ++w) up += sum_at(w * TN * TM + t + kTilesN * TM)[l];
+    }
+    emit<GATED>(p, split, m0 + r, n0 + 4 * q, y, up);
+  }
+}
+
+// ---- tiles -------------------------------------------------------------------
 
 // A tile's rows lie in LDS 128 bytes each, in eight pieces of 16 whose places
 // are permuted by the row (piece c of row r at c ^ (r & 7)), so that the same
@@ -298,14 +398,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   __shared__ __attribute__((aligned(16))) char stage1[kStage];
   const int wave = static_cast<int>(threadIdx.x) / 64, lane = static_cast<int>(threadIdx.x) % 64;
 
-  // Tiles in groups of 8 along x's rows; consecutive ones on one XCD, whose L2
-  // then serves the group's shared rows.
-  int id = static_cast<int>(blockIdx.x);
-  const int tiles = p.m_tiles * p.n_tiles;
-  {
-    const int per = tiles / 8, rest = tiles % 8, xcd = id % 8, nth = id / 8;
-    id = xcd * per + (xcd < rest ? xcd : rest) + nth;
-  }
+  // Tiles in groups of 8 along x's rows.
+  const int id = tile_of(static_cast<int>(blockIdx.x), p.m_tiles * p.n_tiles);
   constexpr int kGroup = 8;
   const int in_group = kGroup * p.n_tiles, g0 = id / in_group * kGroup;
   const int height = p.m_tiles - g0 < kGroup ? p.m_tiles - g0 : kGroup;
@@ -579,22 +673,45 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
 }  // namespace
 
-template <typename E, bool GATED>
-static void launch_few(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(p.n_tiles), static_cast<unsigned>(p.splits)), block(kFewThreads);
-#define TTS_FEW(MT, NT, U) hipLaunchKernelGGL((few_rows_kernel<E, MT, NT, GATED, U>), grid, block, 0, stream, p)
+// Stages of a small tile: as many as leave room for two workgroups on a
+// compute unit (160 KB of LDS), at most eight.
+template <int BM, int BN>
+constexpr int thin_stages() {
+  constexpr int n = 78 * 1024 / ((BM + BN) * kThinChunk);
+  return n > 8 ? 8 : n;
+}
+
+template <typename E, bool GATED, bool ALIGNED, int BM>
+static void launch_thin_m(const LinearParams& p, int bn, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles), static_cast<unsigned>(p.splits)), block(kThinThreads);
+#define TTS_THIN(BN) \
+  hipLaunchKernelGGL((thin_kernel<E, BM, BN, ALIGNED ? thin_stages<BM, BN>() : 2, GATED, ALIGNED>), grid, block, 0, stream, p)
+  if (bn == 64) {
+    TTS_THIN(64);
+    return;
+  }
   if constexpr (!GATED) {
-    if (plan.bn == 16) {
-      if (plan.bm == 16) TTS_FEW(1, 1, 4);
-      else if (plan.bm == 32) TTS_FEW(2, 1, 4);
-      else TTS_FEW(4, 1, 2);
+    if (bn == 48) {
+      TTS_THIN(48);
+      return;
+    }
+    if (bn == 16) {
+      TTS_THIN(16);
       return;
     }
   }
-  if (plan.bm == 16) TTS_FEW(1, 2, 4);
-  else if (plan.bm == 32) TTS_FEW(2, 2, 2);
-  else TTS_FEW(4, 2, 2);
-#undef TTS_FEW
+  TTS_THIN(32);
+#undef TTS_THIN
+}
+
+template <typename E, bool GATED, bool ALIGNED>
+static void launch_thin(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
+  if (plan.bm == 16)
+    launch_thin_m<E, GATED, ALIGNED, 16>(p, plan.bn, stream);
+  else if (plan.bm == 32)
+    launch_thin_m<E, GATED, ALIGNED, 32>(p, plan.bn, stream);
+  else
+    launch_thin_m<E, GATED, ALIGNED, 64>(p, plan.bn, stream);
 }
 
 template <typename E, bool GATED, bool ALIGNED>
@@ -615,8 +732,10 @@ static hipError_t launch_linear_t(LinearParams p, const LinearPlan& plan, bool a
   p.chunks = plan.chunks;
   p.m_tiles = ceil_div(p.rows, plan.bm);
   p.n_tiles = ceil_div(static_cast<int64_t>(p.n) * (GATED ? 2 : 1), plan.bn);
-  if (plan.tile == 0)
-    launch_few<E, GATED>(p, plan, stream);
+  if (plan.tile == 0 && aligned)
+    launch_thin<E, GATED, true>(p, plan, stream);
+  else if (plan.tile == 0)
+    launch_thin<E, GATED, false>(p, plan, stream);
   else if (aligned)
     launch_tiles<E, GATED, true>(p, plan, stream);
   else
