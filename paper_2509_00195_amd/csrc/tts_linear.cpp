@@ -24,7 +24,8 @@ LinearPlan linear_plan(int32_t rows, int32_t n, int32_t k_bytes, bool f32, bool 
     r.bn = cols >= 8192 ? 64 : (gated || cols >= 4096 ? 32 : 16);
   } else {
     const bool wide = aligned && !f32 && static_cast<int64_t>(ceil_div(rows, 256)) * ceil_div(cols, 256) >= kUnits;
-    r.tile = r.bm = r.bn = wide ? 256 : 128;
+    r.bm = r.bn = wide ? 256 : 128;
+    r.tile = 2;
     if (wide) slots = kUnits;
   }
   const int total = ceil_div(k_bytes, r.tile ? kLinearChunk : kThinChunk);

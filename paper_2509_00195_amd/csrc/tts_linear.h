@@ -27,7 +27,7 @@ struct LinearParams {
 };
 
 // How a product is launched: `tile` 0: small tiles, whose workgroup deals the
-// inner dimension to its waves; 128 or 256: large tiles.
+// inner dimension to its waves; else large tiles, of so many stages.
 struct LinearPlan {
   int tile;
   int bm, bn;  // rows of x and rows of weights to a workgroup

@@ -200,13 +200,16 @@ __device__ __forceinline__ void each(F f) {
   each(f, std::make_integer_sequence<int, N>{});
 }
 
+// (One value to the wave, which the compiler then keeps in a scalar register.)
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / 64); }
+
 __device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
 
-// Position of a workgroup in the order of its XCD: workgroups go to the eight
-// XCDs in turn, and this gives each a run of consecutive tiles, whose shared
-// rows its L2 then serves.
-__device__ __forceinline__ int tile_of(int id, int tiles) {
-  const int per = tiles / 8, rest = tiles % 8, xcd = id % 8;
+// Place of a workgroup in the order of the tiles (those of the first split,
+// then of the next): workgroups go to the eight XCDs in turn, and this gives
+// each a run of consecutive tiles, whose shared rows its L2 then serves.
+__device__ __forceinline__ int place_of(int id, int places) {
+  const int per = places / 8, rest = places % 8, xcd = id % 8;
   return xcd * per + (xcd < rest ? xcd : rest) + id / 8;
 }
 
@@ -243,8 +246,9 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
     else if constexpr (k == 6) return s6;
     else return s7;
   };
-  const int wave = static_cast<int>(threadIdx.x) / 64, lane = static_cast<int>(threadIdx.x) % 64;
-  const int id = tile_of(static_cast<int>(blockIdx.x), p.m_tiles * p.n_tiles), split = static_cast<int>(blockIdx.y);
+  const int wave = wave_id(), lane = static_cast<int>(threadIdx.x) % 64;
+  const int tiles = p.m_tiles * p.n_tiles, place = place_of(static_cast<int>(blockIdx.x), tiles * p.splits);
+  const int id = place % tiles, split = place / tiles;
   const int m0 = id % p.m_tiles * BM, n0 = id / p.m_tiles * kCols;
   const int total = (p.k_bytes + kThinRow - 1) / kThinRow;
   const int first = split * p.chunks, end = first + p.chunks < total ? first + p.chunks : total;
@@ -386,7 +390,7 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
 // piece of 16 rows, which a matrix operand reads, is spread over the banks. The
 // LDS side of a load into LDS is fixed (lane after lane), so the lanes' global
 // addresses carry the permutation.
-template <typename E, int BM, int BN, int WM, int WN, bool GATED, bool ALIGNED>
+template <typename E, int BM, int BN, int WM, int WN, int S, bool GATED, bool ALIGNED>
 __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 tiles of a wave
@@ -394,18 +398,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   constexpr int kLoadsN = BN / 8 / kWaves, kLoadsM = BM / 8 / kWaves;
   constexpr int kPlanes = GATED ? 2 : 1;
   constexpr int kCols = BN / kPlanes;
-  __shared__ __attribute__((aligned(16))) char stage0[kStage];
-  __shared__ __attribute__((aligned(16))) char stage1[kStage];
-  const int wave = static_cast<int>(threadIdx.x) / 64, lane = static_cast<int>(threadIdx.x) % 64;
+  static_assert(S >= 2 && S <= 4 && (ALIGNED || S == 2), "stages");
+  __shared__ __attribute__((aligned(16))) char stage0[kStage], stage1[kStage], stage2[S > 2 ? kStage : 16],
+      stage3[S > 3 ? kStage : 16];
+  const auto stage_of = [&](auto i) -> char* {
+    constexpr int k = decltype(i)::value % S;
+    if constexpr (k == 0) return stage0;
+    else if constexpr (k == 1) return stage1;
+    else if constexpr (k == 2) return stage2;
+    else return stage3;
+  };
+  const int wave = wave_id(), lane = static_cast<int>(threadIdx.x) % 64;
 
   // Tiles in groups of 8 along x's rows.
-  const int id = tile_of(static_cast<int>(blockIdx.x), p.m_tiles * p.n_tiles);
+  const int tiles = p.m_tiles * p.n_tiles, spot = place_of(static_cast<int>(blockIdx.x), tiles * p.splits);
+  const int id = spot % tiles, split = spot / tiles;
   constexpr int kGroup = 8;
   const int in_group = kGroup * p.n_tiles, g0 = id / in_group * kGroup;
   const int height = p.m_tiles - g0 < kGroup ? p.m_tiles - g0 : kGroup;
   const int m0 = (g0 + id % in_group % height) * BM, n0 = id % in_group / height * kCols;
 
-  const int split = static_cast<int>(blockIdx.y);
   const int total = (p.k_bytes + kLinearChunk - 1) / kLinearChunk;
   const int first = split * p.chunks, end = first + p.chunks < total ? first + p.chunks : total;
   const int stop = end == total ? p.k_bytes : end * kLinearChunk;  // of a row's bytes
@@ -431,27 +443,27 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   const uint32_t off_m = static_cast<uint32_t>(row_m(0) * p.x_stride + 16 * piece);
   u32x4 held[ALIGNED ? 1 : kLoadsN + kLoadsM];
 
-  // Starts the loads of chunk c (aligned: into LDS; else into registers, for put()).
-  auto start = [&](char* stage, int c) {
+  // Load i of chunk c (aligned: into LDS; else into registers, for put()).
+  constexpr int kLoads = kLoadsN + kLoadsM, kLoadsPlane = kLoadsN / kPlanes;
+  const uint32_t step_n = static_cast<uint32_t>(kStep * p.w_stride), step_m = static_cast<uint32_t>(kStep * p.x_stride);
+  const auto load = [&](char* stage, int c, int i) {
     const int at = c * kLinearChunk;
     if constexpr (ALIGNED) {
       const bool out = at + 16 * piece >= stop;
-      const uint32_t from_n = out ? kOutside : off_n, from_m = out ? kOutside : off_m;
-      const uint32_t step_n = static_cast<uint32_t>(kStep * p.w_stride), step_m = static_cast<uint32_t>(kStep * p.x_stride);
-#pragma unroll
-      for (int i = 0; i < kLoadsN; ++i)
-        wr[i / (kLoadsN / kPlanes)].load(stage + (i * kWaves + wave) * 1024, from_n + (i % (kLoadsN / kPlanes)) * step_n, at);
-#pragma unroll
-      for (int i = 0; i < kLoadsM; ++i)
-        xr.load(stage + BN * kLinearChunk + (i * kWaves + wave) * 1024, from_m + i * step_m, at);
+      if (i < kLoadsN)
+        wr[i / kLoadsPlane].load(stage + (i * kWaves + wave) * 1024, (out ? kOutside : off_n) + i % kLoadsPlane * step_n, at);
+      else
+        xr.load(stage + (i * kWaves + wave) * 1024, (out ? kOutside : off_m) + (i - kLoadsN) * step_m, at);
     } else {
-#pragma unroll
-      for (int i = 0; i < kLoadsN; ++i)
-        held[i] = load_piece<E>(wb[i / (kLoadsN / kPlanes)] + least(row_n(i), rows_n - 1) * p.w_stride, at + 16 * piece, stop);
-#pragma unroll
-      for (int i = 0; i < kLoadsM; ++i)
-        held[kLoadsN + i] = load_piece<E>(xb + least(row_m(i), rows_m - 1) * p.x_stride, at + 16 * piece, stop);
+      const char* src = i < kLoadsN ? wb[i / kLoadsPlane] + least(row_n(i), rows_n - 1) * p.w_stride
+                                    : xb + least(row_m(i - kLoadsN), rows_m - 1) * p.x_stride;
+      held[i] = at + kLinearChunk <= stop ? *reinterpret_cast<const u32x4u*>(src + at + 16 * piece)
+                                          : load_piece<E>(src, at + 16 * piece, stop);
     }
+  };
+  const auto start = [&](char* stage, int c) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(stage, c, i);
   };
   auto put = [&](char* stage) {
     if constexpr (!ALIGNED) {
@@ -471,63 +483,95 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
 #pragma unroll
     for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   struct Operands {
-    u32x4 a[TN], b[TM];
+    u32x4 v[TN + TM];
+  } lo, hi;
+  // This lane's place in the first step's operands; the second's is 64 bytes
+  // on, before the permutation. It is made anew for each step (the compiler
+  // would keep one in registers for every stage and step, and spill them).
+  const int from = row * kLinearChunk + (group ^ (row & 7)) * 16;
+  const auto operands_at = [&](int step) {
+    int at = from;
+    asm volatile("" : "+v"(at));
+    return at ^ (64 * step);
   };
-  auto read = [&](const char* stage, int step) {
-    Operands o;
-    const char* at = stage + row * kLinearChunk + ((4 * step + group) ^ (row & 7)) * 16;
+  // Operand t of a step: tiles of weights, then of x.
+  const auto read = [&](const char* at, Operands& o, int t) {
+    int r;
+    if (t >= TN)
+      r = BN + (wm * TM + t - TN) * 16;
+    else if (GATED)
+      r = (t >= TN / 2 ? kCols : 0) + wn * (TN / 2 * 16) + t % (TN / 2) * 16;
+    else
+      r = (wn * TN + t) * 16;
+    o.v[t] = *reinterpret_cast<const u32x4*>(at + r * kLinearChunk);
+  };
+  // A step's products, with other(0) .. other(others - 1) between the first of them.
+  constexpr int kProducts = TN * TM, kRate = (TN + TM + kLoads + kProducts - 1) / kProducts;
+  const auto multiply = [&](const Operands& o, int others, auto other) {
 #pragma unroll
-    for (int t = 0; t < TN; ++t) {
-      const int r = GATED ? (t >= TN / 2 ? kCols : 0) + wn * (TN / 2 * 16) + t % (TN / 2) * 16 : (wn * TN + t) * 16;
-      o.a[t] = *reinterpret_cast<const u32x4*>(at + r * kLinearChunk);
+    for (int q = 0; q < kProducts; ++q) {
+      acc[q / TM][q % TM] = mma<E>(o.v[q / TM], o.v[TN + q % TM], acc[q / TM][q % TM]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = q * kRate; t < (q + 1) * kRate && t < others; ++t) other(t);
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int t = 0; t < TM; ++t) o.b[t] = *reinterpret_cast<const u32x4*>(at + (BN + (wm * TM + t) * 16) * kLinearChunk);
-    return o;
-  };
-  auto multiply = [&](const Operands& o) {
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-      for (int j = 0; j < TM; ++j) acc[i][j] = mma<E>(o.a[i], o.b[j], acc[i][j]);
   };
 
   // Each chunk is two steps. The first step's operands of a chunk are read
   // while the second of the chunk before it is multiplied; the one barrier per
-  // chunk lies between: all waves have read the chunk, and the next one's
-  // loads, started a chunk ago, have landed. Chunks behind the end load
-  // nothing and are zero, so that the loop holds no branch.
-  start(stage0, first);
-  put(stage0);
-  landed();
-  __syncthreads();
-  start(stage1, first + 1);
-  Operands lo = read(stage0, 0), hi;
+  // chunk lies between: all waves have read the chunk, whose stage takes the
+  // loads of the chunk S further on, and the next chunk's loads have landed.
+  // What is loaded and read stands between the products one by one (all at the
+  // start of a step, the loads' issue held the products up: 8192 x 14336 x 3584
+  // 722 -> 697 us). Chunks behind the end load nothing and are zero, so that the
+  // loop holds no branch.
+  if constexpr (ALIGNED) {
+    each<S>([&](auto j) { start(stage_of(j), first + decltype(j)::value); });
+    landed<kLoads*(S - 1)>();
+    barrier();
+  } else {
+    start(stage0, first);
+    put(stage0);
+    __syncthreads();
+    start(stage1, first + 1);
+  }
+#pragma unroll
+  for (int t = 0; t < TN + TM; ++t) read(stage0 + from, lo, t);
   const auto chunk = [&](char* cur, char* next, int c) {
     __builtin_amdgcn_sched_barrier(0);
-    hi = read(cur, 1);
+    const char* at_hi = cur + operands_at(1);
+    multiply(lo, TN + TM, [&](int t) { read(at_hi, hi, t); });
     __builtin_amdgcn_sched_barrier(0);
-    multiply(lo);
-    __builtin_amdgcn_sched_barrier(0);
-    put(next);
-    landed();
-    __syncthreads();
-    start(cur, c + 2);
-    lo = read(next, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(hi);
+    if constexpr (ALIGNED) {
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the second step's operands
+      landed<kLoads*(S - 2)>();
+      barrier();
+    } else {
+      put(next);
+      __syncthreads();
+    }
+    const char* at_lo = next + operands_at(0);
+    multiply(hi, TN + TM + kLoads, [&](int t) {
+      if (t < kLoads)
+        load(cur, c + S, t);
+      else
+        read(at_lo, lo, t - kLoads);
+    });
   };
-  for (int c = first; c < end; c += 2) {
-    chunk(stage0, stage1, c);
-    chunk(stage1, stage0, c + 1);
-  }
+  for (int c = first; c < end; c += S)
+    each<S>([&](auto j) {
+      constexpr int k = decltype(j)::value;
+      chunk(stage_of(j), stage_of(std::integral_constant<int, k + 1>{}), c + k);
+    });
 
   // The sums go through LDS, two tiles of rows at a time, so that what is
   // written is whole runs of columns (and the code of the activations stands
   // once per pass).
   constexpr int kWidth = TN * 4, kQuads = GATED ? kWidth / 2 : kWidth;  // four columns each
-  static_assert(kWaves * 32 * kWidth * 16 <= kStage && (kWidth & (kWidth - 1)) == 0, "a wave's part of a stage");
-  f32x4* const tile = reinterpret_cast<f32x4*>(stage0) + wave * (32 * kWidth);
+  constexpr int kPart = 32 * kWidth * 16, kParts = kStage / kPart;  // bytes of a wave's tiles, waves to a stage
+  static_assert(kWaves <= 2 * kParts && (kWidth & (kWidth - 1)) == 0, "the waves' parts of two stages");
+  f32x4* const tile = reinterpret_cast<f32x4*>((wave < kParts ? stage0 : stage1) + wave % kParts * kPart);
   const auto place = [&](int r, int q) { return tile + r * kWidth + (q ^ (r & (kWidth - 1))); };  // (spread over the banks)
 #pragma unroll
   for (int j = 0; j < TM; j += 2) {
@@ -681,49 +725,55 @@ constexpr int thin_stages() {
   return n > 8 ? 8 : n;
 }
 
-template <typename E, bool GATED, bool ALIGNED, int BM>
-static void launch_thin_m(const LinearParams& p, int bn, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles), static_cast<unsigned>(p.splits)), block(kThinThreads);
-#define TTS_THIN(BN) \
-  hipLaunchKernelGGL((thin_kernel<E, BM, BN, ALIGNED ? thin_stages<BM, BN>() : 2, GATED, ALIGNED>), grid, block, 0, stream, p)
-  if (bn == 64) {
-    TTS_THIN(64);
-    return;
+template <typename E, bool GATED, bool ALIGNED>
+static hipError_t launch_thin(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles * p.splits));
+#define TTS_THIN(BM, BN)                                                                                            \
+  if (plan.bm == BM && plan.bn == BN) {                                                                             \
+    hipLaunchKernelGGL((thin_kernel<E, BM, BN, ALIGNED ? thin_stages<BM, BN>() : 2, GATED, ALIGNED>), grid,          \
+                       dim3(kThinThreads), 0, stream, p);                                                            \
+    return hipGetLastError();                                                                                        \
   }
   if constexpr (!GATED) {
-    if (bn == 48) {
-      TTS_THIN(48);
-      return;
-    }
-    if (bn == 16) {
-      TTS_THIN(16);
-      return;
-    }
+    TTS_THIN(16, 16)
+    TTS_THIN(32, 16)
+    TTS_THIN(64, 16)
+    TTS_THIN(16, 48)
+    TTS_THIN(32, 48)
+    TTS_THIN(64, 48)
   }
-  TTS_THIN(32);
+  TTS_THIN(16, 32)
+  TTS_THIN(32, 32)
+  TTS_THIN(64, 32)
+  TTS_THIN(16, 64)
+  TTS_THIN(32, 64)
+  TTS_THIN(64, 64)
 #undef TTS_THIN
+  return hipErrorInvalidValue;
 }
 
+// (A plan whose tile has no kernel is refused: a grid counted in other tiles
+// than the kernel's would leave the operands.)
 template <typename E, bool GATED, bool ALIGNED>
-static void launch_thin(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
-  if (plan.bm == 16)
-    launch_thin_m<E, GATED, ALIGNED, 16>(p, plan.bn, stream);
-  else if (plan.bm == 32)
-    launch_thin_m<E, GATED, ALIGNED, 32>(p, plan.bn, stream);
-  else
-    launch_thin_m<E, GATED, ALIGNED, 64>(p, plan.bn, stream);
-}
-
-template <typename E, bool GATED, bool ALIGNED>
-static void launch_tiles(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles), static_cast<unsigned>(p.splits));
-  if constexpr (ALIGNED && sizeof(E) == 2) {
-    if (plan.tile == 256) {
-      hipLaunchKernelGGL((tile_kernel<E, 256, 256, 2, 4, GATED, true>), grid, dim3(512), 0, stream, p);
-      return;
-    }
+static hipError_t launch_tiles(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles * p.splits));
+#define TTS_TILE(BM, BN, WM, WN, S)                                                                               \
+  if (plan.bm == BM && plan.bn == BN && plan.tile == S) {                                                        \
+    hipLaunchKernelGGL((tile_kernel<E, BM, BN, WM, WN, S, GATED, ALIGNED>), grid, dim3(64 * WM * WN), 0, stream, p); \
+    return hipGetLastError();                                                                                     \
   }
-  hipLaunchKernelGGL((tile_kernel<E, 128, 128, 2, 2, GATED, ALIGNED>), grid, dim3(256), 0, stream, p);
+  TTS_TILE(128, 128, 2, 2, 2)
+  if constexpr (ALIGNED && sizeof(E) == 2) {
+    TTS_TILE(256, 256, 2, 4, 2)
+    TTS_TILE(256, 128, 4, 2, 3)
+    TTS_TILE(128, 256, 2, 4, 3)
+    TTS_TILE(128, 128, 2, 2, 4)
+    TTS_TILE(128, 128, 2, 2, 3)
+    TTS_TILE(64, 128, 1, 4, 3)
+    TTS_TILE(128, 64, 4, 1, 3)
+  }
+#undef TTS_TILE
+  return hipErrorInvalidValue;
 }
 
 template <typename E, bool GATED>
@@ -732,15 +782,11 @@ static hipError_t launch_linear_t(LinearParams p, const LinearPlan& plan, bool a
   p.chunks = plan.chunks;
   p.m_tiles = ceil_div(p.rows, plan.bm);
   p.n_tiles = ceil_div(static_cast<int64_t>(p.n) * (GATED ? 2 : 1), plan.bn);
-  if (plan.tile == 0 && aligned)
-    launch_thin<E, GATED, true>(p, plan, stream);
-  else if (plan.tile == 0)
-    launch_thin<E, GATED, false>(p, plan, stream);
-  else if (aligned)
-    launch_tiles<E, GATED, true>(p, plan, stream);
+  hipError_t e;
+  if (plan.tile == 0)
+    e = aligned ? launch_thin<E, GATED, true>(p, plan, stream) : launch_thin<E, GATED, false>(p, plan, stream);
   else
-    launch_tiles<E, GATED, false>(p, plan, stream);
-  hipError_t e = hipGetLastError();
+    e = aligned ? launch_tiles<E, GATED, true>(p, plan, stream) : launch_tiles<E, GATED, false>(p, plan, stream);
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t items = static_cast<int64_t>((p.n + 3) / 4) * p.rows;
   hipLaunchKernelGGL(join_kernel<GATED>, dim3(static_cast<unsigned>((items + kJoinThreads - 1) / kJoinThreads)),
