@@ -994,7 +994,7 @@ static tts_status check_linear(const tts_linear_desc* d) {
 static size_t linear_size(const tts_linear_desc* d, int32_t num_rows, bool gated) {
   if (check_linear(d) != TTS_OK || num_rows <= 0) return 0;
   const bool f32 = d->dtype == TTS_F32;
-  return tts::linear_workspace(num_rows, d->out_features, d->in_features * (f32 ? 4 : 2), f32, gated);
+  return tts::linear_workspace(num_rows, d->out_features, d->in_features * (f32 ? 4 : 2), gated);
 }
 
 size_t tts_linear_workspace_size(const tts_linear_desc* d, int32_t num_rows) { return linear_size(d, num_rows, false); }

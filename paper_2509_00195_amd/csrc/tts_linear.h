@@ -26,8 +26,9 @@ struct LinearParams {
   int32_t m_tiles, n_tiles;
 };
 
-// How a product is launched: `tile` 0: small tiles, whose workgroup deals the
-// inner dimension to its waves; else large tiles, of so many stages.
+// How a product is launched. tile 0: small tiles, whose workgroup deals the
+// inner dimension to its waves; else large tiles, x's and the weights' stages
+// as two digits.
 struct LinearPlan {
   int tile;
   int bm, bn;  // rows of x and rows of weights to a workgroup
@@ -39,11 +40,24 @@ struct LinearPlan {
 constexpr int kLinearChunk = 128;  // bytes of a row to a step of the large tiles
 constexpr int kThinChunk = 256;    // and of the small ones
 
+// The small tiles that there are. (64 x 48 has no third stage, and was slower
+// than 64 x 32 at every size; 64 x 16 was nowhere the best.)
+constexpr bool thin_has(int bm, int bn, bool gated) {
+  return gated ? bn == 32 || bn == 64 : bn == 32 || bn == 64 || bm < 64;
+}
+
+// Their stages: as many as leave room for two workgroups on a compute unit
+// (160 KB of LDS), at most eight.
+constexpr int thin_stages(int bm, int bn) {
+  const int n = 78 * 1024 / ((bm + bn) * kThinChunk);
+  return n > 8 ? 8 : n;
+}
+
 // `aligned`: every row of both operands starts at a multiple of 16 bytes.
 LinearPlan linear_plan(int32_t rows, int32_t n, int32_t k_bytes, bool f32, bool gated, bool aligned);
 
-// The most that a call of up to `rows` rows needs.
-size_t linear_workspace(int32_t rows, int32_t n, int32_t k_bytes, bool f32, bool gated);
+// What a call of up to `rows` rows needs at most.
+size_t linear_workspace(int32_t rows, int32_t n, int32_t k_bytes, bool gated);
 
 struct RmsParams {
   const void* x;

@@ -200,6 +200,16 @@ __device__ __forceinline__ void each(F f) {
   each(f, std::make_integer_sequence<int, N>{});
 }
 
+// Whether f(integral_constant<int, 0>{}), ... are all true; ends with the first that is not.
+template <typename F, int... J>
+__device__ __forceinline__ bool all(F f, std::integer_sequence<int, J...>) {
+  return (f(std::integral_constant<int, J>{}) && ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ bool all(F f) {
+  return all(f, std::make_integer_sequence<int, N>{});
+}
+
 // (One value to the wave, which the compiler then keeps in a scalar register.)
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / 64); }
 
@@ -390,23 +400,30 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
 // piece of 16 rows, which a matrix operand reads, is spread over the banks. The
 // LDS side of a load into LDS is fixed (lane after lane), so the lanes' global
 // addresses carry the permutation.
-template <typename E, int BM, int BN, int WM, int WN, int S, bool GATED, bool ALIGNED>
+template <typename E, int BM, int BN, int WM, int WN, int SM, int SN, bool GATED, bool ALIGNED>
 __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 tiles of a wave
-  constexpr int kStage = (BM + BN) * kLinearChunk;
-  constexpr int kLoadsN = BN / 8 / kWaves, kLoadsM = BM / 8 / kWaves;
+  constexpr int kLoadsN = BN / 8 / kWaves, kLoadsM = BM / 8 / kWaves, kLoads = kLoadsN + kLoadsM;
   constexpr int kPlanes = GATED ? 2 : 1;
   constexpr int kCols = BN / kPlanes;
-  static_assert(S >= 2 && S <= 4 && (ALIGNED || S == 2), "stages");
-  __shared__ __attribute__((aligned(16))) char stage0[kStage], stage1[kStage], stage2[S > 2 ? kStage : 16],
-      stage3[S > 3 ? kStage : 16];
-  const auto stage_of = [&](auto i) -> char* {
-    constexpr int k = decltype(i)::value % S;
-    if constexpr (k == 0) return stage0;
-    else if constexpr (k == 1) return stage1;
-    else if constexpr (k == 2) return stage2;
-    else return stage3;
+  static_assert(SM >= 2 && SM <= SN && SN <= SM + 1 && SN <= 4 && (ALIGNED || SN == 2), "stages");
+  constexpr int kBytesN = BN * kLinearChunk, kBytesM = BM * kLinearChunk;
+  __shared__ __attribute__((aligned(16))) char n_0[kBytesN], n_1[kBytesN], n_2[SN > 2 ? kBytesN : 16],
+      n_3[SN > 3 ? kBytesN : 16], m_0[kBytesM], m_1[kBytesM], m_2[SM > 2 ? kBytesM : 16], m_3[SM > 3 ? kBytesM : 16];
+  const auto stage_n = [&](auto i) -> char* {
+    constexpr int k = decltype(i)::value % SN;
+    if constexpr (k == 0) return n_0;
+    else if constexpr (k == 1) return n_1;
+    else if constexpr (k == 2) return n_2;
+    else return n_3;
+  };
+  const auto stage_m = [&](auto i) -> char* {
+    constexpr int k = decltype(i)::value % SM;
+    if constexpr (k == 0) return m_0;
+    else if constexpr (k == 1) return m_1;
+    else if constexpr (k == 2) return m_2;
+    else return m_3;
   };
   const int wave = wave_id(), lane = static_cast<int>(threadIdx.x) % 64;
 
@@ -443,36 +460,43 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   const uint32_t off_m = static_cast<uint32_t>(row_m(0) * p.x_stride + 16 * piece);
   u32x4 held[ALIGNED ? 1 : kLoadsN + kLoadsM];
 
-  // Load i of chunk c (aligned: into LDS; else into registers, for put()).
-  constexpr int kLoads = kLoadsN + kLoadsM, kLoadsPlane = kLoadsN / kPlanes;
+  // Load i of chunk c of the weights and of x (aligned: into LDS; else into registers, for put()).
+  constexpr int kLoadsPlane = kLoadsN / kPlanes;
   const uint32_t step_n = static_cast<uint32_t>(kStep * p.w_stride), step_m = static_cast<uint32_t>(kStep * p.x_stride);
-  const auto load = [&](char* stage, int c, int i) {
+  const auto fetch = [&](const char* src, int at) -> u32x4 {
+    if (at + kLinearChunk <= stop) return *reinterpret_cast<const u32x4u*>(src + at + 16 * piece);
+    return load_piece<E>(src, at + 16 * piece, stop);
+  };
+  const auto load_n = [&](char* stage, int c, int i) {
     const int at = c * kLinearChunk;
-    if constexpr (ALIGNED) {
-      const bool out = at + 16 * piece >= stop;
-      if (i < kLoadsN)
-        wr[i / kLoadsPlane].load(stage + (i * kWaves + wave) * 1024, (out ? kOutside : off_n) + i % kLoadsPlane * step_n, at);
-      else
-        xr.load(stage + (i * kWaves + wave) * 1024, (out ? kOutside : off_m) + (i - kLoadsN) * step_m, at);
-    } else {
-      const char* src = i < kLoadsN ? wb[i / kLoadsPlane] + least(row_n(i), rows_n - 1) * p.w_stride
-                                    : xb + least(row_m(i - kLoadsN), rows_m - 1) * p.x_stride;
-      held[i] = at + kLinearChunk <= stop ? *reinterpret_cast<const u32x4u*>(src + at + 16 * piece)
-                                          : load_piece<E>(src, at + 16 * piece, stop);
-    }
+    if constexpr (ALIGNED)
+      wr[i / kLoadsPlane].load(stage + (i * kWaves + wave) * 1024,
+                               (at + 16 * piece >= stop ? kOutside : off_n) + i % kLoadsPlane * step_n, at);
+    else
+      held[i] = fetch(wb[i / kLoadsPlane] + least(row_n(i), rows_n - 1) * p.w_stride, at);
   };
-  const auto start = [&](char* stage, int c) {
+  const auto load_m = [&](char* stage, int c, int i) {
+    const int at = c * kLinearChunk;
+    if constexpr (ALIGNED)
+      xr.load(stage + (i * kWaves + wave) * 1024, (at + 16 * piece >= stop ? kOutside : off_m) + i * step_m, at);
+    else
+      held[kLoadsN + i] = fetch(xb + least(row_m(i), rows_m - 1) * p.x_stride, at);
+  };
+  const auto start_n = [&](char* stage, int c) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(stage, c, i);
+    for (int i = 0; i < kLoadsN; ++i) load_n(stage, c, i);
   };
-  auto put = [&](char* stage) {
+  const auto start_m = [&](char* stage, int c) {
+#pragma unroll
+    for (int i = 0; i < kLoadsM; ++i) load_m(stage, c, i);
+  };
+  const auto put = [&](char* to_n, char* to_m) {
     if constexpr (!ALIGNED) {
 #pragma unroll
-      for (int i = 0; i < kLoadsN; ++i)
-        *reinterpret_cast<u32x4*>(stage + (i * kWaves + wave) * 1024 + lane * 16) = held[i];
+      for (int i = 0; i < kLoadsN; ++i) *reinterpret_cast<u32x4*>(to_n + (i * kWaves + wave) * 1024 + lane * 16) = held[i];
 #pragma unroll
       for (int i = 0; i < kLoadsM; ++i)
-        *reinterpret_cast<u32x4*>(stage + BN * kLinearChunk + (i * kWaves + wave) * 1024 + lane * 16) = held[kLoadsN + i];
+        *reinterpret_cast<u32x4*>(to_m + (i * kWaves + wave) * 1024 + lane * 16) = held[kLoadsN + i];
     }
   };
 
@@ -494,16 +518,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
     asm volatile("" : "+v"(at));
     return at ^ (64 * step);
   };
-  // Operand t of a step: tiles of weights, then of x.
-  const auto read = [&](const char* at, Operands& o, int t) {
-    int r;
-    if (t >= TN)
-      r = BN + (wm * TM + t - TN) * 16;
-    else if (GATED)
-      r = (t >= TN / 2 ? kCols : 0) + wn * (TN / 2 * 16) + t % (TN / 2) * 16;
-    else
-      r = (wn * TN + t) * 16;
-    o.v[t] = *reinterpret_cast<const u32x4*>(at + r * kLinearChunk);
+  // Operand t of a step, `at` its place: tiles of weights, then of x.
+  const auto read = [&](const char* from_n, const char* from_m, int at, Operands& o, int t) {
+    if (t >= TN) {
+      o.v[t] = *reinterpret_cast<const u32x4*>(from_m + at + (wm * TM + t - TN) * 16 * kLinearChunk);
+    } else {
+      const int r = GATED ? (t >= TN / 2 ? kCols : 0) + wn * (TN / 2 * 16) + t % (TN / 2) * 16 : (wn * TN + t) * 16;
+      o.v[t] = *reinterpret_cast<const u32x4*>(from_n + at + r * kLinearChunk);
+    }
   };
   // A step's products, with other(0) .. other(others - 1) between the first of them.
   constexpr int kProducts = TN * TM, kRate = (TN + TM + kLoads + kProducts - 1) / kProducts;
@@ -520,58 +542,75 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
 
   // Each chunk is two steps. The first step's operands of a chunk are read
   // while the second of the chunk before it is multiplied; the one barrier per
-  // chunk lies between: all waves have read the chunk, whose stage takes the
-  // loads of the chunk S further on, and the next chunk's loads have landed.
-  // What is loaded and read stands between the products one by one (all at the
-  // start of a step, the loads' issue held the products up: 8192 x 14336 x 3584
-  // 722 -> 697 us). Chunks behind the end load nothing and are zero, so that the
-  // loop holds no branch.
+  // chunk lies between: all waves have read the chunk, whose stages take the
+  // loads of x's chunk SM and the weights' chunk SN further on, and the next
+  // chunk's loads have landed, of which the weights' may have had a chunk
+  // longer. What is loaded and read stands between the products one by one
+  // (all at the start of a step, the loads' issue held the products up: 8192 x
+  // 14336 x 3584 722 -> 697 us). Chunks behind the end load nothing.
+  constexpr int kLate = SN > SM ? kLoadsN : 0;  // loads of the weights that may still be under way
   if constexpr (ALIGNED) {
-    each<S>([&](auto j) { start(stage_of(j), first + decltype(j)::value); });
-    landed<kLoads*(S - 1)>();
+    each<SN>([&](auto j) {
+      constexpr int k = decltype(j)::value;
+      if constexpr (k < SM) start_m(stage_m(j), first + k);
+      start_n(stage_n(j), first + k);
+    });
+    landed<kLoads*(SM - 1) + kLate>();
     barrier();
   } else {
-    start(stage0, first);
-    put(stage0);
+    start_n(n_0, first);
+    start_m(m_0, first);
+    put(n_0, m_0);
     __syncthreads();
-    start(stage1, first + 1);
+    start_n(n_1, first + 1);
+    start_m(m_1, first + 1);
   }
 #pragma unroll
-  for (int t = 0; t < TN + TM; ++t) read(stage0 + from, lo, t);
-  const auto chunk = [&](char* cur, char* next, int c) {
+  for (int t = 0; t < TN + TM; ++t) read(n_0, m_0, from, lo, t);
+  int c = first;
+  const auto chunk = [&](auto j) {
+    constexpr int k = decltype(j)::value;
+    constexpr std::integral_constant<int, k + 1> next{};
     __builtin_amdgcn_sched_barrier(0);
-    const char* at_hi = cur + operands_at(1);
-    multiply(lo, TN + TM, [&](int t) { read(at_hi, hi, t); });
+    const int at_hi = operands_at(1);
+    multiply(lo, TN + TM, [&](int t) { read(stage_n(j), stage_m(j), at_hi, hi, t); });
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (ALIGNED) {
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the second step's operands
-      landed<kLoads*(S - 2)>();
+      landed<kLoads*(SM - 2) + kLate>();
       barrier();
     } else {
-      put(next);
+      put(stage_n(next), stage_m(next));
       __syncthreads();
     }
-    const char* at_lo = next + operands_at(0);
+    const int at_lo = operands_at(0);
     multiply(hi, TN + TM + kLoads, [&](int t) {
-      if (t < kLoads)
-        load(cur, c + S, t);
+      if (t < kLoadsM)
+        load_m(stage_m(j), c + SM, t);
+      else if (t < kLoads)
+        load_n(stage_n(j), c + SN, t - kLoadsM);
       else
-        read(at_lo, lo, t - kLoads);
+        read(stage_n(next), stage_m(next), at_lo, lo, t - kLoads);
     });
+    return ++c < end;
   };
-  for (int c = first; c < end; c += S)
-    each<S>([&](auto j) {
-      constexpr int k = decltype(j)::value;
-      chunk(stage_of(j), stage_of(std::integral_constant<int, k + 1>{}), c + k);
-    });
+  // Rounds of as many chunks as both operands' stages come round in, without a
+  // branch between them (at a loop's head that others lead to, the compiler
+  // waits for all loads), and the last ones.
+  constexpr int kRound = SM == SN ? SN : SM * SN;
+  while (c + kRound <= end) each<kRound>(chunk);
+  if (c < end) all<kRound - 1>(chunk);
 
   // The sums go through LDS, two tiles of rows at a time, so that what is
   // written is whole runs of columns (and the code of the activations stands
   // once per pass).
   constexpr int kWidth = TN * 4, kQuads = GATED ? kWidth / 2 : kWidth;  // four columns each
-  constexpr int kPart = 32 * kWidth * 16, kParts = kStage / kPart;  // bytes of a wave's tiles, waves to a stage
-  static_assert(kWaves <= 2 * kParts && (kWidth & (kWidth - 1)) == 0, "the waves' parts of two stages");
-  f32x4* const tile = reinterpret_cast<f32x4*>((wave < kParts ? stage0 : stage1) + wave % kParts * kPart);
+  constexpr int kPart = 32 * kWidth * 16, kInN = kBytesN / kPart, kInM = kBytesM / kPart;  // a wave's bytes, waves to a stage
+  static_assert(kWaves <= 2 * (kInN + kInM) && (kWidth & (kWidth - 1)) == 0, "the waves' parts of two stages");
+  char* const part = wave < kInN       ? n_0 + wave * kPart
+                     : wave < 2 * kInN ? n_1 + (wave - kInN) * kPart
+                     : wave < 2 * kInN + kInM ? m_0 + (wave - 2 * kInN) * kPart : m_1 + (wave - 2 * kInN - kInM) * kPart;
+  f32x4* const tile = reinterpret_cast<f32x4*>(part);
   const auto place = [&](int r, int q) { return tile + r * kWidth + (q ^ (r & (kWidth - 1))); };  // (spread over the banks)
 #pragma unroll
   for (int j = 0; j < TM; j += 2) {
@@ -717,30 +756,20 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
 }  // namespace
 
-// Stages of a small tile: as many as leave room for two workgroups on a
-// compute unit (160 KB of LDS), at most eight.
-template <int BM, int BN>
-constexpr int thin_stages() {
-  constexpr int n = 78 * 1024 / ((BM + BN) * kThinChunk);
-  return n > 8 ? 8 : n;
-}
-
 template <typename E, bool GATED, bool ALIGNED>
 static hipError_t launch_thin(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles * p.splits));
 #define TTS_THIN(BM, BN)                                                                                            \
   if (plan.bm == BM && plan.bn == BN) {                                                                             \
-    hipLaunchKernelGGL((thin_kernel<E, BM, BN, ALIGNED ? thin_stages<BM, BN>() : 2, GATED, ALIGNED>), grid,          \
+    hipLaunchKernelGGL((thin_kernel<E, BM, BN, ALIGNED ? thin_stages(BM, BN) : 2, GATED, ALIGNED>), grid,          \
                        dim3(kThinThreads), 0, stream, p);                                                            \
     return hipGetLastError();                                                                                        \
   }
   if constexpr (!GATED) {
     TTS_THIN(16, 16)
     TTS_THIN(32, 16)
-    TTS_THIN(64, 16)
     TTS_THIN(16, 48)
     TTS_THIN(32, 48)
-    TTS_THIN(64, 48)
   }
   TTS_THIN(16, 32)
   TTS_THIN(32, 32)
@@ -757,20 +786,18 @@ static hipError_t launch_thin(const LinearParams& p, const LinearPlan& plan, hip
 template <typename E, bool GATED, bool ALIGNED>
 static hipError_t launch_tiles(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles * p.splits));
-#define TTS_TILE(BM, BN, WM, WN, S)                                                                               \
-  if (plan.bm == BM && plan.bn == BN && plan.tile == S) {                                                        \
-    hipLaunchKernelGGL((tile_kernel<E, BM, BN, WM, WN, S, GATED, ALIGNED>), grid, dim3(64 * WM * WN), 0, stream, p); \
-    return hipGetLastError();                                                                                     \
+#define TTS_TILE(BM, BN, WM, WN, SM, SN)                                                                                  \
+  if (plan.bm == BM && plan.bn == BN && plan.tile == 10 * SM + SN) {                                                       \
+    hipLaunchKernelGGL((tile_kernel<E, BM, BN, WM, WN, SM, SN, GATED, ALIGNED>), grid, dim3(64 * WM * WN), 0, stream, p); \
+    return hipGetLastError();                                                                                              \
   }
-  TTS_TILE(128, 128, 2, 2, 2)
   if constexpr (ALIGNED && sizeof(E) == 2) {
-    TTS_TILE(256, 256, 2, 4, 2)
-    TTS_TILE(256, 128, 4, 2, 3)
-    TTS_TILE(128, 256, 2, 4, 3)
-    TTS_TILE(128, 128, 2, 2, 4)
-    TTS_TILE(128, 128, 2, 2, 3)
-    TTS_TILE(64, 128, 1, 4, 3)
-    TTS_TILE(128, 64, 4, 1, 3)
+    TTS_TILE(256, 256, 2, 4, 2, 3)
+    TTS_TILE(128, 256, 2, 4, 3, 3)
+    TTS_TILE(128, 128, 2, 2, 4, 4)
+    TTS_TILE(64, 128, 1, 4, 3, 3)
+  } else {
+    TTS_TILE(128, 128, 2, 2, 2, 2)
   }
 #undef TTS_TILE
   return hipErrorInvalidValue;

@@ -59,6 +59,41 @@ def test_gated_shapes(kind, m, k, n):
     L.close(out, *L.gated(x, wg, wu), kind)
 
 
+# Shapes that the plan gives to each of its tiles in turn, aligned rows (whole and partial tiles, several rounds of their
+# stages) and others.
+PLAIN_TILES = [(1, 624, 16), (1, 608, 4217), (1, 616, 8269), (1, 72, 26688), (17, 624, 2380), (17, 648, 4538),
+               (17, 656, 8545), (35, 680, 6179), (36, 624, 6232), (101, 608, 6734), (931, 608, 8414), (322, 632, 10998),
+               (131, 608, 11194), (67, 656, 9625), (200, 2048, 2056), (1, 607, 16), (1, 673, 9370), (1, 630, 8300), (17, 957, 8180),
+               (17, 714, 2081), (18, 633, 4364), (19, 651, 8214), (33, 789, 6271), (35, 718, 6148), (39, 627, 11528),
+               (534, 671, 170)]
+GATED_TILES = [(1, 608, 16), (1, 608, 8288), (17, 720, 2155), (17, 624, 4365), (38, 608, 2698), (35, 624, 6956),
+               (282, 640, 10897), (140, 608, 11253), (65, 616, 8802), (33, 712, 8240), (200, 2048, 1100), (1, 603, 16), (1, 625, 8272),
+               (18, 615, 2274), (33, 618, 2806), (35, 766, 2724), (36, 633, 5530), (519, 638, 160)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", PLAIN_TILES)
+def test_every_plain_tile(kind, m, k, n):
+    g = L.generator(m + k)
+    x, w = L.rows((m, k), 0, kind, g), L.rows((n, k), 0, kind, g, k ** -0.5)
+    res = L.rows((m, n), 0, kind, g)
+    out = torch.full((m, n), math.nan, dtype=L.TYPES[kind], device=L.DEV)
+    run_linear(x, w, out, kind, kind, "none", None, res)
+    L.close(out, *L.linear(x, w, None, "none", res), kind)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", GATED_TILES)
+def test_every_gated_tile(kind, m, k, n):
+    g = L.generator(m + k)
+    x = L.rows((m, k), 0, kind, g)
+    wg, wu = (L.rows((n, k), 0, kind, g, k ** -0.5) for _ in range(2))
+    bg = L.rows((1, n), 0, kind, g)[0]
+    out = torch.full((m, n), math.nan, dtype=L.TYPES[kind], device=L.DEV)
+    run_gated(x, wg, wu, out, kind, kind, "gelu_tanh", bg)
+    L.close(out, *L.gated(x, wg, wu, bg, None, "gelu_tanh"), kind)
+
+
 @pytest.mark.parametrize("act", L.ACTS)
 @pytest.mark.parametrize("kind,out_kind", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
 @pytest.mark.parametrize("m", [5, 100])

@@ -58,13 +58,13 @@ def test_workspaces():
     for need, call in ((T.tts_linear_workspace_size, _linear), (T.tts_gated_linear_workspace_size, _gated)):
         size = need(d, 16)
         assert size > 0
-        assert call(k=8192, n=144, m=16, work=A, size=size - 1) == WSP
+        assert call(k=8192, n=144, m=16, work=A, size=16 * 144 * 4) == WSP  # less than one part's sums
         assert call(k=8192, n=144, m=16, work=None, size=size) == WSP
         assert call(k=8192, n=144, m=16, work=A + 8, size=size) == INV
         assert need(d, 0) == 0 and need(d, -3) == 0
         assert need(T.make_linear(64, 144), 16) == 0  # too short to split
-        sizes = [need(d, m) for m in (1, 2, 16, 17, 33, 64, 65, 128, 129, 300, 1000, 5000, 1 << 30)]
-        assert sizes == sorted(sizes) and sizes[-1] == sizes[-2]
+        sizes = [need(d, m) for m in (1, 2, 16, 17, 33, 64, 65, 128, 129, 300, 1000, 1 << 20, 1 << 30)]
+        assert sizes == sorted(sizes) and sizes[-1] == sizes[-2]  # large calls are not split
     assert T.tts_linear_workspace_size(T.make_linear(0, 144), 16) == 0
 
 
