@@ -90,18 +90,49 @@ __device__ __forceinline__ f32x4 load_row4(const void* p, int64_t i, int count, 
   return r;
 }
 
-// The finished columns n .. n + 3 (those below p.n) of row m from their sums.
+// What an output's four columns n .. n + 3 (those below p.n) are made with
+// beside their sums. Loaded early: behind the products, the round trip would
+// count for every row (8192 x 3584 x 3584 with a residual 199 -> 185 us).
 template <bool GATED>
-__device__ __forceinline__ void finish(const LinearParams& p, int m, int n, f32x4 y, f32x4 up) {
-  const int count = p.n - n < 4 ? p.n - n : 4;
-  if (p.bias[0]) y += load_row4(p.bias[0], n, count, p.in_bf16);
+struct Extra {
+  f32x4 bias[GATED ? 2 : 1], residual;
+};
+
+__device__ __forceinline__ int columns(const LinearParams& p, int n) { return p.n - n < 4 ? p.n - n : 4; }
+
+__device__ __forceinline__ f32x4 load_bias(const LinearParams& p, int plane, int n) {
+  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+  return p.bias[plane] && n < p.n ? load_row4(p.bias[plane], n, columns(p, n), p.in_bf16) : none;
+}
+
+__device__ __forceinline__ f32x4 load_residual(const LinearParams& p, int m, int n) {
+  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+  return p.residual && m < p.rows && n < p.n ? load_row4(p.residual, m * p.residual_stride + n, columns(p, n), p.out_bf16)
+                                             : none;
+}
+
+template <bool GATED>
+__device__ __forceinline__ Extra<GATED> load_extra(const LinearParams& p, int m, int n) {
+  Extra<GATED> e;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) y[j] = activate(y[j], p.act);
-  if constexpr (GATED) {
-    if (p.bias[1]) up += load_row4(p.bias[1], n, count, p.in_bf16);
-    y *= up;
-  }
-  if (p.residual) y += load_row4(p.residual, m * p.residual_stride + n, count, p.out_bf16);
+  for (int i = 0; i < (GATED ? 2 : 1); ++i) e.bias[i] = load_bias(p, i, n);
+  e.residual = load_residual(p, m, n);
+  return e;
+}
+
+// act(y + bias), gated: times (up + its bias).
+template <bool GATED>
+__device__ __forceinline__ f32x4 activated(const LinearParams& p, const f32x4 (&bias)[GATED ? 2 : 1], f32x4 y, f32x4 up) {
+  y += bias[0];
+  if (p.act != kActNone)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = activate(y[j], p.act);
+  if constexpr (GATED) y *= up + bias[1];
+  return y;
+}
+
+__device__ __forceinline__ void store_out(const LinearParams& p, int m, int n, f32x4 y) {
+  const int count = columns(p, n);
   const int64_t at = m * p.out_stride + n;
   if (p.out_bf16) {
     __bf16* o = static_cast<__bf16*>(p.out) + at;
@@ -135,16 +166,10 @@ __device__ __forceinline__ void store_part(float* dst, int count, f32x4 y) {
 }
 
 template <bool GATED>
-__device__ __forceinline__ void emit(const LinearParams& p, int split, int m, int n, f32x4 y, f32x4 up) {
-  if (m >= p.rows || n >= p.n) return;
-  if (p.splits == 1) {
-    finish<GATED>(p, m, n, y, up);
-    return;
-  }
+__device__ __forceinline__ void store_parts(const LinearParams& p, int split, int m, int n, f32x4 y, f32x4 up) {
   constexpr int kPlanes = GATED ? 2 : 1;
-  const int count = p.n - n < 4 ? p.n - n : 4;
-  store_part(p.part + part_at(p, split, 0, kPlanes, m, n), count, y);
-  if constexpr (GATED) store_part(p.part + part_at(p, split, 1, kPlanes, m, n), count, up);
+  store_part(p.part + part_at(p, split, 0, kPlanes, m, n), columns(p, n), y);
+  if constexpr (GATED) store_part(p.part + part_at(p, split, 1, kPlanes, m, n), columns(p, n), up);
 }
 
 // ---- loads into LDS ------------------------------------------------------------
@@ -337,6 +362,18 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
       for (int j = 0; j < TM; ++j) acc[i][j] = mma<E>(a[i], b[j], acc[i][j]);
   };
 
+  // A thread's outputs, and what they are made with (older than the chunks'
+  // loads, so that waiting for these covers it).
+  constexpr int kQuads = kCols / 4, kItems = BM * kQuads, kEach = (kItems + kThinThreads - 1) / kThinThreads;
+  Extra<GATED> extra[kEach];
+  if (p.splits == 1)
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = static_cast<int>(threadIdx.x) + e * kThinThreads;
+      extra[e] = load_extra<GATED>(p, m0 + i / kQuads, n0 + i % kQuads * 4);
+    }
+  __builtin_amdgcn_sched_barrier(0);
+
   // Stage j's chunk has landed once all but the S - 2 newer ones have; behind
   // the barrier the stage read before it is free for the chunk S - 1 further
   // on. Chunks behind the end load nothing and are zero.
@@ -377,10 +414,12 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
 #pragma unroll
     for (int j = 0; j < TM; ++j) sum_at(wave * TN * TM + i * TM + j)[lane] = acc[i][j];
   __syncthreads();
-  constexpr int kQuads = kCols / 4;
-#pragma nounroll
-  for (int i = threadIdx.x; i < BM * kQuads; i += kThinThreads) {
-    const int r = i / kQuads, q = i % kQuads, l = (r & 15) + 16 * (q & 3), t = q / 4 * TM + r / 16;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int i = static_cast<int>(threadIdx.x) + e * kThinThreads, r = i / kQuads, q = i % kQuads;
+    const int m = m0 + r, n = n0 + 4 * q;
+    if ((kItems % kThinThreads != 0 && i >= kItems) || m >= p.rows || n >= p.n) continue;
+    const int l = (r & 15) + 16 * (q & 3), t = q / 4 * TM + r / 16;
     f32x4 y = sum_at(t)[l], up = y;
 #pragma unroll
     for (int w = 1; w < kThinWaves; ++w) y += sum_at(w * TN * TM + t)[l];
@@ -389,7 +428,10 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
 #pragma unroll
       for (int w = 1; w < kThinWaves; ++w) up += sum_at(w * TN * TM + t + kTilesN * TM)[l];
     }
-    emit<GATED>(p, split, m0 + r, n0 + 4 * q, y, up);
+    if (p.splits > 1)
+      store_parts<GATED>(p, split, m, n, y, up);
+    else
+      store_out(p, m, n, activated<GATED>(p, extra[e].bias, y, up) + extra[e].residual);
   }
 }
 
@@ -596,14 +638,22 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   };
   // Rounds of as many chunks as both operands' stages come round in, without a
   // branch between them (at a loop's head that others lead to, the compiler
-  // waits for all loads), and the last ones.
+  // waits for all loads), and the last ones. But for the largest tile, a round
+  // of six, whose registers do not suffice for the code twice (1% there; 320 x
+  // 14336 x 3584 with 128 x 256: 55 -> 50 us).
   constexpr int kRound = SM == SN ? SN : SM * SN;
-  while (c + kRound <= end) each<kRound>(chunk);
-  if (c < end) all<kRound - 1>(chunk);
+  if constexpr (SM == SN) {
+    while (c + kRound <= end) each<kRound>(chunk);
+    if (c < end) all<kRound - 1>(chunk);
+  } else {
+    while (all<kRound>(chunk)) {
+    }
+  }
 
   // The sums go through LDS, two tiles of rows at a time, so that what is
-  // written is whole runs of columns (and the code of the activations stands
-  // once per pass).
+  // written is whole runs of columns: a lane has the same four columns in
+  // every row. The activation, a long one, stands in a loop; what waits for
+  // memory does not.
   constexpr int kWidth = TN * 4, kQuads = GATED ? kWidth / 2 : kWidth;  // four columns each
   constexpr int kPart = 32 * kWidth * 16, kInN = kBytesN / kPart, kInM = kBytesM / kPart;  // a wave's bytes, waves to a stage
   static_assert(kWaves <= 2 * (kInN + kInM) && (kWidth & (kWidth - 1)) == 0, "the waves' parts of two stages");
@@ -612,8 +662,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
                      : wave < 2 * kInN + kInM ? m_0 + (wave - 2 * kInN) * kPart : m_1 + (wave - 2 * kInN - kInM) * kPart;
   f32x4* const tile = reinterpret_cast<f32x4*>(part);
   const auto place = [&](int r, int q) { return tile + r * kWidth + (q ^ (r & (kWidth - 1))); };  // (spread over the banks)
+  constexpr int kStride = 64 / kQuads, kRows = 32 / kStride;  // rows apart, and rows, of a lane
+  const int q = lane % kQuads, r0 = lane / kQuads, n = n0 + (wn * kQuads + q) * 4;
+  const bool whole = p.splits == 1, heavy = whole && (GATED || p.act != kActNone);
+  f32x4 bias[kPlanes];
+#pragma unroll
+  for (int i = 0; i < kPlanes; ++i) bias[i] = load_bias(p, i, n);
 #pragma unroll
   for (int j = 0; j < TM; j += 2) {
+    const int m = m0 + (wm * TM + j) * 16 + r0;
+    f32x4 residual[kRows];
+    if (whole)
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) residual[i] = load_residual(p, m + i * kStride, n);
     landed();
     __syncthreads();
 #pragma unroll
@@ -621,11 +682,23 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
 #pragma unroll
       for (int i = 0; i < TN; ++i) *place(16 * h + row, 4 * i + group) = acc[i][j + h];
     __syncthreads();
+    if (heavy) {
 #pragma nounroll
-    for (int i = lane; i < 32 * kQuads; i += 64) {
-      const int r = i / kQuads, q = i % kQuads;
-      emit<GATED>(p, split, m0 + (wm * TM + j) * 16 + r, n0 + (wn * kQuads + q) * 4, *place(r, q),
-                  *place(r, q + (GATED ? kQuads : 0)));
+      for (int i = 0; i < kRows; ++i) {
+        f32x4* at = place(r0 + i * kStride, q);
+        *at = activated<GATED>(p, bias, *at, *place(r0 + i * kStride, q + (GATED ? kQuads : 0)));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      if (m + i * kStride >= p.rows || n >= p.n) continue;
+      f32x4 y = *place(r0 + i * kStride, q);
+      if (!whole) {
+        store_parts<GATED>(p, split, m + i * kStride, n, y, *place(r0 + i * kStride, q + (GATED ? kQuads : 0)));
+        continue;
+      }
+      if (!heavy) y += bias[0];
+      store_out(p, m + i * kStride, n, y + residual[i]);
     }
   }
 }
@@ -641,13 +714,14 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(LinearParams p) {
   if (i >= static_cast<int64_t>(quads) * p.rows) return;
   const int m = static_cast<int>(i / quads), n = static_cast<int>(i % quads) * 4;
   const int count = p.n - n < 4 ? p.n - n : 4;
+  const Extra<GATED> extra = load_extra<GATED>(p, m, n);
   f32x4 y[kPlanes];
 #pragma unroll
   for (int q = 0; q < kPlanes; ++q) {
     y[q] = load_row4(p.part, part_at(p, 0, q, kPlanes, m, n), count, false);
     for (int s = 1; s < p.splits; ++s) y[q] += load_row4(p.part, part_at(p, s, q, kPlanes, m, n), count, false);
   }
-  finish<GATED>(p, m, n, y[0], y[kPlanes - 1]);
+  store_out(p, m, n, activated<GATED>(p, extra.bias, y[0], y[kPlanes - 1]) + extra.residual);
 }
 
 // ---- norm --------------------------------------------------------------------
