@@ -9,13 +9,9 @@ namespace tts {
 constexpr int kRopeTile = 4096;   // elements (tokens x heads x head dims) of a K or V part
 constexpr int kRopeTasks = 1024;  // units of the query rows to a part
 
-// Lanes that a row of so many units takes with head norms: a power of two, at
-// most a wave.
-constexpr int rope_lanes(int units) {
-  int n = 1;
-  while (n < units && n < 64) n *= 2;
-  return n;
-}
+// Lanes that a row takes with head norms, read eight elements at a time or one
+// by one: sixteen elements or two (64 or 128 dims) to a lane.
+constexpr int rope_lanes(int head_dim, int width) { return width == 8 ? head_dim / 16 : head_dim / 2; }
 
 struct RopeParams {
   const void* q;  // null: no queries

@@ -346,20 +346,25 @@ __device__ __forceinline__ int rope_units(const RopeParams& p) {
   return (p.interleaved && W > 1 ? p.rot / W : p.rot / 2 / W) + passed;
 }
 
-// Elements `at` .. + W of a row, of a normalised one its `scale` and weights applied.
+// x times the row's scale and its weights.
+template <int W, typename E>
+__device__ __forceinline__ void normalise(float (&x)[W], const E* weight, int at, float scale) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int i = 0; i < W; ++i) x[i] = x[i] * scale;
+  if (weight) {
+    float w[W];
+    load_elems<W>(weight + at, w);
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = x[i] * w[i];
+  }
+}
+
+// Elements `at` .. + W of a row, of a normalised one with its norm.
 template <int W, bool NORM, typename E>
 __device__ __forceinline__ void load_row(const E* src, const E* weight, float scale, int at, float (&x)[W]) {
-#pragma clang fp contract(off)
   load_elems<W>(src + at, x);
-  if constexpr (NORM) {
-    float w[W];
-    if (weight) load_elems<W>(weight + at, w);
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      x[i] = x[i] * scale;
-      if (weight) x[i] = x[i] * w[i];
-    }
-  }
+  if constexpr (NORM) normalise(x, weight, at, scale);
 }
 
 template <int W, bool NORM, typename E>
@@ -410,25 +415,32 @@ __device__ __forceinline__ RopeUnit<W> rope_unit(const RopeParams& p, const E* s
 // products round one by one, as those of the rotation behind them do: what is
 // stored in 8 and 4 bits then follows from the formula, whatever the order of
 // the sum.
-template <int W, typename E>
-__device__ __forceinline__ double squares(const E* src, int at) {
-  float x[W];
-  load_elems<W>(src + at, x);
+template <int W>
+__device__ __forceinline__ double squares(const float (&x)[W]) {
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < W; ++i) s += static_cast<double>(x[i]) * static_cast<double>(x[i]);
   return s;
 }
 
-// The sum of the squares of a unit's elements.
-template <int W, typename E>
-__device__ __forceinline__ double rope_squares(const RopeParams& p, const E* src, int u) {
-  const int half = p.rot / 2, turned = p.interleaved && W > 1 ? p.rot / W : half / W;
-  if (u >= turned) return squares<W>(src, p.rot + (u - turned) * W);
-  if (W > 1 && p.interleaved) return squares<W>(src, u * W);
-  return p.interleaved ? squares<W>(src, 2 * u) + squares<W>(src, 2 * u + 1)
-                       : squares<W>(src, u * W) + squares<W>(src, half + u * W);
+// 1 / sqrt(m), m >= 0 or NaN, in 64 bits: the hardware's estimate and two of
+// Newton's steps, each of which doubles its digits (23 of them at first).
+__device__ __forceinline__ double inverse_root(double m) {
+  double y = __builtin_amdgcn_rsq(m);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const double h = 0.5 * y, e = __builtin_fma(-m * y, h, 0.5);
+    y = __builtin_fma(y, e, y);
+  }
+  // (0 and infinity are not to be corrected.)
+  return m == 0.0 ? __builtin_inf() : (m == __builtin_inf() ? 0.0 : y);
 }
+
+__device__ __forceinline__ float head_scale(const RopeParams& p, double sum) {
+  return static_cast<float>(inverse_root(sum * (p.head_dim == 64 ? 1.0 / 64 : 1.0 / 128) + p.eps));
+}
+
+__device__ __forceinline__ int least_int(int a, int b) { return a < b ? a : b; }
 
 __device__ __forceinline__ int64_t rope_pos(const RopeParams& p, const RopeItem& it, int i) {
   return p.positions ? p.positions[it.row + i] : it.pos + i;
@@ -445,30 +457,99 @@ __device__ __forceinline__ uint32_t rope_tokens(const RopeParams& p, const RopeI
   return static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(good));
 }
 
+// Eight elements of pairs, in place.
+__device__ __forceinline__ void turn_pairs(float (&x)[8], const float* cos, const float* sin) {
+#pragma clang fp contract(off)
+  float c[4], s[4];
+  load_elems<4>(cos, c);
+  load_elems<4>(sin, s);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const float xc = x[i] * c[i / 2], ys = x[i + 1] * s[i / 2], yc = x[i + 1] * c[i / 2], xs = x[i] * s[i / 2];
+    x[i] = xc - ys;
+    x[i + 1] = yc + xs;
+  }
+}
+
+// Eight pairs of two halves, in place.
+__device__ __forceinline__ void turn_halves(float (&x)[8], float (&y)[8], const float* cos, const float* sin) {
+#pragma clang fp contract(off)
+  float c[8], s[8];
+  load_elems<8>(cos, c);
+  load_elems<8>(sin, s);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float xc = x[i] * c[i], ys = y[i] * s[i], yc = y[i] * c[i], xs = x[i] * s[i];
+    x[i] = xc - ys;
+    y[i] = yc + xs;
+  }
+}
+
 // Calls f(token, head - h0, unit) for the units of heads h0 .. h1 of the
 // item's good tokens, with the unit rotated.
 //
-// With head norms (`weight`: null for ones) a row's units go to adjacent
-// lanes, as many as rope_lanes() has, and `first` and `last` count lanes: its
-// sum of squares is then a sum over them, of what they hold in registers.
+// With head norms (`weight`: null for ones) a row goes to adjacent lanes, as
+// many as rope_lanes() says, and `first` and `last` count lanes: its sum of
+// squares is then a sum over them.
 template <int W, bool NORM, typename E, typename F>
 __device__ __forceinline__ void rope_each(const RopeParams& p, const RopeItem& it, uint32_t good, const E* src,
                                           int64_t stride, const E* weight, int h0, int h1, int first, int last, F f) {
   const int units = rope_units<W>(p), heads = h1 - h0;
-  if constexpr (NORM) {
-    const int lanes = rope_lanes(units), all = it.n * heads * lanes, stop = last < all ? last : all;
+  if constexpr (NORM && W == 8) {
+    // Sixteen elements to a lane, which stay in registers between the sum and
+    // the turn: eight pairs of two halves, or sixteen adjacent ones. (Four and
+    // two rows at a time, for more loads under way, were slower: 9187 tokens,
+    // 28 over 4 heads of 128, bf16 34.7 us at one row, 37 at two, 49 at four.)
+    const int lanes = p.head_dim / 16, log = 31 - __builtin_clz(lanes), half = p.rot / 2;
+    const int lane = static_cast<int>(threadIdx.x) & (lanes - 1), turned = p.interleaved ? 0 : half / 8;
+    const bool halves = lane < turned;
+    const int at0 = halves ? lane * 8 : (p.interleaved ? 0 : p.rot) + (lane - turned) * 16, at1 = halves ? half + lane * 8 : at0 + 8;
+    // (`first` and kRopeThreads are multiples of lanes, a power of two.)
+    const int rows = least_int(last >> log, it.n * heads), step = kRopeThreads >> log;
+    const int step_t = step / heads, step_h = step % heads;
+    int row = (first + static_cast<int>(threadIdx.x)) >> log, t = row / heads, h = row % heads;
+    for (; row < rows; row += step, t += step_t, h += step_h) {
+      if (h >= heads) h -= heads, ++t;
+      if (!((good >> t) & 1u)) continue;  // (all of a row's lanes)
+      const E* from = src + (it.row + t) * stride + static_cast<int64_t>(h0 + h) * p.head_dim;
+      RopeUnit<8> r;
+      r.parts = 2;
+      r.at[0] = at0;
+      r.at[1] = at1;
+      load_elems<8>(from + at0, r.x[0]);
+      load_elems<8>(from + at1, r.x[1]);
+      double sum = squares(r.x[0]) + squares(r.x[1]);
+      for (int o = lanes / 2; o > 0; o /= 2) sum += __shfl_xor(sum, o);
+      const float scale = head_scale(p, sum);
+      normalise(r.x[0], weight, at0, scale);
+      normalise(r.x[1], weight, at1, scale);
+      const int64_t angle = p.rot > 0 ? rope_pos(p, it, t) * half : 0;
+      if (halves)
+        turn_halves(r.x[0], r.x[1], p.cos + angle + at0, p.sin + angle + at0);
+      if (p.interleaved) {
+        if (at0 < p.rot) turn_pairs(r.x[0], p.cos + angle + at0 / 2, p.sin + angle + at0 / 2);
+        if (at1 < p.rot) turn_pairs(r.x[1], p.cos + angle + at1 / 2, p.sin + angle + at1 / 2);
+      }
+      f(t, h, r);
+    }
+    return;
+  } else if constexpr (NORM) {
+    const int lanes = rope_lanes(p.head_dim, W), all = it.n * heads * lanes, stop = last < all ? last : all;
     for (int i = first + static_cast<int>(threadIdx.x); i < stop; i += kRopeThreads) {
       const int lane = i % lanes, h = i / lanes % heads, t = i / lanes / heads;
       if (!((good >> t) & 1u)) continue;  // (all of a row's lanes)
       const int64_t at = p.rot > 0 ? rope_pos(p, it, t) * (p.rot / 2) : 0;
       const E* row = src + (it.row + t) * stride + static_cast<int64_t>(h0 + h) * p.head_dim;
-      double sum = lane < units ? rope_squares<W>(p, row, lane) : 0.0;
-      if (W == 1 && lane + lanes < units) sum += rope_squares<W>(p, row, lane + lanes);
+      double sum = 0.0;
+      for (int e = lane; e < p.head_dim; e += lanes) {
+        float x[1];
+        load_elems<1>(row + e, x);
+        sum += squares(x);
+      }
       for (int o = lanes / 2; o > 0; o /= 2) sum += __shfl_xor(sum, o);
-      const float scale = static_cast<float>(1.0 / sqrt(sum / p.head_dim + p.eps));
-      if (lane < units) f(t, h, rope_unit<W, true>(p, row, weight, scale, lane, p.cos + at, p.sin + at));
-      if (W == 1 && lane + lanes < units)
-        f(t, h, rope_unit<W, true>(p, row, weight, scale, lane + lanes, p.cos + at, p.sin + at));
+      const float scale = head_scale(p, sum);
+      for (int u = lane; u < units; u += lanes)
+        f(t, h, rope_unit<W, true>(p, row, weight, scale, u, p.cos + at, p.sin + at));
     }
     return;
   }
@@ -899,7 +980,7 @@ hipError_t launch_rope_append(RopeParams p, int kv_kind, bool norm, hipStream_t 
   p.kv_parts = (p.hkv + p.heads_per - 1) / p.heads_per;
   const int width = p.q_wide ? 8 : 1;
   const int row = (p.interleaved && p.q_wide ? p.rot / width : half / width) + (p.head_dim - p.rot) / width;
-  const int64_t units = norm ? rope_lanes(row) : row;
+  const int64_t units = norm ? rope_lanes(p.head_dim, width) : row;
   const int64_t q_parts = p.q ? (most_tokens * p.hq * units + kRopeTasks - 1) / kRopeTasks : 0;
   const int64_t parts = 2 * static_cast<int64_t>(p.kv_parts) + q_parts;
   if (parts > kMaxGridY) return hipErrorInvalidValue;
