@@ -110,21 +110,28 @@ class DecoderLayer:
         size = max(size, _t.tts_gated_linear_workspace_size(self.lin_ffn, max_tokens),
                    _t.tts_paged_decode_workspace_size(desc, max_seqs, self.max_seq_len))
         self.ws = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
+        self.outgrown = []  # (graphs that were captured with them, and calls under way, still write to them)
 
     def __call__(self, x, k_cache, v_cache, block_tables, seq_lens, k_scale=None, v_scale=None, tok_offsets=None,
                  meta: Optional[_t.PrefixMeta] = None, stream=None):
         """x [tokens][hidden], replaced by the layer's output. Without ``tok_offsets`` every sequence has one new token,
         and the attention is the paged call, or with ``meta`` the prefix-shared one; else it is the prefill. A call that
-        needs a larger workspace than the calls before it allocates one: make it once before capturing it."""
+        needs a larger workspace than the calls before it allocates one: make it once before capturing it (a captured one
+        raises). Calls of one layer, replayed ones too, must not overlap in time: they share its buffers."""
         w, ws, n, s = self.w, self.ws, int(x.shape[0]), int(seq_lens.shape[0])
         hq, hkv, d = self.desc.num_q_heads, self.desc.num_kv_heads, self.desc.head_dim
         cols, cache, scales = int(block_tables.shape[1]), (k_cache, v_cache), (k_scale, v_scale)
         need = 0
+        if n > self.normed.shape[0]:
+            raise ValueError(f"{n} tokens in a layer made for {self.normed.shape[0]}")
         if tok_offsets is not None:
             need = _t.tts_paged_prefill_workspace_size(self.desc, s, n, self.max_seq_len)
         elif meta is not None:
             need = _t.tts_prefix_decode_workspace_size(self.desc, meta)
         if need > ws.numel():
+            if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the workspace grows with this call: make it once before capturing it")
+            self.outgrown.append(ws)
             ws = self.ws = torch.empty(need, dtype=torch.uint8, device=ws.device)
         size, qkv, q, o, f = ws.numel(), self.qkv[:n], self.q[:n], self.o[:n], self.ffn[:n]
         _t.tts_rms_norm(self.norm, n, x, w["attn_norm"], self.normed, stream)
