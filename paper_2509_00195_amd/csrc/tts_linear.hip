@@ -24,6 +24,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // Loads and stores at the addresses of a caller's rows, which need only the
 // alignment of an element (the hardware takes them, an instruction each).
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
@@ -90,44 +92,88 @@ __device__ __forceinline__ f32x4 load_row4(const void* p, int64_t i, int count, 
   return r;
 }
 
-// What an output's four columns n .. n + 3 (those below p.n) are made with
-// beside their sums. Loaded early: behind the products, the round trip would
-// count for every row (8192 x 3584 x 3584 with a residual 199 -> 185 us).
-template <bool GATED>
-struct Extra {
-  f32x4 bias[GATED ? 2 : 1], residual;
-};
-
 __device__ __forceinline__ int columns(const LinearParams& p, int n) { return p.n - n < 4 ? p.n - n : 4; }
 
-__device__ __forceinline__ f32x4 load_bias(const LinearParams& p, int plane, int n) {
-  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-  return p.bias[plane] && n < p.n ? load_row4(p.bias[plane], n, columns(p, n), p.in_bf16) : none;
-}
+__device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
 
-__device__ __forceinline__ f32x4 load_residual(const LinearParams& p, int m, int n) {
-  const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-  return p.residual && m < p.rows && n < p.n ? load_row4(p.residual, m * p.residual_stride + n, columns(p, n), p.out_bf16)
-                                             : none;
-}
+// What an output's four columns are made with beside their sums, four values
+// each: bits as they are stored, where every row has whole quads of columns,
+// else fp32. Loaded early, and with no branch but uniform ones: where lanes
+// branch, the compiler waits for each load before the next (a wave's residual
+// in a 256 x 256 tile was 32 round trips one after another: 8192 x 3584 x 3584
+// with all of it from memory 216 -> 184 us).
+typedef u32x4 Four;
 
-template <bool GATED>
-__device__ __forceinline__ Extra<GATED> load_extra(const LinearParams& p, int m, int n) {
-  Extra<GATED> e;
+struct FourType {
+  bool wide, is_bf16;  // whole quads, and their type
+
+  __device__ __forceinline__ Four load(const void* p, int64_t i) const {  // wide
+    if (!is_bf16) return *reinterpret_cast<const u32x4u*>(static_cast<const float*>(p) + i);
+    const u32x2 r = *reinterpret_cast<const u32x2u*>(static_cast<const uint16_t*>(p) + i);
+    return Four{r[0], r[1], 0u, 0u};
+  }
+  __device__ __forceinline__ f32x4 value(Four v) const {
+    if (!wide || !is_bf16) return __builtin_bit_cast(f32x4, v);
+    const uint32_t b[4] = {v[0] << 16, v[0] & 0xFFFF0000u, v[1] << 16, v[1] & 0xFFFF0000u};
+    return f32x4{__builtin_bit_cast(float, b[0]), __builtin_bit_cast(float, b[1]), __builtin_bit_cast(float, b[2]),
+                 __builtin_bit_cast(float, b[3])};
+  }
+};
+
+__device__ __forceinline__ FourType bias_type(const LinearParams& p) { return {p.n % 4 == 0, p.in_bf16 != 0}; }
+__device__ __forceinline__ FourType residual_type(const LinearParams& p) { return {p.n % 4 == 0, p.out_bf16 != 0}; }
+
+// Of N places (m(i), n(i)); behind the last row or column what is loaded is not used.
+template <int N, typename F>
+__device__ __forceinline__ void load_bias(const LinearParams& p, int plane, Four (&r)[N], F n) {
+  const FourType t = bias_type(p);
 #pragma unroll
-  for (int i = 0; i < (GATED ? 2 : 1); ++i) e.bias[i] = load_bias(p, i, n);
-  e.residual = load_residual(p, m, n);
-  return e;
+  for (int i = 0; i < N; ++i) r[i] = Four{0u, 0u, 0u, 0u};
+  if (!p.bias[plane]) return;
+  if (t.wide) {
+    if (t.is_bf16)
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = FourType{true, true}.load(p.bias[plane], least(n(i), p.n - 4));
+    else
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = FourType{true, false}.load(p.bias[plane], least(n(i), p.n - 4));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (n(i) < p.n) r[i] = __builtin_bit_cast(Four, load_row4(p.bias[plane], n(i), columns(p, n(i)), t.is_bf16));
+  }
+}
+
+template <int N, typename M, typename F>
+__device__ __forceinline__ void load_residual(const LinearParams& p, Four (&r)[N], M m, F n) {
+  const FourType t = residual_type(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = Four{0u, 0u, 0u, 0u};
+  if (!p.residual) return;
+  const auto at = [&](int i) { return least(m(i), p.rows - 1) * p.residual_stride + least(n(i), p.n - 4); };
+  if (t.wide) {
+    if (t.is_bf16)
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = FourType{true, true}.load(p.residual, at(i));
+    else
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = FourType{true, false}.load(p.residual, at(i));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (m(i) < p.rows && n(i) < p.n)
+        r[i] = __builtin_bit_cast(Four, load_row4(p.residual, m(i) * p.residual_stride + n(i), columns(p, n(i)), t.is_bf16));
+  }
 }
 
 // act(y + bias), gated: times (up + its bias).
 template <bool GATED>
-__device__ __forceinline__ f32x4 activated(const LinearParams& p, const f32x4 (&bias)[GATED ? 2 : 1], f32x4 y, f32x4 up) {
-  y += bias[0];
+__device__ __forceinline__ f32x4 activated(const LinearParams& p, f32x4 bias, f32x4 up_bias, f32x4 y, f32x4 up) {
+  y += bias;
   if (p.act != kActNone)
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = activate(y[j], p.act);
-  if constexpr (GATED) y *= up + bias[1];
+  if constexpr (GATED) y *= up + up_bias;
   return y;
 }
 
@@ -215,6 +261,15 @@ __device__ __forceinline__ void barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// What a wave's lanes have written to LDS is read by its other lanes behind
+// this: a wave's accesses to LDS are made in their order, so that only the
+// compiler has to keep it.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // f(integral_constant<int, 0>{}), ..., f(integral_constant<int, N - 1>{}).
 template <typename F, int... J>
 __device__ __forceinline__ void each(F f, std::integer_sequence<int, J...>) {
@@ -237,8 +292,6 @@ __device__ __forceinline__ bool all(F f) {
 
 // (One value to the wave, which the compiler then keeps in a scalar register.)
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / 64); }
-
-__device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
 
 // Place of a workgroup in the order of the tiles (those of the first split,
 // then of the next): workgroups go to the eight XCDs in turn, and this gives
@@ -365,13 +418,14 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
   // A thread's outputs, and what they are made with (older than the chunks'
   // loads, so that waiting for these covers it).
   constexpr int kQuads = kCols / 4, kItems = BM * kQuads, kEach = (kItems + kThinThreads - 1) / kThinThreads;
-  Extra<GATED> extra[kEach];
-  if (p.splits == 1)
+  const auto m_of = [&](int e) { return m0 + (static_cast<int>(threadIdx.x) + e * kThinThreads) / kQuads; };
+  const auto n_of = [&](int e) { return n0 + (static_cast<int>(threadIdx.x) + e * kThinThreads) % kQuads * 4; };
+  Four bias[kPlanes][kEach], residual[kEach];
+  if (p.splits == 1) {
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = static_cast<int>(threadIdx.x) + e * kThinThreads;
-      extra[e] = load_extra<GATED>(p, m0 + i / kQuads, n0 + i % kQuads * 4);
-    }
+    for (int i = 0; i < kPlanes; ++i) load_bias(p, i, bias[i], n_of);
+    load_residual(p, residual, m_of, n_of);
+  }
   __builtin_amdgcn_sched_barrier(0);
 
   // Stage j's chunk has landed once all but the S - 2 newer ones have; behind
@@ -431,7 +485,8 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
     if (p.splits > 1)
       store_parts<GATED>(p, split, m, n, y, up);
     else
-      store_out(p, m, n, activated<GATED>(p, extra[e].bias, y, up) + extra[e].residual);
+      store_out(p, m, n, activated<GATED>(p, bias_type(p).value(bias[0][e]), bias_type(p).value(bias[kPlanes - 1][e]), y, up) +
+                             residual_type(p).value(residual[e]));
   }
 }
 
@@ -665,28 +720,36 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
   constexpr int kStride = 64 / kQuads, kRows = 32 / kStride;  // rows apart, and rows, of a lane
   const int q = lane % kQuads, r0 = lane / kQuads, n = n0 + (wn * kQuads + q) * 4;
   const bool whole = p.splits == 1, heavy = whole && (GATED || p.act != kActNone);
-  f32x4 bias[kPlanes];
+  const int first_row = m0 + wm * TM * 16 + r0;
+  Four ahead[kRows], stored[kPlanes][1];
+  const auto look_ahead = [&](int j) {
+    load_residual(p, ahead, [&](int i) { return first_row + j * 16 + i * kStride; }, [&](int) { return n; });
+  };
+  landed();
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
 #pragma unroll
-  for (int i = 0; i < kPlanes; ++i) bias[i] = load_bias(p, i, n);
+  for (int i = 0; i < kPlanes; ++i) load_bias(p, i, stored[i], [&](int) { return n; });
+  if (whole) look_ahead(0);
+  barrier();  // (the stages are free; from here on each wave keeps to its own part)
+  const f32x4 bias = bias_type(p).value(stored[0][0]), up_bias = bias_type(p).value(stored[kPlanes - 1][0]);
 #pragma unroll
   for (int j = 0; j < TM; j += 2) {
-    const int m = m0 + (wm * TM + j) * 16 + r0;
-    f32x4 residual[kRows];
-    if (whole)
+    const int m = first_row + j * 16;
+    Four residual[kRows];
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) residual[i] = load_residual(p, m + i * kStride, n);
-    landed();
-    __syncthreads();
+    for (int i = 0; i < kRows; ++i) residual[i] = ahead[i];
+    if (whole && j + 2 < TM) look_ahead(j + 2);
+    wave_sync();
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < TN; ++i) *place(16 * h + row, 4 * i + group) = acc[i][j + h];
-    __syncthreads();
+    wave_sync();
     if (heavy) {
 #pragma nounroll
       for (int i = 0; i < kRows; ++i) {
         f32x4* at = place(r0 + i * kStride, q);
-        *at = activated<GATED>(p, bias, *at, *place(r0 + i * kStride, q + (GATED ? kQuads : 0)));
+        *at = activated<GATED>(p, bias, up_bias, *at, *place(r0 + i * kStride, q + (GATED ? kQuads : 0)));
       }
     }
 #pragma unroll
@@ -697,8 +760,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LinearParams p) {
         store_parts<GATED>(p, split, m + i * kStride, n, y, *place(r0 + i * kStride, q + (GATED ? kQuads : 0)));
         continue;
       }
-      if (!heavy) y += bias[0];
-      store_out(p, m + i * kStride, n, y + residual[i]);
+      if (!heavy) y += bias;
+      store_out(p, m + i * kStride, n, y + residual_type(p).value(residual[i]));
     }
   }
 }
@@ -713,15 +776,29 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(LinearParams p) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kJoinThreads + threadIdx.x;
   if (i >= static_cast<int64_t>(quads) * p.rows) return;
   const int m = static_cast<int>(i / quads), n = static_cast<int>(i % quads) * 4;
-  const int count = p.n - n < 4 ? p.n - n : 4;
-  const Extra<GATED> extra = load_extra<GATED>(p, m, n);
+  Four bias[kPlanes][1], residual[1];
+#pragma unroll
+  for (int q = 0; q < kPlanes; ++q) load_bias(p, q, bias[q], [&](int) { return n; });
+  load_residual(p, residual, [&](int) { return m; }, [&](int) { return n; });
   f32x4 y[kPlanes];
 #pragma unroll
   for (int q = 0; q < kPlanes; ++q) {
-    y[q] = load_row4(p.part, part_at(p, 0, q, kPlanes, m, n), count, false);
-    for (int s = 1; s < p.splits; ++s) y[q] += load_row4(p.part, part_at(p, s, q, kPlanes, m, n), count, false);
+    y[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int64_t step = part_at(p, 1, q, kPlanes, m, n) - part_at(p, 0, q, kPlanes, m, n);
+    const float* from = p.part + part_at(p, 0, q, kPlanes, m, n);
+    int s = 0;
+    if (p.n % 4 == 0)
+      for (; s + 4 <= p.splits; s += 4, from += 4 * step) {
+        f32x4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const f32x4u*>(from + i * step);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[q] += v[i];
+      }
+    for (; s < p.splits; ++s, from += step) y[q] += load_row4(from, 0, columns(p, n), false);
   }
-  store_out(p, m, n, activated<GATED>(p, extra.bias, y[0], y[kPlanes - 1]) + extra.residual);
+  store_out(p, m, n, activated<GATED>(p, bias_type(p).value(bias[0][0]), bias_type(p).value(bias[kPlanes - 1][0]), y[0],
+                                      y[kPlanes - 1]) + residual_type(p).value(residual[0]));
 }
 
 // ---- norm --------------------------------------------------------------------
