@@ -284,3 +284,26 @@ def test_two_streams():
     torch.cuda.synchronize()
     for o, v in zip(outs, want):
         assert all(torch.equal(y, v) for y in o)
+
+
+# Shapes for each large tile whose columns are whole quads, where biases and residuals are loaded as quads: tiles that
+# end in the middle, rows and columns.
+QUADS = [(931, 608, 8416), (322, 632, 11000), (131, 608, 11196), (67, 656, 9624), (4101, 200, 4120), (534, 671, 172),
+         (64, 4096, 36), (33, 712, 4)]
+
+
+@pytest.mark.parametrize("kind,out_kind", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("m,k,n", QUADS)
+def test_biases_and_residuals_as_quads(kind, out_kind, m, k, n):
+    g = L.generator(m + n)
+    x = L.rows((m, k), 0, kind, g)
+    w, u = (L.rows((n, k), 0, kind, g, k ** -0.5) for _ in range(2))
+    b0, b1 = (L.rows((1, n), 0, kind, g)[0] for _ in range(2))
+    res = L.rows((m, n), 5, out_kind, g)
+    for act in ("none", "gelu"):
+        out = torch.full((m, n), math.nan, dtype=L.TYPES[out_kind], device=L.DEV)
+        run_linear(x, w, out, kind, out_kind, act, b0, res)
+        L.close(out, *L.linear(x, w, b0, act, res), out_kind)
+    out = torch.full((m, n), math.nan, dtype=L.TYPES[out_kind], device=L.DEV)
+    run_gated(x, w, u, out, kind, out_kind, "relu", b0, b1)
+    L.close(out, *L.gated(x, w, u, b0, b1, "relu"), out_kind)
