@@ -233,8 +233,8 @@ __global__ __launch_bounds__(kKvThreads) void append_kernel(AppendParams p) {
 // tokens (16 sequences 4.9 us; 512 over an fp8 cache, whose earlier codes may
 // have to be read and encoded again, 10.1 us). With head norms (NORM) a head's
 // row is held by a few lanes, which add its squares up: 64 single tokens, 28 over
-// 4 heads of 128, bf16 4.5 us, chunks of 9,187 tokens 34.7 (fp8 41.6 against 35.9
-// without norms: the sums in 64 bits, and keys made twice, once for the scale).
+// 4 heads of 128, bf16 4.0 us, chunks of 9,187 tokens from memory 44.6 (3.8 TB/s),
+// into an fp8 cache 48.9 (keys are made twice, once for the scale).
 //
 // The products of the rotation and their sum are rounded one by one (no
 // fused multiply-add), so codes do not depend on how the compiler contracts.
@@ -349,25 +349,25 @@ __device__ __forceinline__ int rope_units(const RopeParams& p) {
   return (p.interleaved && W > 1 ? p.rot / W : p.rot / 2 / W) + passed;
 }
 
-// x times the row's scale and its weights.
-template <int W, typename E>
-__device__ __forceinline__ void normalise(float (&x)[W], const E* weight, int at, float scale) {
+// x times the row's scale and its weights, one after the other.
+template <int W>
+__device__ __forceinline__ void normalise(float (&x)[W], const float (&weight)[W], float scale) {
 #pragma clang fp contract(off)
 #pragma unroll
-  for (int i = 0; i < W; ++i) x[i] = x[i] * scale;
-  if (weight) {
-    float w[W];
-    load_elems<W>(weight + at, w);
-#pragma unroll
-    for (int i = 0; i < W; ++i) x[i] = x[i] * w[i];
-  }
+  for (int i = 0; i < W; ++i) x[i] = x[i] * scale * weight[i];
 }
 
 // Elements `at` .. + W of a row, of a normalised one with its norm.
 template <int W, bool NORM, typename E>
 __device__ __forceinline__ void load_row(const E* src, const E* weight, float scale, int at, float (&x)[W]) {
   load_elems<W>(src + at, x);
-  if constexpr (NORM) normalise(x, weight, at, scale);
+  if constexpr (NORM) {
+    float w[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 1.f;
+    if (weight) load_elems<W>(weight + at, w);
+    normalise(x, w, scale);
+  }
 }
 
 template <int W, bool NORM, typename E>
@@ -461,11 +461,8 @@ __device__ __forceinline__ uint32_t rope_tokens(const RopeParams& p, const RopeI
 }
 
 // Eight elements of pairs, in place.
-__device__ __forceinline__ void turn_pairs(float (&x)[8], const float* cos, const float* sin) {
+__device__ __forceinline__ void turn_pairs(float (&x)[8], const float (&c)[4], const float (&s)[4]) {
 #pragma clang fp contract(off)
-  float c[4], s[4];
-  load_elems<4>(cos, c);
-  load_elems<4>(sin, s);
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     const float xc = x[i] * c[i / 2], ys = x[i + 1] * s[i / 2], yc = x[i + 1] * c[i / 2], xs = x[i] * s[i / 2];
@@ -475,14 +472,12 @@ __device__ __forceinline__ void turn_pairs(float (&x)[8], const float* cos, cons
 }
 
 // Eight pairs of two halves, in place.
-__device__ __forceinline__ void turn_halves(float (&x)[8], float (&y)[8], const float* cos, const float* sin) {
+__device__ __forceinline__ void turn_halves(float (&x)[8], float (&y)[8], const float (&c)[2][4], const float (&s)[2][4]) {
 #pragma clang fp contract(off)
-  float c[8], s[8];
-  load_elems<8>(cos, c);
-  load_elems<8>(sin, s);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float xc = x[i] * c[i], ys = y[i] * s[i], yc = y[i] * c[i], xs = x[i] * s[i];
+    const float xc = x[i] * c[i / 4][i % 4], ys = y[i] * s[i / 4][i % 4], yc = y[i] * c[i / 4][i % 4],
+                xs = x[i] * s[i / 4][i % 4];
     x[i] = xc - ys;
     y[i] = yc + xs;
   }
@@ -500,13 +495,26 @@ __device__ __forceinline__ void rope_each(const RopeParams& p, const RopeItem& i
   const int units = rope_units<W>(p), heads = h1 - h0;
   if constexpr (NORM && W == 8) {
     // Sixteen elements to a lane, which stay in registers between the sum and
-    // the turn: eight pairs of two halves, or sixteen adjacent ones. (Four and
-    // two rows at a time, for more loads under way, were slower: 9187 tokens,
-    // 28 over 4 heads of 128, bf16 34.7 us at one row, 37 at two, 49 at four.)
+    // the turn: eight pairs of two halves, or sixteen adjacent ones. A row and
+    // what turns it are loaded at once, the weights before all rows (one behind
+    // the other they made three round trips: 9187 tokens, 28 over 4 heads of
+    // 128, bf16 47.0 -> 44.6 us). Loading the next row ahead took 45.5 us, two
+    // and four rows at a time more still.
     const int lanes = p.head_dim / 16, log = 31 - __builtin_clz(lanes), half = p.rot / 2;
     const int lane = static_cast<int>(threadIdx.x) & (lanes - 1), turned = p.interleaved ? 0 : half / 8;
     const bool halves = lane < turned;
     const int at0 = halves ? lane * 8 : (p.interleaved ? 0 : p.rot) + (lane - turned) * 16, at1 = halves ? half + lane * 8 : at0 + 8;
+    // What a row is turned by (rows that are not turned load it too, and leave
+    // it), and the weights, which are the lane's for all rows.
+    const int turn0 = least_int(p.interleaved ? at0 / 2 : lane * 8, half - (p.interleaved ? 4 : 8));
+    const int turn1 = p.interleaved ? least_int(at1 / 2, half - 4) : turn0 + 4;
+    float w0[8], w1[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w0[i] = w1[i] = 1.f;
+    if (weight) {
+      load_elems<8>(weight + at0, w0);
+      load_elems<8>(weight + at1, w1);
+    }
     // (`first` and kRopeThreads are multiples of lanes, a power of two.)
     const int rows = least_int(last >> log, it.n * heads), step = kRopeThreads >> log;
     const int step_t = step / heads, step_h = step % heads;
@@ -521,17 +529,24 @@ __device__ __forceinline__ void rope_each(const RopeParams& p, const RopeItem& i
       r.at[1] = at1;
       load_elems<8>(from + at0, r.x[0]);
       load_elems<8>(from + at1, r.x[1]);
+      float c[2][4], s[2][4];
+      if (p.rot > 0) {
+        const int64_t angle = rope_pos(p, it, t) * half;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          load_elems<4>(p.cos + angle + (k ? turn1 : turn0), c[k]);
+          load_elems<4>(p.sin + angle + (k ? turn1 : turn0), s[k]);
+        }
+      }
       double sum = squares(r.x[0]) + squares(r.x[1]);
       for (int o = lanes / 2; o > 0; o /= 2) sum += __shfl_xor(sum, o);
       const float scale = head_scale(p, sum);
-      normalise(r.x[0], weight, at0, scale);
-      normalise(r.x[1], weight, at1, scale);
-      const int64_t angle = p.rot > 0 ? rope_pos(p, it, t) * half : 0;
-      if (halves)
-        turn_halves(r.x[0], r.x[1], p.cos + angle + at0, p.sin + angle + at0);
+      normalise(r.x[0], w0, scale);
+      normalise(r.x[1], w1, scale);
+      if (halves) turn_halves(r.x[0], r.x[1], c, s);
       if (p.interleaved) {
-        if (at0 < p.rot) turn_pairs(r.x[0], p.cos + angle + at0 / 2, p.sin + angle + at0 / 2);
-        if (at1 < p.rot) turn_pairs(r.x[1], p.cos + angle + at1 / 2, p.sin + angle + at1 / 2);
+        if (at0 < p.rot) turn_pairs(r.x[0], c[0], s[0]);
+        if (at1 < p.rot) turn_pairs(r.x[1], c[1], s[1]);
       }
       f(t, h, r);
     }
