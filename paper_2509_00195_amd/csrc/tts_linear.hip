@@ -317,7 +317,7 @@ constexpr int kThinRow = kThinChunk;  // bytes of a row to a stage: a quarter to
 // that each byte is read from LDS once; the waves' sums are added at the end,
 // in their order. Measured (bf16): 1 x 1536 x 2048 4.4 us and 16 x 1536 x 6144
 // gated 9.0 (launches 3.5), 64 x 3584 x 4608 11.2, of which 33 MB of weights are
-// 6.6 at a copy's rate: 144 workgroups of 32 x 48, none of which fills a unit.
+// 6.6 at a copy's rate: 192 workgroups of 32 x 48, each of which draws 0.57 MB.
 // Rows of 64 bytes to a stage, for more stages, were slower.
 template <typename E, int BM, int BN, int S, bool GATED, bool ALIGNED>
 __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
