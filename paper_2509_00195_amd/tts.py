@@ -545,6 +545,27 @@ def _type(x) -> int:
     return DTYPES[x] if isinstance(x, str) else int(x)
 
 
+_TAKEN: dict = {}  # torch's type -> the types that its elements are taken as
+
+
+def _typed(x, dtype: int, name: str) -> None:
+    """Refuses elements that are not of a call's type (integers as wide pass: they are taken as bits)."""
+    taken = _TAKEN.get(x.dtype)
+    if taken is None:
+        floats = {"torch.float32": (TTS_F32,), "torch.bfloat16": (TTS_BF16,)}
+        bits = {} if x.dtype.is_floating_point or x.dtype.is_complex else {4: (TTS_F32,), 2: (TTS_BF16,)}
+        taken = _TAKEN[x.dtype] = floats.get(str(x.dtype)) or bits.get(x.dtype.itemsize, ())
+    if dtype not in taken:
+        raise ValueError(f"{name}: elements of {x.dtype}")
+
+
+def _vector(x, n: int, dtype: int, name: str) -> None:
+    """Refuses a vector of fewer than n elements, or of another type than the call's."""
+    if x is not None and not isinstance(x, int):
+        _typed(x, dtype, name)
+        _holds(x, n * (4 if dtype == TTS_F32 else 2), name)
+
+
 def make_linear(in_features: int, out_features: int, dtype="bf16", out_dtype="bf16", act="none") -> tts_linear_desc:
     return tts_linear_desc(in_features, out_features, _type(dtype), _type(out_dtype),
                            ACTS[act] if isinstance(act, str) else int(act))
@@ -562,8 +583,7 @@ def _matrix(x, rows: int, cols: int, dtype: int, name: str):
     shape = x.shape
     if len(shape) != 2 or shape[1] != cols or shape[0] < rows:
         raise ValueError(f"{name}: expected [{rows}][{cols}], got {tuple(shape)}")
-    if x.itemsize != (4 if dtype == TTS_F32 else 2):
-        raise ValueError(f"{name}: elements of {x.dtype}")
+    _typed(x, dtype, name)
     row, col = x.stride()
     if col != 1 and cols > 1 and shape[0]:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
@@ -586,7 +606,7 @@ def tts_linear(desc: tts_linear_desc, num_rows: int, x, w, out, bias=None, resid
     wp, ws = _matrix(w, n, k, t, "w")
     rp, rs = _matrix(residual, num_rows, n, o, "residual")
     op, os_ = _matrix(out, num_rows, n, o, "out")
-    _holds(bias, n * (4 if t == TTS_F32 else 2), "bias")
+    _vector(bias, n, t, "bias")
     _check(load().tts_linear(C.byref(desc), num_rows, xp, xs, wp, ws, _ptr(bias), rp, rs, op, os_, _ptr(workspace),
                              workspace_bytes, _stream(stream)))
 
@@ -601,8 +621,8 @@ def tts_gated_linear(desc: tts_linear_desc, num_rows: int, x, w_gate, w_up, out,
     if gs != us:
         raise ValueError("w_gate and w_up must have one row stride")
     op, os_ = _matrix(out, num_rows, n, desc.out_dtype, "out")
-    for b, name in ((bias_gate, "bias_gate"), (bias_up, "bias_up")):
-        _holds(b, n * (4 if t == TTS_F32 else 2), name)
+    _vector(bias_gate, n, t, "bias_gate")
+    _vector(bias_up, n, t, "bias_up")
     _check(load().tts_gated_linear(C.byref(desc), num_rows, xp, xs, gp, up, gs, _ptr(bias_gate), _ptr(bias_up), op, os_,
                                    _ptr(workspace), workspace_bytes, _stream(stream)))
 
@@ -611,7 +631,7 @@ def tts_rms_norm(desc: tts_norm_desc, num_rows: int, x, weight, out, stream=None
     """x and out [num_rows][row_len], whose rows may lie apart; weight [row_len] or None."""
     xp, xs = _matrix(x, num_rows, desc.row_len, desc.dtype, "x")
     op, os_ = _matrix(out, num_rows, desc.row_len, desc.out_dtype, "out")
-    _holds(weight, desc.row_len * (4 if desc.dtype == TTS_F32 else 2), "weight")
+    _vector(weight, desc.row_len, desc.dtype, "weight")
     _check(load().tts_rms_norm(C.byref(desc), num_rows, xp, xs, _ptr(weight), op, os_, _stream(stream)))
 
 

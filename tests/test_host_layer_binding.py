@@ -1,0 +1,95 @@
+"""What the binding refuses of the tensors that a layer's products, norm and appends are given (CPU: nothing is launched)."""
+
+import pytest
+import torch
+
+from paper_2509_00195_amd import tts as T
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture
+def launched(monkeypatch):
+    """The entry points' arguments, in the place of their calls."""
+    calls = []
+    lib = T.load()
+
+    class Spy:
+        def __getattr__(self, name):
+            if name == "tts_last_error":
+                return getattr(lib, name)
+            return lambda *a: calls.append((name, a)) or 0
+
+    spy = Spy()
+    monkeypatch.setattr(T, "load", lambda: spy)
+    return calls
+
+
+def _linear(t=BF16, to=BF16, kind="bf16", out_kind="bf16", **kw):
+    m, k, n = 4, 64, 32
+    args = dict(x=torch.zeros((m, k), dtype=t), w=torch.zeros((n, k), dtype=t), out=torch.zeros((m, n), dtype=to),
+                bias=torch.zeros(n, dtype=t), residual=torch.zeros((m, n), dtype=to))
+    args.update(kw)
+    T.tts_linear(T.make_linear(k, n, kind, out_kind), m, **args)
+
+
+def _gated(t=BF16, **kw):
+    m, k, n = 4, 64, 32
+    args = dict(x=torch.zeros((m, k), dtype=t), w_gate=torch.zeros((n, k), dtype=t), w_up=torch.zeros((n, k), dtype=t),
+                out=torch.zeros((m, n), dtype=t), bias_gate=torch.zeros(n, dtype=t), bias_up=torch.zeros(n, dtype=t))
+    args.update(kw)
+    T.tts_gated_linear(T.make_linear(k, n), m, **args)
+
+
+def _rms(t=BF16, kind="bf16", **kw):
+    args = dict(x=torch.zeros((4, 64), dtype=t), weight=torch.zeros(64, dtype=t), out=torch.zeros((4, 64), dtype=t))
+    args.update(kw)
+    T.tts_rms_norm(T.make_norm(64, 1e-6, kind, kind), 4, **args)
+
+
+def test_tensors_of_the_calls_types_pass(launched):
+    _linear()
+    _linear(F32, BF16, "f32", "bf16")
+    _linear(BF16, F32, "bf16", "f32")
+    _gated()
+    _rms()
+    _rms(F32, "f32")
+    # (Elements as bits, longer vectors, none.)
+    _linear(torch.int16, torch.int16)
+    _linear(bias=torch.zeros(40, dtype=BF16))
+    _rms(weight=None)
+    assert len(launched) == 9
+
+
+@pytest.mark.parametrize("t", [F32, torch.float64, F16])
+def test_vectors_of_another_type(launched, t):
+    """A weight in 32 bits beside rows of bf16 holds bytes enough, but is not what the call reads."""
+    with pytest.raises(ValueError, match="bias"):
+        _linear(bias=torch.zeros(32, dtype=t))
+    for name in ("bias_gate", "bias_up"):
+        with pytest.raises(ValueError, match=name):
+            _gated(**{name: torch.zeros(32, dtype=t)})
+    with pytest.raises(ValueError, match="weight"):
+        _rms(weight=torch.zeros(64, dtype=t))
+    assert not launched
+
+
+def test_vectors_of_32_bits_are_refused_others(launched):
+    with pytest.raises(ValueError, match="bias"):
+        _linear(F32, F32, "f32", "f32", bias=torch.zeros(64, dtype=BF16))
+    with pytest.raises(ValueError, match="weight"):
+        _rms(F32, "f32", weight=torch.zeros(128, dtype=BF16))
+    assert not launched
+
+
+def test_half_precision_is_not_bf16(launched):
+    for name, shape in (("x", (4, 64)), ("w", (32, 64)), ("out", (4, 32)), ("residual", (4, 32))):
+        with pytest.raises(ValueError, match=name):
+            _linear(**{name: torch.zeros(shape, dtype=F16)})
+    for name in ("w_gate", "w_up"):
+        with pytest.raises(ValueError, match=name):
+            _gated(**{name: torch.zeros((32, 64), dtype=F16)})
+    for name in ("x", "out"):
+        with pytest.raises(ValueError, match=name):
+            _rms(**{name: torch.zeros((4, 64), dtype=F16)})
+    assert not launched
