@@ -520,8 +520,11 @@ def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_ne
 
 
 def make_head_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> tts_head_norm_desc:
-    """Head norms with device weights [head_dim] in the queries' type (which the caller keeps; None: ones)."""
-    return tts_head_norm_desc(float(eps), _ptr(q_weight), _ptr(k_weight))
+    """Head norms with device weights [head_dim] in the queries' type (None: ones). Tensors are kept with the descriptor,
+    and checked by the calls that take it."""
+    norm = tts_head_norm_desc(float(eps), _ptr(q_weight), _ptr(k_weight))
+    norm.weights = (q_weight, k_weight)
+    return norm
 
 
 def tts_norm_rope_append_kv(desc: tts_attn_desc, norm: tts_head_norm_desc, num_seqs: int, num_tokens: int, k_new, v_new,
@@ -530,6 +533,8 @@ def tts_norm_rope_append_kv(desc: tts_attn_desc, norm: tts_head_norm_desc, num_s
                             tok_offsets=None, positions=None, stream=None):
     """Tensors as for tts_rope_append_kv."""
     hq, hkv, d, size = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, 4 if desc.q_dtype == TTS_F32 else 2
+    for w, name in zip(getattr(norm, "weights", ()), ("q_weight", "k_weight")):
+        _vector(w, d, desc.q_dtype, name)
     qp, qs = _rows(q, hq, d, num_tokens, size)
     kp, ks = _rows(k_new, hkv, d, num_tokens, size)
     vp, vs = _rows(v_new, hkv, d, num_tokens, size)

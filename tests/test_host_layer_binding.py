@@ -93,3 +93,34 @@ def test_half_precision_is_not_bf16(launched):
         with pytest.raises(ValueError, match=name):
             _rms(**{name: torch.zeros((4, 64), dtype=F16)})
     assert not launched
+
+
+def _append(norm, d=64, t=BF16, kind="bf16"):
+    hq, hkv, n = 4, 2, 3
+    x = torch.zeros((n, hq + 2 * hkv, d), dtype=t)
+    a = 1 << 20
+    T.tts_norm_rope_append_kv(T.make_desc(hq, hkv, d, q_dtype=kind, kv_dtype=kind), norm, n, n, x[:, hq:hq + hkv],
+                              x[:, hq + hkv:], a, 4, a, 8, a, a, q=x[:, :hq], q_out=torch.zeros((n, hq, d), dtype=t))
+
+
+@pytest.mark.parametrize("which", ["q_weight", "k_weight"])
+def test_head_norm_weights_of_another_size_or_type(launched, which):
+    """A weight of too few elements would be read past its end."""
+    for w in (torch.zeros(63, dtype=BF16), torch.zeros(64, dtype=F32), torch.zeros(64, dtype=F16)):
+        with pytest.raises(ValueError, match=which):
+            _append(T.make_head_norm(**{which: w}))
+    with pytest.raises(ValueError, match=which):
+        _append(T.make_head_norm(**{which: torch.zeros(64, dtype=BF16)}), d=128)
+    for w in (torch.zeros(64, dtype=BF16), torch.zeros(128, dtype=BF16)):
+        with pytest.raises(ValueError, match=which):
+            _append(T.make_head_norm(**{which: w}), t=F32, kind="f32")
+    assert not launched
+
+
+def test_head_norm_weights_that_fit(launched):
+    _append(T.make_head_norm(torch.zeros(64, dtype=BF16), torch.zeros(72, dtype=BF16)))
+    _append(T.make_head_norm(torch.zeros(64), None), t=F32, kind="f32")
+    _append(T.make_head_norm())
+    _append(T.make_head_norm(1 << 20, 1 << 20))  # (addresses are the caller's)
+    _append(T.tts_head_norm_desc(1e-6, None, None))
+    assert len(launched) == 5
