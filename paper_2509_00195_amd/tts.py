@@ -66,6 +66,7 @@ class tts_rope_desc(C.Structure):
 
 class tts_head_norm_desc(C.Structure):
     _fields_ = [("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+    held = None  # what is known of the weights (make_head_norm): each one's elements, and the types they are taken as
 
 
 class tts_linear_desc(C.Structure):
@@ -520,10 +521,11 @@ def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_ne
 
 
 def make_head_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> tts_head_norm_desc:
-    """Head norms with device weights [head_dim] in the queries' type (None: ones). Tensors are kept with the descriptor,
-    and checked by the calls that take it."""
+    """Head norms with device weights [head_dim] in the queries' type (which the caller keeps; None: ones). The calls that
+    take the descriptor check that they fit."""
     norm = tts_head_norm_desc(float(eps), _ptr(q_weight), _ptr(k_weight))
-    norm.weights = (q_weight, k_weight)
+    norm.held = [(name, w.numel(), _TAKEN[w.dtype]) for name, w in (("q_weight", q_weight), ("k_weight", k_weight))
+                 if w is not None and not isinstance(w, int)]
     return norm
 
 
@@ -533,8 +535,9 @@ def tts_norm_rope_append_kv(desc: tts_attn_desc, norm: tts_head_norm_desc, num_s
                             tok_offsets=None, positions=None, stream=None):
     """Tensors as for tts_rope_append_kv."""
     hq, hkv, d, size = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, 4 if desc.q_dtype == TTS_F32 else 2
-    for w, name in zip(getattr(norm, "weights", ()), ("q_weight", "k_weight")):
-        _vector(w, d, desc.q_dtype, name)
+    for name, elements, taken in (norm.held or ()) if norm is not None else ():
+        if elements < d or desc.q_dtype not in taken:
+            raise ValueError(f"{name} is not a vector of {d} elements of the queries' type")
     qp, qs = _rows(q, hq, d, num_tokens, size)
     kp, ks = _rows(k_new, hkv, d, num_tokens, size)
     vp, vs = _rows(v_new, hkv, d, num_tokens, size)
@@ -550,25 +553,32 @@ def _type(x) -> int:
     return DTYPES[x] if isinstance(x, str) else int(x)
 
 
-_TAKEN: dict = {}  # torch's type -> the types that its elements are taken as
+class _Taken(dict):
+    """torch's type -> the types that its elements are taken as (integers as wide are taken as bits)."""
+
+    def __missing__(self, t):
+        if t.is_floating_point or t.is_complex:
+            taken = {"torch.float32": (TTS_F32,), "torch.bfloat16": (TTS_BF16,)}.get(str(t), ())
+        else:
+            taken = {4: (TTS_F32,), 2: (TTS_BF16,)}.get(t.itemsize, ())
+        self[t] = taken
+        return taken
 
 
-def _typed(x, dtype: int, name: str) -> None:
-    """Refuses elements that are not of a call's type (integers as wide pass: they are taken as bits)."""
-    taken = _TAKEN.get(x.dtype)
-    if taken is None:
-        floats = {"torch.float32": (TTS_F32,), "torch.bfloat16": (TTS_BF16,)}
-        bits = {} if x.dtype.is_floating_point or x.dtype.is_complex else {4: (TTS_F32,), 2: (TTS_BF16,)}
-        taken = _TAKEN[x.dtype] = floats.get(str(x.dtype)) or bits.get(x.dtype.itemsize, ())
-    if dtype not in taken:
+_TAKEN = _Taken()
+
+
+def _vector(x, n: int, dtype: int, name: str) -> Optional[int]:
+    """The address of a vector of n elements or more of a type."""
+    if x is None or isinstance(x, int):
+        return x
+    if dtype not in _TAKEN[x.dtype]:
         raise ValueError(f"{name}: elements of {x.dtype}")
-
-
-def _vector(x, n: int, dtype: int, name: str) -> None:
-    """Refuses a vector of fewer than n elements, or of another type than the call's."""
-    if x is not None and not isinstance(x, int):
-        _typed(x, dtype, name)
-        _holds(x, n * (4 if dtype == TTS_F32 else 2), name)
+    if x.numel() < n:
+        raise ValueError(f"{name} holds {x.numel()} elements, the call takes {n}")
+    if not x.is_contiguous():
+        raise ValueError(f"{name}: device tensors must be contiguous")
+    return x.data_ptr()
 
 
 def make_linear(in_features: int, out_features: int, dtype="bf16", out_dtype="bf16", act="none") -> tts_linear_desc:
@@ -588,7 +598,8 @@ def _matrix(x, rows: int, cols: int, dtype: int, name: str):
     shape = x.shape
     if len(shape) != 2 or shape[1] != cols or shape[0] < rows:
         raise ValueError(f"{name}: expected [{rows}][{cols}], got {tuple(shape)}")
-    _typed(x, dtype, name)
+    if dtype not in _TAKEN[x.dtype]:
+        raise ValueError(f"{name}: elements of {x.dtype}")
     row, col = x.stride()
     if col != 1 and cols > 1 and shape[0]:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
@@ -611,8 +622,8 @@ def tts_linear(desc: tts_linear_desc, num_rows: int, x, w, out, bias=None, resid
     wp, ws = _matrix(w, n, k, t, "w")
     rp, rs = _matrix(residual, num_rows, n, o, "residual")
     op, os_ = _matrix(out, num_rows, n, o, "out")
-    _vector(bias, n, t, "bias")
-    _check(load().tts_linear(C.byref(desc), num_rows, xp, xs, wp, ws, _ptr(bias), rp, rs, op, os_, _ptr(workspace),
+    bp = _vector(bias, n, t, "bias")
+    _check(load().tts_linear(C.byref(desc), num_rows, xp, xs, wp, ws, bp, rp, rs, op, os_, _ptr(workspace),
                              workspace_bytes, _stream(stream)))
 
 
@@ -626,18 +637,17 @@ def tts_gated_linear(desc: tts_linear_desc, num_rows: int, x, w_gate, w_up, out,
     if gs != us:
         raise ValueError("w_gate and w_up must have one row stride")
     op, os_ = _matrix(out, num_rows, n, desc.out_dtype, "out")
-    _vector(bias_gate, n, t, "bias_gate")
-    _vector(bias_up, n, t, "bias_up")
-    _check(load().tts_gated_linear(C.byref(desc), num_rows, xp, xs, gp, up, gs, _ptr(bias_gate), _ptr(bias_up), op, os_,
-                                   _ptr(workspace), workspace_bytes, _stream(stream)))
+    bg, bu = _vector(bias_gate, n, t, "bias_gate"), _vector(bias_up, n, t, "bias_up")
+    _check(load().tts_gated_linear(C.byref(desc), num_rows, xp, xs, gp, up, gs, bg, bu, op, os_, _ptr(workspace),
+                                   workspace_bytes, _stream(stream)))
 
 
 def tts_rms_norm(desc: tts_norm_desc, num_rows: int, x, weight, out, stream=None):
     """x and out [num_rows][row_len], whose rows may lie apart; weight [row_len] or None."""
     xp, xs = _matrix(x, num_rows, desc.row_len, desc.dtype, "x")
     op, os_ = _matrix(out, num_rows, desc.row_len, desc.out_dtype, "out")
-    _vector(weight, desc.row_len, desc.dtype, "weight")
-    _check(load().tts_rms_norm(C.byref(desc), num_rows, xp, xs, _ptr(weight), op, os_, _stream(stream)))
+    wp = _vector(weight, desc.row_len, desc.dtype, "weight")
+    _check(load().tts_rms_norm(C.byref(desc), num_rows, xp, xs, wp, op, os_, _stream(stream)))
 
 
 def tts_paged_prefill_workspace_size(desc: tts_attn_desc, num_seqs: int, num_tokens: int, max_seq_len: int) -> int:
