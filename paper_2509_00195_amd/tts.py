@@ -66,7 +66,8 @@ class tts_rope_desc(C.Structure):
 
 class tts_head_norm_desc(C.Structure):
     _fields_ = [("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
-    held = None  # what is known of the weights (make_head_norm): each one's elements, and the types they are taken as
+    held = (None, None)  # the weights' tensors, where they are known (make_head_norm)
+    fits = None  # the heads that they have been found to fit: (dims, type)
 
 
 class tts_linear_desc(C.Structure):
@@ -218,12 +219,11 @@ def _ptr(x) -> Optional[int]:
     if x is None or isinstance(x, int):
         return x
     try:
-        contiguous, at = x.is_contiguous(), x.data_ptr()
+        if x.is_contiguous():
+            return x.data_ptr()
     except AttributeError:
         raise TypeError(f"cannot pass {type(x)} as a device pointer") from None
-    if not contiguous:
-        raise ValueError("device tensors must be contiguous")
-    return at
+    raise ValueError("device tensors must be contiguous")
 
 
 def _stream(stream) -> Optional[int]:
@@ -471,26 +471,31 @@ def make_rope(cos, sin, interleaved: bool = False) -> tts_rope_desc:
     shape = cos.shape
     if len(shape) != 2 or shape != sin.shape:
         raise ValueError("cos and sin must both be [max_pos][rot_dim / 2]")
-    if cos.dtype.itemsize != 4 or not cos.dtype.is_floating_point or sin.dtype != cos.dtype:
+    t = cos.dtype
+    if t.itemsize != 4 or not t.is_floating_point or sin.dtype != t:
         raise ValueError("cos and sin must be float32")
-    return tts_rope_desc(2 * shape[1], 1 if interleaved else 0, shape[0], _ptr(cos), _ptr(sin))
+    if not (cos.is_contiguous() and sin.is_contiguous()):
+        raise ValueError("device tensors must be contiguous")
+    return tts_rope_desc(2 * shape[1], 1 if interleaved else 0, shape[0], cos.data_ptr(), sin.data_ptr())
 
 
-def _rows(x, heads: int, head_dim: int, tokens: int = 0, itemsize: int = 0):
+def _rows(x, heads: int, head_dim: int, tokens: int = 0, dtype: Optional[int] = None):
     """(address, elements between tokens) of [tokens][heads][head_dim] rows whose tokens may lie apart; at least `tokens`
-    of them, of elements of `itemsize` bytes (0: any)."""
+    of them, of elements of a type (None: any)."""
     if x is None:
         return None, 0
     if isinstance(x, int):
         return x, heads * head_dim
-    shape = x.shape
-    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
-        raise ValueError(f"expected rows of [{heads}][{head_dim}], got {tuple(shape)}")
-    n = shape[0]
+    try:
+        n, h, d = x.shape
+    except ValueError:
+        n, h, d = 0, 0, 0
+    if h != heads or d != head_dim:
+        raise ValueError(f"expected rows of [{heads}][{head_dim}], got {tuple(x.shape)}")
     if n < tokens:
         raise ValueError(f"expected {tokens} tokens, got {n}")
-    if itemsize and x.itemsize != itemsize:
-        raise ValueError(f"expected elements of {itemsize} bytes, got {x.dtype}")
+    if dtype is not None and dtype not in _TAKEN[x.dtype]:
+        raise ValueError(f"expected elements of the queries' type, got {x.dtype}")
     token, head, dim = x.stride()
     if n and (dim != 1 or (head != head_dim and heads > 1)):
         raise ValueError("the heads of a token must be contiguous")
@@ -503,29 +508,42 @@ def _holds(x, nbytes: int, name: str) -> None:
         raise ValueError(f"{name} holds {x.nbytes} bytes, the call takes {nbytes}")
 
 
+def _queries(x, nbytes: int, dtype: int) -> Optional[int]:
+    """The address of a tensor that takes a call's queries: of bytes enough, and of no other float than the call's."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.nbytes < nbytes:
+        raise ValueError(f"q_out holds {x.nbytes} bytes, the call takes {nbytes}")
+    t = x.dtype
+    if dtype not in _TAKEN[t] and t.is_floating_point:
+        raise ValueError(f"q_out: elements of {t}")
+    if not x.is_contiguous():
+        raise ValueError("device tensors must be contiguous")
+    return x.data_ptr()
+
+
 def tts_rope_append_kv(desc: tts_attn_desc, num_seqs: int, num_tokens: int, k_new, v_new, block_tables,
                        max_blocks_per_seq: int, seq_lens, num_blocks: int, k_cache, v_cache, k_scale=None, v_scale=None,
                        rope: Optional[tts_rope_desc] = None, q=None, q_out=None, tok_offsets=None, positions=None,
                        stream=None):
     """q, k_new and v_new: [tokens][heads][head_dim], possibly views of one projection's output, of num_tokens tokens at
     least."""
-    hq, hkv, d, size = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, 4 if desc.q_dtype == TTS_F32 else 2
-    qp, qs = _rows(q, hq, d, num_tokens, size)
-    kp, ks = _rows(k_new, hkv, d, num_tokens, size)
-    vp, vs = _rows(v_new, hkv, d, num_tokens, size)
-    _holds(q_out, num_tokens * hq * d * size, "q_out")
+    hq, hkv, d, t = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.q_dtype
+    qp, qs = _rows(q, hq, d, num_tokens, t)
+    kp, ks = _rows(k_new, hkv, d, num_tokens, t)
+    vp, vs = _rows(v_new, hkv, d, num_tokens, t)
+    op = _queries(q_out, num_tokens * hq * d * (4 if t == TTS_F32 else 2), t)
     _check(load().tts_rope_append_kv(
         C.byref(desc), C.byref(rope) if rope is not None else None, num_seqs, num_tokens, _ptr(tok_offsets),
         _ptr(positions), qp, qs, kp, ks, vp, vs, _ptr(block_tables), max_blocks_per_seq, _ptr(seq_lens), num_blocks,
-        _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
+        op, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
 
 
 def make_head_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> tts_head_norm_desc:
-    """Head norms with device weights [head_dim] in the queries' type (which the caller keeps; None: ones). The calls that
-    take the descriptor check that they fit."""
+    """Head norms with device weights [head_dim] in the queries' type (None: ones). Tensors are kept with the descriptor,
+    and the calls that take it check that they fit."""
     norm = tts_head_norm_desc(float(eps), _ptr(q_weight), _ptr(k_weight))
-    norm.held = [(name, w.numel(), _TAKEN[w.dtype]) for name, w in (("q_weight", q_weight), ("k_weight", k_weight))
-                 if w is not None and not isinstance(w, int)]
+    norm.held = q_weight, k_weight
     return norm
 
 
@@ -534,19 +552,20 @@ def tts_norm_rope_append_kv(desc: tts_attn_desc, norm: tts_head_norm_desc, num_s
                             k_scale=None, v_scale=None, rope: Optional[tts_rope_desc] = None, q=None, q_out=None,
                             tok_offsets=None, positions=None, stream=None):
     """Tensors as for tts_rope_append_kv."""
-    hq, hkv, d, size = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, 4 if desc.q_dtype == TTS_F32 else 2
-    for name, elements, taken in (norm.held or ()) if norm is not None else ():
-        if elements < d or desc.q_dtype not in taken:
-            raise ValueError(f"{name} is not a vector of {d} elements of the queries' type")
-    qp, qs = _rows(q, hq, d, num_tokens, size)
-    kp, ks = _rows(k_new, hkv, d, num_tokens, size)
-    vp, vs = _rows(v_new, hkv, d, num_tokens, size)
-    _holds(q_out, num_tokens * hq * d * size, "q_out")
+    hq, hkv, d, t = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.q_dtype
+    if norm is not None and norm.fits != (d, t):
+        for w, name in zip(norm.held, ("q_weight", "k_weight")):
+            if w is not None and type(w) is not int and (w.numel() < d or t not in _TAKEN[w.dtype]):
+                raise ValueError(f"{name} is not a vector of {d} elements of the queries' type")
+        norm.fits = d, t
+    qp, qs = _rows(q, hq, d, num_tokens, t)
+    kp, ks = _rows(k_new, hkv, d, num_tokens, t)
+    vp, vs = _rows(v_new, hkv, d, num_tokens, t)
+    op = _queries(q_out, num_tokens * hq * d * (4 if t == TTS_F32 else 2), t)
     _check(load().tts_norm_rope_append_kv(
         C.byref(desc), C.byref(norm) if norm is not None else None, C.byref(rope) if rope is not None else None, num_seqs,
         num_tokens, _ptr(tok_offsets), _ptr(positions), qp, qs, kp, ks, vp, vs, _ptr(block_tables), max_blocks_per_seq,
-        _ptr(seq_lens), num_blocks, _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
-        _stream(stream)))
+        _ptr(seq_lens), num_blocks, op, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream)))
 
 
 def _type(x) -> int:

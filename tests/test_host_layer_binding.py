@@ -124,3 +124,31 @@ def test_head_norm_weights_that_fit(launched):
     _append(T.make_head_norm(1 << 20, 1 << 20))  # (addresses are the caller's)
     _append(T.tts_head_norm_desc(1e-6, None, None))
     assert len(launched) == 5
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("which", ["q", "k_new", "v_new", "q_out"])
+def test_appended_rows_of_another_type(launched, norm, which):
+    """fp16 rows are as wide as bf16 ones, and are not what either append reads; nor do queries go into another float."""
+    hq, hkv, d, n, a = 4, 2, 64, 3, 1 << 20
+    args = dict(q=torch.zeros((n, hq, d), dtype=BF16), k_new=torch.zeros((n, hkv, d), dtype=BF16),
+                v_new=torch.zeros((n, hkv, d), dtype=BF16), q_out=torch.zeros((n, hq, d), dtype=BF16))
+    desc = T.make_desc(hq, hkv, d)
+
+    def call(x):
+        rest = dict(k_new=x["k_new"], v_new=x["v_new"], block_tables=a, max_blocks_per_seq=4, seq_lens=a, num_blocks=8,
+                    k_cache=a, v_cache=a, q=x["q"], q_out=x["q_out"], rope=T.tts_rope_desc(64, 0, 16, a, a))
+        if norm:
+            T.tts_norm_rope_append_kv(desc, T.make_head_norm(), n, n, **rest)
+        else:
+            T.tts_rope_append_kv(desc, n, n, **rest)
+
+    call(args)
+    call({k: x.view(torch.int16) for k, x in args.items()})
+    assert len(launched) == 2
+    with pytest.raises(ValueError):
+        call({**args, which: args[which].half()})
+    if which == "q_out":
+        with pytest.raises(ValueError):
+            call({**args, which: args[which].float()})
+    assert len(launched) == 2
