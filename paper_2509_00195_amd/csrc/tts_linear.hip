@@ -940,7 +940,7 @@ __global__ __launch_bounds__(kRmsThreads) void rms_wave_kernel(RmsParams p) {
 template <typename E, typename O>
 __global__ __launch_bounds__(kRmsThreads) void rms_long_kernel(RmsParams p) {
   __shared__ float red[2][kRmsThreads / 64];
-  const int pieces = (p.len + 7) / 8, tid = static_cast<int>(threadIdx.x);
+  const int pieces = (p.len - 1) / 8 + 1, tid = static_cast<int>(threadIdx.x);
   const auto count = [&](int at) { return at + 1 < pieces ? 8 : p.len - 8 * at; };
   const E* weight = static_cast<const E*>(p.weight);
   int turn = 0;  // (the sums' place alternates: one barrier per row)
