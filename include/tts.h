@@ -595,7 +595,8 @@ typedef struct {
 
 /* out[m][i] = x[m][i] / sqrt(mean of x[m]^2 + eps) * weight[i], in fp32,
  * rounded once (the squares are fp32 too: a row's sum of them has to lie below
- * 2^128). x, out [num_rows][row_len]; weight [row_len] or NULL (ones).
+ * 2^128; with an eps below 2^-120 all of it is in 64 bits, and rows may be of
+ * any magnitude). x, out [num_rows][row_len]; weight [row_len] or NULL (ones).
  * out may be x itself (same type and stride), and otherwise does not overlap it. */
 tts_status tts_rms_norm(const tts_norm_desc* d, int32_t num_rows, const void* x, int64_t x_stride, const void* weight,
                         void* out, int64_t out_stride, hipStream_t stream);

@@ -872,24 +872,28 @@ struct Piece {
       return __builtin_bit_cast(float, bits);
     }
   }
-  __device__ __forceinline__ float squares() const {
-    float s = 0.f;
+  template <typename T>
+  __device__ __forceinline__ T squares() const {
+    T s = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += at(i) * at(i);
+    for (int i = 0; i < 8; ++i) s += static_cast<T>(at(i)) * static_cast<T>(at(i));
     return s;
   }
 };
 
-template <typename E, typename O>
-__device__ __forceinline__ void rms_store(O* dst, int count, const Piece<E>& x, const Piece<E>& w, float scale) {
+template <typename T, typename E, typename O>
+__device__ __forceinline__ void rms_store(O* dst, int count, const Piece<E>& x, const Piece<E>& w, T scale) {
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = x.at(i) * scale * w.at(i);
+  for (int i = 0; i < 8; ++i) y[i] = static_cast<float>(static_cast<T>(x.at(i)) * scale * static_cast<T>(w.at(i)));
   store_row8(dst, count, y);
 }
 
 __device__ __forceinline__ float rms_scale(const RmsParams& p, float sum) {
   return 1.f / sqrtf(sum / static_cast<float>(p.len) + p.eps);
+}
+__device__ __forceinline__ double rms_scale(const RmsParams& p, double sum) {
+  return 1.0 / sqrt(sum / static_cast<double>(p.len) + static_cast<double>(p.eps));
 }
 
 // out[i] = x[i] / sqrt(mean of x^2 + eps) * weight[i]. Rows of whole pieces of
@@ -897,9 +901,16 @@ __device__ __forceinline__ float rms_scale(const RmsParams& p, float sum) {
 // stored, with no barrier, and the weights for all of the wave's rows. Bound by
 // memory (16384 rows of 3584 in bf16 41 us, a copy of as many bytes 47; with a
 // workgroup to a row, 55), for few rows by the launch.
+//
+// T, in which squares, sum, scale and products are: float where eps is at
+// least kRmsLeastEps. What squares lose below 2^-149 is then at most 2^-30 of
+// mean + eps. A smaller eps may leave the scale to a row whose squares vanish in
+// fp32, or whose scale passes its range: double (16384 rows of 3584 in bf16 56
+// us, in float 46; of 2048 27 and 25).
+constexpr float kRmsLeastEps = 0x1p-120f;
 constexpr int kRmsRows = kRmsThreads / 64;  // to a workgroup at a time
 
-template <typename E, typename O, int P>
+template <typename T, typename E, typename O, int P>
 __global__ __launch_bounds__(kRmsThreads) void rms_wave_kernel(RmsParams p) {
   const int pieces = p.len / 8, lane = static_cast<int>(threadIdx.x) % 64;
   const E* weight = static_cast<const E*>(p.weight);
@@ -919,16 +930,16 @@ __global__ __launch_bounds__(kRmsThreads) void rms_wave_kernel(RmsParams p) {
 #pragma unroll
     for (int i = 0; i < P; ++i)
       if (64 * i < pieces) held[i].load(x + at(i), 8);
-    float sum = 0.f;
+    T sum = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       if (64 * i >= pieces) continue;
-      const float s = held[i].squares();
-      sum += lane + 64 * i < pieces ? s : 0.f;
+      const T s = held[i].template squares<T>();
+      sum += lane + 64 * i < pieces ? s : 0;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    const float scale = rms_scale(p, sum);
+    const T scale = rms_scale(p, sum);
 #pragma unroll
     for (int i = 0; i < P; ++i)
       if (lane + 64 * i < pieces) rms_store(out + 8 * (lane + 64 * i), 8, held[i], w[i], scale);
@@ -937,9 +948,9 @@ __global__ __launch_bounds__(kRmsThreads) void rms_wave_kernel(RmsParams p) {
 
 // Other rows (and those of over 4096: 4096 rows of 6144 in 20.9 us, a wave to
 // each 25.4): a workgroup to each, which is read twice.
-template <typename E, typename O>
+template <typename T, typename E, typename O>
 __global__ __launch_bounds__(kRmsThreads) void rms_long_kernel(RmsParams p) {
-  __shared__ float red[2][kRmsThreads / 64];
+  __shared__ T red[2][kRmsThreads / 64];
   const int pieces = (p.len - 1) / 8 + 1, tid = static_cast<int>(threadIdx.x);
   const auto count = [&](int at) { return at + 1 < pieces ? 8 : p.len - 8 * at; };
   const E* weight = static_cast<const E*>(p.weight);
@@ -947,21 +958,21 @@ __global__ __launch_bounds__(kRmsThreads) void rms_long_kernel(RmsParams p) {
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
     const E* x = static_cast<const E*>(p.x) + row * p.x_stride;
     O* out = static_cast<O*>(p.out) + row * p.out_stride;
-    float sum = 0.f;
+    T sum = 0;
     Piece<E> piece, w;
     w.ones();
     for (int at = tid; at < pieces; at += kRmsThreads) {
       piece.load(x + 8 * at, count(at));
-      sum += piece.squares();
+      sum += piece.template squares<T>();
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if ((tid & 63) == 0) red[turn][tid / 64] = sum;
     __syncthreads();
-    sum = 0.f;
+    sum = 0;
 #pragma unroll
     for (int i = 0; i < kRmsThreads / 64; ++i) sum += red[turn][i];
-    const float scale = rms_scale(p, sum);
+    const T scale = rms_scale(p, sum);
     for (int at = tid; at < pieces; at += kRmsThreads) {
       piece.load(x + 8 * at, count(at));
       if (weight) w.load(weight + 8 * at, count(at));
@@ -1047,7 +1058,7 @@ hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, bool gat
                : launch_linear_t<float, false>(p, plan, aligned, stream);
 }
 
-template <typename E, typename O>
+template <typename T, typename E, typename O>
 static hipError_t launch_rms_t(const RmsParams& p, hipStream_t stream) {
   const dim3 block(kRmsThreads);
   // As many workgroups as run at once take the rows in turn.
@@ -1056,22 +1067,27 @@ static hipError_t launch_rms_t(const RmsParams& p, hipStream_t stream) {
   constexpr int kMost = 256 * 8;
   const dim3 grid(static_cast<unsigned>(groups < kMost ? groups : kMost));
   if (lane_pieces == 0 || lane_pieces > 8)
-    hipLaunchKernelGGL((rms_long_kernel<E, O>), dim3(static_cast<unsigned>(p.rows < kMost ? p.rows : kMost)), block, 0,
+    hipLaunchKernelGGL((rms_long_kernel<T, E, O>), dim3(static_cast<unsigned>(p.rows < kMost ? p.rows : kMost)), block, 0,
                        stream, p);
   else if (lane_pieces <= 2)
-    hipLaunchKernelGGL((rms_wave_kernel<E, O, 2>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((rms_wave_kernel<T, E, O, 2>), grid, block, 0, stream, p);
   else if (lane_pieces <= 4)
-    hipLaunchKernelGGL((rms_wave_kernel<E, O, 4>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((rms_wave_kernel<T, E, O, 4>), grid, block, 0, stream, p);
   else if (lane_pieces <= 6)
-    hipLaunchKernelGGL((rms_wave_kernel<E, O, 6>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((rms_wave_kernel<T, E, O, 6>), grid, block, 0, stream, p);
   else
-    hipLaunchKernelGGL((rms_wave_kernel<E, O, 8>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((rms_wave_kernel<T, E, O, 8>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
 
+template <typename T>
+static hipError_t launch_rms_of(const RmsParams& p, hipStream_t stream) {
+  if (p.in_bf16) return p.out_bf16 ? launch_rms_t<T, __bf16, __bf16>(p, stream) : launch_rms_t<T, __bf16, float>(p, stream);
+  return p.out_bf16 ? launch_rms_t<T, float, __bf16>(p, stream) : launch_rms_t<T, float, float>(p, stream);
+}
+
 hipError_t launch_rms(const RmsParams& p, hipStream_t stream) {
-  if (p.in_bf16) return p.out_bf16 ? launch_rms_t<__bf16, __bf16>(p, stream) : launch_rms_t<__bf16, float>(p, stream);
-  return p.out_bf16 ? launch_rms_t<float, __bf16>(p, stream) : launch_rms_t<float, float>(p, stream);
+  return p.eps >= kRmsLeastEps ? launch_rms_of<float>(p, stream) : launch_rms_of<double>(p, stream);
 }
 
 }  // namespace tts
