@@ -569,8 +569,8 @@ size_t tts_gated_linear_workspace_size(const tts_linear_desc* d, int32_t num_row
  *   that needs more than it is given is TTS_ERR_WORKSPACE); NULL allowed when
  *   that size is 0. Calls that overlap in time must not share one.
  * The order of the sums depends on the sizes and on the rows' alignment, not
- * on the values, and a call repeats itself bit for bit. Outputs whose tiles
- * pass one launch (2^32 threads) are TTS_ERR_UNSUPPORTED. */
+ * on the values, and a call repeats itself bit for bit. Outputs that pass one
+ * launch (2^32 threads) in every tile that there is are TTS_ERR_UNSUPPORTED. */
 tts_status tts_linear(const tts_linear_desc* d, int32_t num_rows, const void* x, int64_t x_stride, const void* w,
                       int64_t w_stride, const void* bias, const void* residual, int64_t residual_stride, void* out,
                       int64_t out_stride, void* workspace, size_t workspace_bytes, hipStream_t stream);

@@ -81,13 +81,11 @@ constexpr int64_t kMx4Units = 512;
 constexpr int32_t kMaxSeqLen = 0x7FFF0000;
 // Query heads of a rotating append: the parts of its grid stay below 65,536.
 constexpr int32_t kMaxRopeHeads = 8192;
-// Products: bytes of a row and 128-byte chunks stay inside int32, tiles of 512
-// threads inside one launch.
+// Products: bytes of a row and 128-byte chunks stay inside int32.
 constexpr int32_t kMaxInFeatures = 1 << 28;
 constexpr int32_t kMaxOutFeatures = 1 << 26;
 constexpr int64_t kMaxStride = int64_t{1} << 31;
 constexpr int64_t kMaxTileStride = int64_t{1} << 22;  // bytes; 256 rows of it and one more stay below 2^31
-constexpr int64_t kMaxLinearGroups = (int64_t{1} << 32) / 512 - 1;
 
 tts_status check_desc(const tts_attn_desc* d) {
   if (!d) return fail(TTS_ERR_INVALID_ARG, "desc is NULL");
@@ -1049,7 +1047,7 @@ static tts_status linear(const tts_linear_desc* d, int32_t num_rows, const void*
   const bool aligned = at(x, 16) && at(w0, 16) && at(w1, 16) && p.x_stride % 16 == 0 && p.w_stride % 16 == 0 &&
                        p.k_bytes % 16 == 0 && p.x_stride < kMaxTileStride && p.w_stride < kMaxTileStride;
   const tts::LinearPlan plan = tts::linear_plan(num_rows, p.n, p.k_bytes, f32, gated, aligned);
-  if (plan.groups > kMaxLinearGroups) return fail(TTS_ERR_UNSUPPORTED, "more tiles than one launch takes");
+  if (!plan.fits()) return fail(TTS_ERR_UNSUPPORTED, "more tiles than one launch takes");
   if (plan.workspace > 0) {
     if (!workspace || workspace_bytes < plan.workspace)
       return fail(TTS_ERR_WORKSPACE, "workspace too small: need " + std::to_string(plan.workspace) + " bytes");

@@ -15,23 +15,24 @@ constexpr int kLeastChunk = 2048;  // bytes of a row to a part, at least
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// A tile that has a kernel. resident: workgroups that a compute unit holds.
+// A tile that has a kernel. threads: of a workgroup. resident: workgroups that
+// a compute unit holds.
 // chunk: time of a chunk of the inner dimension, of one workgroup and of two
 // on a compute unit, while its loads keep up (measured; a few percent of which
 // the number of busy units makes).
 struct Tile {
-  int tile, bm, bn, resident;
+  int tile, bm, bn, threads, resident;
   double one, two;
 };
 
 // Large tiles of bf16 rows at multiples of 16 bytes: K 3584 (56 chunks) in 85 us
 // at 224 of 256 units (256 x 256), 50.6 at 224 (128 x 256), 31.9 at 180 (128 x
 // 128), 22.8 and 36.9 at 180 and 360 (64 x 128), less 3.5 for the launch.
-constexpr Tile kTiles[] = {{23, 256, 256, 1, 1.46, 0}, {33, 128, 256, 1, 0.84, 0}, {44, 128, 128, 1, 0.52, 0},
-                           {33, 64, 128, 2, 0.34, 0.60}};
+constexpr Tile kTiles[] = {{23, 256, 256, 512, 1, 1.46, 0}, {33, 128, 256, 512, 1, 0.84, 0},
+                           {44, 128, 128, 256, 1, 0.52, 0}, {33, 64, 128, 256, 2, 0.34, 0.60}};
 // The one for other rows, fp32 by its products (4096 cycles to a chunk), rows
 // that are not aligned by their way through registers.
-constexpr Tile kTileF32 = {22, 128, 128, 2, 1.75, 3.5}, kTileOdd = {22, 128, 128, 2, 1.5, 1.5};
+constexpr Tile kTileF32 = {22, 128, 128, 256, 2, 1.75, 3.5}, kTileOdd = {22, 128, 128, 256, 2, 1.5, 1.5};
 constexpr int kThinM[] = {16, 32, 64}, kThinN[] = {16, 32, 48, 64};
 
 constexpr double kLaunch = 3.5, kJoin = 3.0;  // launches
@@ -96,34 +97,30 @@ LinearPlan linear_plan(int32_t rows, int32_t n, int32_t k_bytes, bool f32, bool 
   const int planes = gated ? 2 : 1;
   const Shape s{rows, static_cast<int64_t>(n) * planes, k_bytes, f32, aligned};
   LinearPlan r{};
-  double best = 1e30;
-  const auto offer = [&](int tile, int bm, int bn, int chunk_bytes, int resident, double one, double two) {
-    int splits = 1;
-    const double t = best_splits(s, bm, bn, chunk_bytes, resident, one, two, &splits);
-    if (t < best) {
-      best = t;
-      r.tile = tile;
-      r.bm = bm;
-      r.bn = bn;
-      r.splits = splits;
+  double best = 0;
+  // (A tile whose workgroups pass one launch is taken only where all do.)
+  const auto offer = [&](const Tile& t, int chunk_bytes) {
+    LinearPlan q{t.tile, t.bm, t.bn, 1, 0, ceil_div(rows, t.bm) * ceil_div(s.cols, t.bn), t.threads, 0};
+    const double us = best_splits(s, t.bm, t.bn, chunk_bytes, t.resident, t.one, t.two, &q.splits);
+    if (r.threads == 0 || (q.fits() != r.fits() ? q.fits() : us < best)) {
+      best = us;
+      r = q;
     }
   };
-  const auto offer_tile = [&](const Tile& t) { offer(t.tile, t.bm, t.bn, kLinearChunk, t.resident, t.one, t.two); };
   if (f32 || !aligned)
-    offer_tile(f32 ? kTileF32 : kTileOdd);
+    offer(f32 ? kTileF32 : kTileOdd, kLinearChunk);
   else
-    for (const Tile& t : kTiles) offer_tile(t);
+    for (const Tile& t : kTiles) offer(t, kLinearChunk);
   for (int bm : kThinM)
     for (int bn : kThinN) {
       if (!thin_has(bm, bn, gated) || (bm > 16 && bm >= 2 * static_cast<int64_t>(rows))) continue;
       double one, two;
       thin_chunk(s, bm, bn, &one, &two);
-      offer(0, bm, bn, kThinChunk, 2, one, two);
+      offer({0, bm, bn, kThinThreads, 2, one, two}, kThinChunk);
     }
   const int64_t total = ceil_div(k_bytes, r.tile ? kLinearChunk : kThinChunk);
   r.chunks = static_cast<int>(ceil_div(total, r.splits));
   r.splits = static_cast<int>(ceil_div(total, r.chunks));
-  r.groups = ceil_div(rows, r.bm) * ceil_div(s.cols, r.bn);
   r.workspace = r.splits == 1 ? 0 : static_cast<size_t>(r.splits) * planes * rows * n * sizeof(float);
   return r;
 }

@@ -34,11 +34,15 @@ struct LinearPlan {
   int bm, bn;  // rows of x and rows of weights to a workgroup
   int splits, chunks;
   int64_t groups;  // workgroups of one split
+  int threads;     // of a workgroup
   size_t workspace;
+
+  bool fits() const { return groups * threads < int64_t{1} << 32; }  // (one launch's threads; split calls are smaller)
 };
 
 constexpr int kLinearChunk = 128;  // bytes of a row to a step of the large tiles
 constexpr int kThinChunk = 256;    // and of the small ones
+constexpr int kThinThreads = 256;  // of whose workgroups
 
 // The small tiles that there are. (64 x 48 has no third stage, and was slower
 // than 64 x 32 at every size; 64 x 16 was nowhere the best.)

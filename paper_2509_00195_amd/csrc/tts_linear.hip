@@ -303,8 +303,7 @@ __device__ __forceinline__ int place_of(int id, int places) {
 
 // ---- small tiles ---------------------------------------------------------------
 
-constexpr int kThinWaves = 4;
-constexpr int kThinThreads = 64 * kThinWaves;
+constexpr int kThinWaves = kThinThreads / 64;
 constexpr int kThinRow = kThinChunk;  // bytes of a row to a stage: a quarter to each wave
 
 // Few rows: bound by the weights' bytes and, where many workgroups read the
@@ -1016,7 +1015,7 @@ template <typename E, bool GATED, bool ALIGNED>
 static hipError_t launch_tiles(const LinearParams& p, const LinearPlan& plan, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(p.m_tiles * p.n_tiles * p.splits));
 #define TTS_TILE(BM, BN, WM, WN, SM, SN)                                                                                  \
-  if (plan.bm == BM && plan.bn == BN && plan.tile == 10 * SM + SN) {                                                       \
+  if (plan.bm == BM && plan.bn == BN && plan.tile == 10 * SM + SN && plan.threads == 64 * WM * WN) {                       \
     hipLaunchKernelGGL((tile_kernel<E, BM, BN, WM, WN, SM, SN, GATED, ALIGNED>), grid, dim3(64 * WM * WN), 0, stream, p); \
     return hipGetLastError();                                                                                              \
   }
