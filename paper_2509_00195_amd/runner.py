@@ -9,6 +9,7 @@ block_tables, seq_lens`` (device tensors) plus a ``shape`` carrying
 
 from __future__ import annotations
 
+from contextlib import nullcontext
 from typing import Optional
 
 import numpy as np
@@ -76,6 +77,17 @@ class PrefixAttention:
         return o
 
 
+def _on(stream, device):
+    """The context that makes a call's stream (one of torch's, a handle, or None) the current one."""
+    if stream is None:
+        return nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
+
+
+def _capturing() -> bool:
+    return torch.cuda.is_available() and torch.cuda.is_current_stream_capturing()
+
+
 class DecoderLayer:
     """One decoder layer over a paged cache: norm, projections, head norms with rotation and append, attention, output
     projection with its residual, norm, gated product, last projection with its residual. Every step is one call of
@@ -129,10 +141,7 @@ class DecoderLayer:
         elif meta is not None:
             need = _t.tts_prefix_decode_workspace_size(self.desc, meta)
         if need > ws.numel():
-            if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("the workspace grows with this call: make it once before capturing it")
-            self.outgrown.append(ws)
-            ws = self.ws = torch.empty(need, dtype=torch.uint8, device=ws.device)
+            ws = self._grow(need, stream)
         size, qkv, q, o, f = ws.numel(), self.qkv[:n], self.q[:n], self.o[:n], self.ffn[:n]
         _t.tts_rms_norm(self.norm, n, x, w["attn_norm"], self.normed, stream)
         _t.tts_linear(self.lin_qkv, n, self.normed, w["qkv"], qkv.flatten(1), w.get("qkv_bias"), None, ws, size, stream)
@@ -156,3 +165,14 @@ class DecoderLayer:
         _t.tts_gated_linear(self.lin_ffn, n, self.normed, w["gate"], w["up"], f, None, None, ws, size, stream)
         _t.tts_linear(self.lin_down, n, f, w["down"], x, None, x, ws, size, stream)
         return x
+
+    def _grow(self, need: int, stream):
+        """A larger workspace, of the memory that belongs to the call's stream: what another stream's work has left may
+        still be in use there."""
+        ws, captured = self.ws, _capturing()
+        with _on(stream, ws.device):
+            if captured or _capturing():
+                raise RuntimeError("the workspace grows with this call: make it once before capturing it")
+            self.outgrown.append(ws)
+            self.ws = torch.empty(need, dtype=torch.uint8, device=ws.device)
+        return self.ws

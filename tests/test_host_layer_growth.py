@@ -1,0 +1,58 @@
+"""When and where a decoder layer allocates a larger workspace (CPU: the calls are replaced)."""
+
+import contextlib
+
+import pytest
+import torch
+
+from paper_2509_00195_amd import runner
+from paper_2509_00195_amd import tts as T
+from tests.test_host_decoder_layer import HIDDEN, OFFS, ROOM, SEQS, TOKENS, _call, _layer, _short, made  # noqa: F401
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    """Streams that are only names: the current one, those that are capturing, and the one that each allocation is of."""
+    state = {"now": "current", "capturing": set(), "of": []}
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, state["now"] = state["now"], stream
+        try:
+            yield
+        finally:
+            state["now"] = before
+
+    empty = torch.empty
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: f"stream {handle}")
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state["now"] in state["capturing"])
+    monkeypatch.setattr(runner.torch, "empty", lambda *a, **kw: state["of"].append(state["now"]) or empty(*a, **kw))
+    return state
+
+
+@pytest.mark.parametrize("stream,of", [(None, "current"), ("side", "side"), (77, "stream 77"), (0, "stream 0")])
+def test_a_larger_workspace_is_of_the_calls_stream(made, streams, stream, of):
+    """Memory that the current stream's work has just left may still be in use there: only a call on that stream may be
+    given it."""
+    layer = _layer()
+    _short(layer)
+    streams["of"].clear()
+    _call(layer, TOKENS, tok_offsets=OFFS, stream=stream)
+    assert streams["of"] == [of] and streams["now"] == "current"
+
+
+@pytest.mark.parametrize("stream", [None, "side"])
+@pytest.mark.parametrize("which", ["current", "side"])
+def test_no_allocation_in_a_capture_on_either_stream(made, streams, stream, which):
+    layer = _layer()
+    _short(layer)
+    streams["capturing"] = {which}
+    streams["of"].clear()
+    if stream is None and which == "side":
+        _call(layer, TOKENS, tok_offsets=OFFS)
+        return
+    with pytest.raises(RuntimeError, match="before capturing"):
+        _call(layer, TOKENS, tok_offsets=OFFS, stream=stream)
+    assert not made and not streams["of"] and streams["now"] == "current"
