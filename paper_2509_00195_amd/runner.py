@@ -120,7 +120,8 @@ class DecoderLayer:
         self.lin_down = _t.make_linear(ffn, hidden, t, t)
         size = max(_t.tts_linear_workspace_size(x, max_tokens) for x in (self.lin_qkv, self.lin_out, self.lin_down))
         size = max(size, _t.tts_gated_linear_workspace_size(self.lin_ffn, max_tokens),
-                   _t.tts_paged_decode_workspace_size(desc, max_seqs, self.max_seq_len))
+                   _t.tts_paged_decode_workspace_size(desc, max_seqs, self.max_seq_len),
+                   _t.tts_paged_prefill_workspace_size(desc, max_seqs, max_tokens, self.max_seq_len))
         self.ws = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
         self.outgrown = []  # (graphs that were captured with them, and calls under way, still write to them)
 
@@ -168,11 +169,11 @@ class DecoderLayer:
 
     def _grow(self, need: int, stream):
         """A larger workspace, of the memory that belongs to the call's stream: what another stream's work has left may
-        still be in use there."""
+        still be in use there. It is twice as large at least, so that all that are kept are less than the last one."""
         ws, captured = self.ws, _capturing()
         with _on(stream, ws.device):
             if captured or _capturing():
                 raise RuntimeError("the workspace grows with this call: make it once before capturing it")
             self.outgrown.append(ws)
-            self.ws = torch.empty(need, dtype=torch.uint8, device=ws.device)
+            self.ws = torch.empty(max(need, 2 * ws.numel()), dtype=torch.uint8, device=ws.device)
         return self.ws

@@ -56,3 +56,22 @@ def test_no_allocation_in_a_capture_on_either_stream(made, streams, stream, whic
     with pytest.raises(RuntimeError, match="before capturing"):
         _call(layer, TOKENS, tok_offsets=OFFS, stream=stream)
     assert not made and not streams["of"] and streams["now"] == "current"
+
+
+def test_kept_workspaces_are_bounded(made, monkeypatch):
+    """A need that grows by a little from call to call: what is kept for earlier captures stays below what is used."""
+    layer = _layer()
+    _short(layer)
+    for need in range(1000, 200000, 64):
+        monkeypatch.setattr(runner._t, "tts_paged_prefill_workspace_size", lambda *a, _need=need: _need)
+        _call(layer, TOKENS, tok_offsets=OFFS)
+        assert layer.ws.numel() >= need
+    assert sum(ws.numel() for ws in layer.outgrown) <= layer.ws.numel() < 2 * 200000 and len(layer.outgrown) < 20
+
+
+def test_the_largest_prefill_has_room_from_the_start(made):
+    layer = _layer()
+    assert layer.ws.numel() >= T.tts_paged_prefill_workspace_size(layer.desc, SEQS, TOKENS, ROOM) > 0
+    ws = layer.ws
+    _call(layer, TOKENS, tok_offsets=OFFS)
+    assert layer.ws is ws and not layer.outgrown
