@@ -104,6 +104,7 @@ class DecoderLayer:
             raise ValueError("the attention's output must be of the queries' type")
         w = self.w = dict(weights)
         self.desc, self.rope, self.max_seq_len, self.num_blocks = desc, rope, int(max_seq_len), int(num_blocks)
+        self.max_seqs = int(max_seqs)
         hq, hkv, d, t = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.q_dtype
         hidden, ffn = int(w["qkv"].shape[1]), int(w["gate"].shape[0])
         dev, torch_t = w["qkv"].device, torch.float32 if t == _t.TTS_F32 else torch.bfloat16
@@ -141,6 +142,8 @@ class DecoderLayer:
             need = _t.tts_paged_prefill_workspace_size(self.desc, s, n, self.max_seq_len)
         elif meta is not None:
             need = _t.tts_prefix_decode_workspace_size(self.desc, meta)
+        elif s > self.max_seqs:
+            need = _t.tts_paged_decode_workspace_size(self.desc, s, self.max_seq_len)
         if need > ws.numel():
             ws = self._grow(need, stream)
         size, qkv, q, o, f = ws.numel(), self.qkv[:n], self.q[:n], self.o[:n], self.ffn[:n]

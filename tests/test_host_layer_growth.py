@@ -75,3 +75,12 @@ def test_the_largest_prefill_has_room_from_the_start(made):
     ws = layer.ws
     _call(layer, TOKENS, tok_offsets=OFFS)
     assert layer.ws is ws and not layer.outgrown
+
+
+def test_more_sequences_than_the_layer_was_made_for(made):
+    """A decode step of more sequences needs more partial states: they are allocated, not refused behind the append."""
+    layer = _layer()
+    n = SEQS + 4
+    x, cache = torch.zeros((n, HIDDEN), dtype=torch.bfloat16), torch.zeros(1, dtype=torch.bfloat16)
+    layer(x, cache, cache, torch.zeros((n, ROOM // 16), dtype=torch.int32), torch.ones(n, dtype=torch.int32))
+    assert layer.ws.numel() >= T.tts_paged_decode_workspace_size(layer.desc, n, ROOM) > 0
