@@ -129,7 +129,9 @@ class DecoderLayer:
     def __call__(self, x, k_cache, v_cache, block_tables, seq_lens, k_scale=None, v_scale=None, tok_offsets=None,
                  meta: Optional[_t.PrefixMeta] = None, stream=None):
         """x [tokens][hidden], replaced by the layer's output. Without ``tok_offsets`` every sequence has one new token,
-        and the attention is the paged call, or with ``meta`` the prefix-shared one; else it is the prefill. A call that
+        and the attention is the paged call, or with ``meta`` the prefix-shared one; else it is the prefill, which takes no
+        ``meta`` (one that is given is not used). Sizes that do not fit together are refused before anything is launched:
+        a call that has appended is not to be repeated. A call that
         needs a larger workspace than the calls before it allocates one: make it once before capturing it (a captured one
         raises). Calls of one layer, replayed ones too, must not overlap in time: they share its buffers."""
         w, ws, n, s = self.w, self.ws, int(x.shape[0]), int(seq_lens.shape[0])
@@ -138,12 +140,21 @@ class DecoderLayer:
         need = 0
         if n > self.normed.shape[0]:
             raise ValueError(f"{n} tokens in a layer made for {self.normed.shape[0]}")
+        if int(block_tables.shape[0]) < s:
+            raise ValueError(f"block_tables of {int(block_tables.shape[0])} sequences for {s}")
         if tok_offsets is not None:
+            if not isinstance(tok_offsets, int) and int(tok_offsets.shape[0]) <= s:
+                raise ValueError(f"tok_offsets has {int(tok_offsets.shape[0])} elements, {s} sequences need {s + 1}")
             need = _t.tts_paged_prefill_workspace_size(self.desc, s, n, self.max_seq_len)
+        elif n != s:
+            raise ValueError(f"{n} tokens for {s} sequences without tok_offsets")
         elif meta is not None:
+            self._check_meta(meta, s, cols)
             need = _t.tts_prefix_decode_workspace_size(self.desc, meta)
         elif s > self.max_seqs:
             need = _t.tts_paged_decode_workspace_size(self.desc, s, self.max_seq_len)
+        if self.max_seq_len > 16 * cols and (tok_offsets is not None or meta is None):
+            raise ValueError(f"block_tables of {cols} columns for sequences of up to {self.max_seq_len} tokens")
         if need > ws.numel():
             ws = self._grow(need, stream)
         size, qkv, q, o, f = ws.numel(), self.qkv[:n], self.q[:n], self.o[:n], self.ffn[:n]
@@ -169,6 +180,20 @@ class DecoderLayer:
         _t.tts_gated_linear(self.lin_ffn, n, self.normed, w["gate"], w["up"], f, None, None, ws, size, stream)
         _t.tts_linear(self.lin_down, n, f, w["down"], x, None, x, ws, size, stream)
         return x
+
+    def _check_meta(self, meta: _t.PrefixMeta, seqs: int, cols: int):
+        """The prefix-shared call refuses most of these itself, but behind the append."""
+        heads = lambda d: (d.num_q_heads, d.num_kv_heads, d.head_dim)  # noqa: E731
+        if not meta.handle:
+            raise ValueError("meta that has been destroyed")
+        if meta.num_seqs != seqs:
+            raise ValueError(f"meta of {meta.num_seqs} sequences for {seqs}")
+        if meta.q_len != 1:
+            raise ValueError("meta of a verification: a layer's step has one token for each sequence")
+        if meta.desc is None or heads(meta.desc) != heads(self.desc):
+            raise ValueError("meta made without a desc, or for other heads than the layer's")
+        if meta.max_blocks != cols or meta.num_blocks > self.num_blocks:
+            raise ValueError("meta of other block tables, or of more blocks than the layer's cache has")
 
     def _grow(self, need: int, stream):
         """A larger workspace, of the memory that belongs to the call's stream: what another stream's work has left may

@@ -254,11 +254,13 @@ def _as_i32p(a: np.ndarray):
 
 
 class PrefixMeta:
-    """Owning wrapper of a ``tts_prefix_meta*`` handle."""
+    """Owning wrapper of a ``tts_prefix_meta*`` handle, and the sizes of the batch that it is of."""
 
-    def __init__(self, handle: int, desc: Optional[tts_attn_desc]):
+    def __init__(self, handle: int, desc: Optional[tts_attn_desc], num_seqs: int, max_blocks: int, num_blocks: int,
+                 q_len: int = 1):
         self.handle = handle
         self.desc = desc
+        self.num_seqs, self.max_blocks, self.num_blocks, self.q_len = num_seqs, max_blocks, num_blocks, q_len
 
     def __del__(self):
         self.destroy()
@@ -290,7 +292,7 @@ def tts_build_prefix_meta(req_seq_offsets, block_tables, seq_lens, block_size: i
     _check(lib.tts_build_prefix_meta(offs.shape[0] - 1, _as_i32p(offs), s, _as_i32p(tables), maxb, _as_i32p(lens),
                                      block_size, num_blocks, C.byref(desc) if desc is not None else None,
                                      _stream(stream) if desc is not None else None, C.byref(h)))
-    return PrefixMeta(h.value, desc)
+    return PrefixMeta(h.value, desc, s, maxb, num_blocks)
 
 
 def tts_fork_prefix_meta(prev: PrefixMeta, req_seq_offsets, block_tables, seq_lens, block_size: int, num_blocks: int,
@@ -304,7 +306,7 @@ def tts_fork_prefix_meta(prev: PrefixMeta, req_seq_offsets, block_tables, seq_le
     h = C.c_void_p()
     _check(lib.tts_fork_prefix_meta(prev.handle, offs.shape[0] - 1, _as_i32p(offs), s, _as_i32p(tables), maxb,
                                     _as_i32p(lens), block_size, num_blocks, _stream(stream), C.byref(h)))
-    return PrefixMeta(h.value, prev.desc)
+    return PrefixMeta(h.value, prev.desc, s, maxb, num_blocks)
 
 
 def tts_truncated_lengths(child_parent, parent_lens, parent_spec, ratio: float, sigma: float, z) -> np.ndarray:
@@ -335,7 +337,7 @@ def tts_build_verify_meta(req_seq_offsets, block_tables, seq_lens, q_len: int, b
     _check(lib.tts_build_verify_meta(offs.shape[0] - 1, _as_i32p(offs), s, _as_i32p(tables), maxb, _as_i32p(lens),
                                      q_len, block_size, num_blocks, C.byref(desc) if desc is not None else None,
                                      _stream(stream) if desc is not None else None, C.byref(h)))
-    return PrefixMeta(h.value, desc)
+    return PrefixMeta(h.value, desc, s, maxb, num_blocks, q_len)
 
 
 def tts_prefix_meta_destroy(meta: PrefixMeta):
