@@ -106,7 +106,19 @@ class DecoderLayer:
         self.desc, self.rope, self.max_seq_len, self.num_blocks = desc, rope, int(max_seq_len), int(num_blocks)
         self.max_seqs = int(max_seqs)
         hq, hkv, d, t = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.q_dtype
+        for name in ("qkv", "gate"):
+            if w[name].dim() != 2:
+                raise ValueError(f"{name}: expected a matrix, got {tuple(w[name].shape)}")
         hidden, ffn = int(w["qkv"].shape[1]), int(w["gate"].shape[0])
+        for name, rows, cols in (("qkv", (hq + 2 * hkv) * d, hidden), ("out", hidden, hq * d), ("gate", ffn, hidden),
+                                 ("up", ffn, hidden), ("down", hidden, ffn)):
+            _t._matrix(w[name], rows, cols, t, name)
+        if _t._matrix(w["gate"], ffn, hidden, t, "gate")[1] != _t._matrix(w["up"], ffn, hidden, t, "up")[1]:
+            raise ValueError("gate and up must have one row stride")
+        for name in ("attn_norm", "ffn_norm"):
+            _t._vector(w[name], hidden, t, name)
+        for name, size in (("qkv_bias", (hq + 2 * hkv) * d), ("q_norm", d), ("k_norm", d)):
+            _t._vector(w.get(name), size, t, name)
         dev, torch_t = w["qkv"].device, torch.float32 if t == _t.TTS_F32 else torch.bfloat16
         empty = lambda *shape: torch.empty(shape, dtype=torch_t, device=dev)  # noqa: E731
         self.normed, self.qkv = empty(max_tokens, hidden), empty(max_tokens, hq + 2 * hkv, d)

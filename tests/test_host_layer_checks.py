@@ -80,3 +80,47 @@ def test_batches_that_do(made):
     _call(layer, n=TOKENS, tok_offsets=OFFS, meta=_meta(seqs=SEQS + 1))  # (the prefill takes no metadata)
     _call(layer, n=TOKENS, tok_offsets=1 << 20)  # (an address)
     assert len(made) == 32
+
+
+def _weights(**kw):
+    t = torch.bfloat16
+    w = dict(attn_norm=torch.ones(HIDDEN, dtype=t), qkv=torch.ones(((HQ + 2 * HKV) * D, HIDDEN), dtype=t),
+             out=torch.ones((HIDDEN, HQ * D), dtype=t), ffn_norm=torch.ones(HIDDEN, dtype=t),
+             gate=torch.ones((256, HIDDEN), dtype=t), up=torch.ones((256, HIDDEN), dtype=t),
+             down=torch.ones((HIDDEN, 256), dtype=t), qkv_bias=torch.ones((HQ + 2 * HKV) * D, dtype=t),
+             q_norm=torch.ones(D, dtype=t), k_norm=torch.ones(D, dtype=t))
+    w.update(kw)
+    return w
+
+
+def _made_of(w):
+    desc = T.make_desc(HQ, HKV, D, block_size=16, kv_dtype="bf16", out_dtype="bf16")
+    return runner.DecoderLayer(desc, w, None, TOKENS, SEQS, ROOM, BLOCKS)
+
+
+@pytest.mark.parametrize("name", ["attn_norm", "qkv", "out", "ffn_norm", "gate", "up", "down", "qkv_bias", "q_norm", "k_norm"])
+def test_weights_of_another_shape_or_type(name):
+    """At the start, not when a call has half run: the last product's weight was looked at behind the append."""
+    x = _weights()[name]
+    short = x[:-1] if name != "gate" else x[:, :-1]  # (the gate's rows give the layer its width)
+    for bad in (x.float(), x.half(), short):
+        with pytest.raises(ValueError, match=name):
+            _made_of(_weights(**{name: bad}))
+    if x.dim() == 2:
+        for bad in (x[:, :-1], x.t(), x.flatten()):
+            with pytest.raises(ValueError):
+                _made_of(_weights(**{name: bad}))
+
+
+def test_weights_that_fit():
+    _made_of(_weights())
+    _made_of(_weights(qkv_bias=None, q_norm=None, k_norm=None))
+    apart = torch.ones((256, HIDDEN + 8), dtype=torch.bfloat16)[:, :HIDDEN]
+    _made_of(_weights(gate=apart, up=apart))
+    with pytest.raises(ValueError, match="stride"):
+        _made_of(_weights(gate=apart))
+    for name in ("down", "ffn_norm"):
+        w = _weights()
+        del w[name]
+        with pytest.raises(KeyError):
+            _made_of(w)
