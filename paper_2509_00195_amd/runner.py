@@ -137,15 +137,19 @@ class DecoderLayer:
                    _t.tts_paged_prefill_workspace_size(desc, max_seqs, max_tokens, self.max_seq_len))
         self.ws = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
         self.outgrown = []  # (graphs that were captured with them, and calls under way, still write to them)
+        if dev.type == "cuda" and not _capturing():
+            # The buffers are the current stream's memory, where what had it before may be under way; a call may be on
+            # another stream.
+            torch.cuda.current_stream(dev).synchronize()
 
     def __call__(self, x, k_cache, v_cache, block_tables, seq_lens, k_scale=None, v_scale=None, tok_offsets=None,
                  meta: Optional[_t.PrefixMeta] = None, stream=None):
         """x [tokens][hidden], replaced by the layer's output. Without ``tok_offsets`` every sequence has one new token,
         and the attention is the paged call, or with ``meta`` the prefix-shared one; else it is the prefill, which takes no
         ``meta`` (one that is given is not used). Sizes that do not fit together are refused before anything is launched:
-        a call that has appended is not to be repeated. A call that
-        needs a larger workspace than the calls before it allocates one: make it once before capturing it (a captured one
-        raises). Calls of one layer, replayed ones too, must not overlap in time: they share its buffers."""
+        a call that has appended is not to be repeated. A call that needs a larger workspace than the calls before it
+        allocates one: make it once before capturing it (a captured one raises). Calls of one layer, replayed ones too,
+        must not overlap in time, since they share its buffers; the layer outlives them."""
         w, ws, n, s = self.w, self.ws, int(x.shape[0]), int(seq_lens.shape[0])
         hq, hkv, d = self.desc.num_q_heads, self.desc.num_kv_heads, self.desc.head_dim
         cols, cache, scales = int(block_tables.shape[1]), (k_cache, v_cache), (k_scale, v_scale)
