@@ -619,6 +619,8 @@ def _matrix(x, rows: int, cols: int, dtype: int, name: str):
     shape = x.shape
     if len(shape) != 2 or shape[1] != cols or shape[0] < rows:
         raise ValueError(f"{name}: expected [{rows}][{cols}], got {tuple(shape)}")
+    if rows > 0x7FFFFFFF:
+        raise ValueError(f"{name}: more than 2^31 - 1 rows")
     if dtype not in _TAKEN[x.dtype]:
         raise ValueError(f"{name}: elements of {x.dtype}")
     row, col = x.stride()

@@ -152,3 +152,17 @@ def test_appended_rows_of_another_type(launched, norm, which):
         with pytest.raises(ValueError):
             call({**args, which: args[which].float()})
     assert len(launched) == 2
+
+
+def test_more_rows_than_an_int32_holds(launched):
+    """2^32 + 1 rows would be passed on as one."""
+    n = (1 << 32) + 1
+    x = torch.empty((n, 1), dtype=BF16, device="meta")
+    w = torch.zeros((1, 1), dtype=BF16)
+    for call in (lambda: T.tts_linear(T.make_linear(1, 1), n, x, w, x), lambda: T.tts_rms_norm(T.make_norm(1), n, x, None, x),
+                 lambda: T.tts_gated_linear(T.make_linear(1, 1), n, x, w, w, x)):
+        with pytest.raises(ValueError, match="rows"):
+            call()
+    assert not launched
+    T.tts_rms_norm(T.make_norm(1), (1 << 31) - 1, x, None, x)
+    assert launched[0][1][1] == (1 << 31) - 1
