@@ -546,7 +546,10 @@ tts_status tts_truncated_lengths(int32_t num_children, const int32_t* child_pare
 typedef enum { TTS_ACT_NONE = 0, TTS_ACT_RELU = 1, TTS_ACT_SILU = 2, TTS_ACT_GELU = 3, TTS_ACT_GELU_TANH = 4 } tts_act;
 
 /* SiLU: y / (1 + exp(-y)); GELU: y Phi(y), Phi the normal distribution's
- * integral; its tanh form: y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) / 2. */
+ * integral; its tanh form: y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) / 2.
+ * In fp32, from y in fp32. An exponential's argument is rounded, so that a
+ * result is off by up to 2^-20 + c 2^-23 of itself, c being |y| for SiLU, y^2
+ * for GELU and 4 |y| + |y|^3 for the tanh form; below 2^-120 it may be 0. */
 typedef struct {
   int32_t in_features;  /* K, 1 .. 2^28 */
   int32_t out_features; /* N, 1 .. 2^26 */
