@@ -67,7 +67,6 @@ class tts_rope_desc(C.Structure):
 class tts_head_norm_desc(C.Structure):
     _fields_ = [("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
     held = (None, None)  # the weights' tensors, where they are known (make_head_norm)
-    fits = None  # the heads that they have been found to fit: (dims, type)
 
 
 class tts_linear_desc(C.Structure):
@@ -486,10 +485,12 @@ def _rows(x, heads: int, head_dim: int, tokens: int = 0, dtype: Optional[int] = 
     of them, of elements of a type (None: any)."""
     if x is None:
         return None, 0
-    if isinstance(x, int):
-        return x, heads * head_dim
     try:
         n, h, d = x.shape
+    except AttributeError:
+        if not isinstance(x, int):
+            raise
+        return x, heads * head_dim
     except ValueError:
         n, h, d = 0, 0, 0
     if h != heads or d != head_dim:
@@ -545,7 +546,7 @@ def make_head_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> tts_head_
     """Head norms with device weights [head_dim] in the queries' type (None: ones). Tensors are kept with the descriptor,
     and the calls that take it check that they fit."""
     norm = tts_head_norm_desc(float(eps), _ptr(q_weight), _ptr(k_weight))
-    norm.held = q_weight, k_weight
+    norm.held = None if isinstance(q_weight, int) else q_weight, None if isinstance(k_weight, int) else k_weight
     return norm
 
 
@@ -555,11 +556,12 @@ def tts_norm_rope_append_kv(desc: tts_attn_desc, norm: tts_head_norm_desc, num_s
                             tok_offsets=None, positions=None, stream=None):
     """Tensors as for tts_rope_append_kv."""
     hq, hkv, d, t = desc.num_q_heads, desc.num_kv_heads, desc.head_dim, desc.q_dtype
-    if norm is not None and norm.fits != (d, t):
-        for w, name in zip(norm.held, ("q_weight", "k_weight")):
-            if w is not None and type(w) is not int and (w.numel() < d or t not in _TAKEN[w.dtype]):
-                raise ValueError(f"{name} is not a vector of {d} elements of the queries' type")
-        norm.fits = d, t
+    if norm is not None:
+        qw, kw = norm.held
+        if qw is not None and (qw.numel() < d or t not in _TAKEN[qw.dtype]):
+            raise ValueError(f"q_weight is not a vector of {d} elements of the queries' type")
+        if kw is not None and (kw.numel() < d or t not in _TAKEN[kw.dtype]):
+            raise ValueError(f"k_weight is not a vector of {d} elements of the queries' type")
     qp, qs = _rows(q, hq, d, num_tokens, t)
     kp, ks = _rows(k_new, hkv, d, num_tokens, t)
     vp, vs = _rows(v_new, hkv, d, num_tokens, t)
