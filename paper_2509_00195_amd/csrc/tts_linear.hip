@@ -497,18 +497,19 @@ __global__ __launch_bounds__(kThinThreads) void thin_kernel(LinearParams p) {
 
 // Many rows: BM rows of x by BN rows of weights to a workgroup of WM x WN
 // waves, whose sums stay in registers, with SM and SN stages of the operands in
-// LDS. Bound by the matrix instructions, on long calls by the power that they
-// draw (the clock falls to 1.5 to 1.9 GHz), in smaller ones by the bytes that a
-// unit draws from its L2, which a larger tile halves. Measured (bf16): 8192 x
-// 3584 x 28672 (gated, 256 x 256) 1,305 us or 1,290 TFLOP/s, a large product of
-// the library 1,290 to 1,560; 8192 x 3584 x 3584 184 us with a residual from
-// memory, where 448 tiles take two rounds of 256 units; 320 x 14336 x 3584
-// (128 x 256 in six parts) 40 and 7 for joining them; 64 x 3584 x 14336 gated
-// (64 x 128) 42, its weights 41 at a copy's rate. Weights have a third stage
-// beside x's two in the largest tile, all that LDS holds: a load that comes late
-// then stops nothing. Instructions of 32 x 32 x 16 were slower (1,388 us against
-// 1,350: more power), so was a tile for four waves of 128 x 128 (the compiler
-// spills: it lets the sums' registers change).
+// LDS. Bound on long calls by the matrix instructions, at a clock that falls to
+// 1.84 GHz under them, and by the waits at a chunk's barrier: the matrix cores
+// are busy 0.63 of the time, the waves wait 0.32 of theirs. In smaller calls
+// bound by the bytes that a unit draws from its L2, which a larger tile halves.
+// Measured (bf16): 8192 x 3584 x 28672 (gated, 256 x 256) 1,285 us or 1,310
+// TFLOP/s, a large product of the library 1,290 to 1,560; 8192 x 3584 x 3584 182
+// us with a residual from memory, where 448 tiles take two rounds of 256 units;
+// 320 x 14336 x 3584 (128 x 256 in six parts) 52 in all, 7 of them for joining
+// the parts; 64 x 3584 x 14336 gated (64 x 128) 43, its weights 41 at a copy's
+// rate. Weights have a third stage beside x's two in the largest tile, all that
+// LDS holds: a load that comes late then stops nothing. Instructions of 32 x 32
+// x 16 were slower (1,388 us against 1,350), so was a tile for four waves of
+// 128 x 128 (the compiler spills: it lets the sums' registers change).
 //
 // A tile's rows lie in LDS 128 bytes each, in eight pieces of 16 whose places
 // are permuted by the row (piece c of row r at c ^ (r & 7)), so that the same
@@ -898,7 +899,7 @@ __device__ __forceinline__ double rms_scale(const RmsParams& p, double sum) {
 // out[i] = x[i] / sqrt(mean of x^2 + eps) * weight[i]. Rows of whole pieces of
 // 8, at most P to a lane: a wave to a row, which stays in registers as it is
 // stored, with no barrier, and the weights for all of the wave's rows. Bound by
-// memory (16384 rows of 3584 in bf16 41 us, a copy of as many bytes 47; with a
+// memory (16384 rows of 3584 in bf16 46 us, a copy of as many bytes 47; with a
 // workgroup to a row, 55), for few rows by the launch.
 //
 // T, in which squares, sum, scale and products are: float where eps is at
