@@ -78,10 +78,11 @@ class PrefixAttention:
 
 
 def _on(stream, device):
-    """The context that makes a call's stream (one of torch's, a handle, or None) the current one."""
+    """The context that makes a call's stream (a handle, what has one as the calls take it, or None) the current one."""
     if stream is None:
         return nullcontext()
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
+    handle = stream if isinstance(stream, int) else stream.cuda_stream
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle, device=device))
 
 
 def _capturing() -> bool:

@@ -1,6 +1,7 @@
 """When and where a decoder layer allocates a larger workspace (CPU: the calls are replaced)."""
 
 import contextlib
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -32,7 +33,10 @@ def streams(monkeypatch):
     return state
 
 
-@pytest.mark.parametrize("stream,of", [(None, "current"), ("side", "side"), (77, "stream 77"), (0, "stream 0")])
+SIDE = SimpleNamespace(cuda_stream=5)
+
+
+@pytest.mark.parametrize("stream,of", [(None, "current"), (SIDE, "stream 5"), (77, "stream 77"), (0, "stream 0")])
 def test_a_larger_workspace_is_of_the_calls_stream(made, streams, stream, of):
     """Memory that the current stream's work has just left may still be in use there: only a call on that stream may be
     given it."""
@@ -43,14 +47,14 @@ def test_a_larger_workspace_is_of_the_calls_stream(made, streams, stream, of):
     assert streams["of"] == [of] and streams["now"] == "current"
 
 
-@pytest.mark.parametrize("stream", [None, "side"])
-@pytest.mark.parametrize("which", ["current", "side"])
+@pytest.mark.parametrize("stream", [None, SIDE])
+@pytest.mark.parametrize("which", ["current", "stream 5"])
 def test_no_allocation_in_a_capture_on_either_stream(made, streams, stream, which):
     layer = _layer()
     _short(layer)
     streams["capturing"] = {which}
     streams["of"].clear()
-    if stream is None and which == "side":
+    if stream is None and which == "stream 5":
         _call(layer, TOKENS, tok_offsets=OFFS)
         return
     with pytest.raises(RuntimeError, match="before capturing"):
