@@ -203,13 +203,14 @@ class DecoderLayer:
         heads = lambda d: (d.num_q_heads, d.num_kv_heads, d.head_dim)  # noqa: E731
         if not meta.handle:
             raise ValueError("meta that has been destroyed")
-        if meta.num_seqs != seqs:
-            raise ValueError(f"meta of {meta.num_seqs} sequences for {seqs}")
+        held = meta.export()["num_seqs"] if meta.num_seqs is None else meta.num_seqs
+        if held != seqs:
+            raise ValueError(f"meta of {held} sequences for {seqs}")
         if meta.q_len != 1:
             raise ValueError("meta of a verification: a layer's step has one token for each sequence")
         if meta.desc is None or heads(meta.desc) != heads(self.desc):
             raise ValueError("meta made without a desc, or for other heads than the layer's")
-        if meta.max_blocks != cols or meta.num_blocks > self.num_blocks:
+        if (meta.max_blocks or cols) != cols or (meta.num_blocks or 0) > self.num_blocks:
             raise ValueError("meta of other block tables, or of more blocks than the layer's cache has")
 
     def _grow(self, need: int, stream):

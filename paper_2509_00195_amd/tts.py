@@ -253,10 +253,10 @@ def _as_i32p(a: np.ndarray):
 
 
 class PrefixMeta:
-    """Owning wrapper of a ``tts_prefix_meta*`` handle, and the sizes of the batch that it is of."""
+    """Owning wrapper of a ``tts_prefix_meta*`` handle, and the sizes of the batch that it is of (where they are known)."""
 
-    def __init__(self, handle: int, desc: Optional[tts_attn_desc], num_seqs: int, max_blocks: int, num_blocks: int,
-                 q_len: int = 1):
+    def __init__(self, handle: int, desc: Optional[tts_attn_desc], num_seqs: Optional[int] = None,
+                 max_blocks: Optional[int] = None, num_blocks: Optional[int] = None, q_len: int = 1):
         self.handle = handle
         self.desc = desc
         self.num_seqs, self.max_blocks, self.num_blocks, self.q_len = num_seqs, max_blocks, num_blocks, q_len

@@ -65,6 +65,19 @@ def test_tables_shorter_than_the_longest_sequence(made, kw):
     assert not made
 
 
+def test_metadata_wrapped_by_hand(prefix):
+    """A handle without the sizes of its batch: how many beams it is of is asked of it."""
+    layer, meta = _layer(), _meta()
+    _call(layer, meta=T.PrefixMeta(meta.handle, meta.desc))
+    assert len(prefix) == 8
+    more = _meta(seqs=SEQS + 1)
+    for m in (meta, more):
+        m.destroy = lambda: None
+    with pytest.raises(ValueError, match="meta"):
+        _call(layer, meta=T.PrefixMeta(more.handle, more.desc))
+    assert len(prefix) == 8
+
+
 def test_metadata_that_has_been_destroyed(prefix):
     meta = _meta()
     meta.destroy()
