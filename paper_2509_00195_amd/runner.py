@@ -148,7 +148,8 @@ class DecoderLayer:
         """x [tokens][hidden], replaced by the layer's output. Without ``tok_offsets`` every sequence has one new token,
         and the attention is the paged call, or with ``meta`` the prefix-shared one; else it is the prefill, which takes no
         ``meta`` (one that is given is not used). Sizes that do not fit together are refused before anything is launched:
-        a call that has appended is not to be repeated. A call that needs a larger workspace than the calls before it
+        a call that has appended is not to be repeated. Tokens behind the last offset (padded batches) reach no other row
+        and no cache; their own rows of x hold no result. A call that needs a larger workspace than the calls before it
         allocates one: make it once before capturing it (a captured one raises). Calls of one layer, replayed ones too,
         must not overlap in time, since they share its buffers; the layer outlives them."""
         w, ws, n, s = self.w, self.ws, int(x.shape[0]), int(seq_lens.shape[0])

@@ -79,3 +79,26 @@ def test_prompts_then_decode_steps_of_heads_of_128(kind, monkeypatch):
 
     monkeypatch.setattr(M, "D", 128)
     M.test_prompts_then_decode_steps(kind, True)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_a_padded_batch(kind):
+    """Rows behind the last offset reach nothing: neither the sequences' rows nor the caches depend on what they hold."""
+    from tests.test_gpu_layer import HIDDEN as WIDTH
+    from tests.test_gpu_layer import Model
+
+    new = [5, 0, 20, 1]
+    offs = torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)).to(DEV)
+    found = []
+    for fill in (0.0, float("nan"), float("inf"), 3.0):
+        m = Model(kind, 4, 5)
+        m.lens += torch.tensor([40, 7, 60, 33], dtype=torch.int32, device=DEV)
+        x = torch.full((sum(new) + 6, WIDTH), fill, dtype=torch.bfloat16, device=DEV)
+        x[:sum(new)] = m.hidden(sum(new))
+        m.layer.o.fill_(fill)
+        m.run(x, offs)
+        torch.cuda.synchronize()
+        found.append([x[:sum(new)].clone(), *(t.clone() for t in m.dev if t is not None)])
+    assert bool(torch.isfinite(found[0][0]).all())
+    for other in found[1:]:
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(found[0], other))
